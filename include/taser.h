@@ -450,6 +450,133 @@ int taser_selector_scores(const taser_selector* s, uint32_t* scores, uint64_t* t
 int taser_selector_size(const taser_selector* s, int64_t* n);
 void taser_selector_free(taser_selector* s);
 
+/* ---------------------------------------------------------------------------
+ * Attention to states of another length, with a learned bias by distance: a
+ * root's aggregation of its sampled neighbors, a decoder's of an encoder's
+ * states, one token's of many.
+ *
+ * For batch entry b, query i, query head h with key head h' = h / (heads / kv_heads):
+ *   x[j]   = scale * <q[b][i][h], k[b][j][h']> + bias_table[h][bucket(b, i, j)]
+ *   out[b][i][h] = sum over j of softmax(x)[j] * v[b][j][h']
+ * over the states j < lengths[b] (clamped to [0, keys]; `keys` where lengths is
+ * NULL) with mask[b][j] != 0 (where given). Other states are not read: whatever
+ * is in their place changes nothing. A query without any state gives zeros.
+ *   bucket(b, i, j) = the number of `bounds` <= query_pos[b][i] - key_pos[b][j]
+ * (bounds ascend; positions below 2^62 in magnitude: token numbers, or query
+ * and interaction times). bias_table NULL: no bias. A table entry of minus
+ * infinity takes its distances out.
+ *   type           of q, k, v, bias_table, out and the gradients
+ *   *_strides      in elements: batch entry, token, head; elements are adjacent
+ *   lengths        device int32[batch] or NULL
+ *   mask           device uint8[batch][keys], entry b at b * mask_stride; or NULL
+ *   bias_table     device [heads][buckets], buckets in [1, TASER_MAX_BUCKETS],
+ *                  (heads / kv_heads) * buckets <= TASER_MAX_GROUP_BUCKETS
+ *   bounds         device int64[buckets - 1]
+ *   query_pos, key_pos  device int64, entry b at b * *_pos_stride (0: the same for all)
+ *   head_dim in [1, TASER_MAX_HEAD_DIM], scale > 0; queries, keys, batch may be 0
+ *
+ * taser_cross_attention: out dense [batch][queries][heads][head_dim]; stats
+ *   float[batch][queries][heads][TASER_ATTENTION_STATS(type, head_dim)] or NULL:
+ *   the largest x of a row (minus infinity: none), the sum of exp(x - largest),
+ *   then what only the gradient reads (how far 16-bit outputs were rounded).
+ * taser_cross_attention_grad: the gradients of sum(out * dout): dq dense like
+ *   out, dk and dv dense [batch][keys][kv_heads][head_dim] (zeros for states
+ *   that took no part), dtable [heads][buckets] (NULL without a bias). q .. v,
+ *   lengths .. and out, stats must be those of the forward call; dout dense.
+ *   Sums have a fixed order: the same call gives the same bits.
+ * Both work in `work`, device memory of the caller's (16-byte aligned, contents
+ * arbitrary, free again when the call's kernels have run), as much as
+ * taser_cross_attention_bytes says (either out-pointer may be NULL) for the
+ * same block. Both only launch kernels.
+ * Sums, softmax statistics and bias are held in 32 bits; softmax weights and
+ * their gradients are rounded to `type` where they enter a matrix product.
+ * ------------------------------------------------------------------------- */
+enum taser_type { TASER_F32 = 0, TASER_F16 = 1, TASER_BF16 = 2 };
+
+#define TASER_MAX_HEAD_DIM 128
+#define TASER_MAX_BUCKETS 64
+#define TASER_MAX_GROUP_BUCKETS 4096
+#define TASER_ATTENTION_STATS(type, head_dim) (2 + ((type) == TASER_F32 ? 0 : ((head_dim) + 1) / 2))
+
+typedef struct taser_attention {
+    int32_t type, heads, kv_heads, head_dim;
+    int64_t batch, queries, keys;
+    float scale;
+    int32_t buckets;
+    const void *q, *k, *v;
+    int64_t q_strides[3], k_strides[3], v_strides[3];
+    const int32_t* lengths;
+    const uint8_t* mask;
+    int64_t mask_stride;
+    const void* bias_table;
+    const int64_t *bounds, *query_pos, *key_pos;
+    int64_t query_pos_stride, key_pos_stride;
+} taser_attention;
+
+int taser_cross_attention_bytes(const taser_attention* a, uint64_t* work_bytes, uint64_t* grad_work_bytes);
+int taser_cross_attention(const taser_attention* a, void* out, float* stats, void* work, uint64_t work_bytes,
+                          void* hip_stream);
+int taser_cross_attention_grad(const taser_attention* a, const void* out, const float* stats, const void* dout,
+                               void* dq, void* dk, void* dv, void* dtable, void* work, uint64_t work_bytes,
+                               void* hip_stream);
+
+/* The bias by itself, for a model that adds it to scores of its own:
+ *   bias[b][h][i][j] = table[h][bucket(b, i, j)]                     dense
+ *   dtable[h][u] = sum of dbias[b][h][i][j] over bucket(b, i, j) = u
+ * Positions, bounds and buckets as above. dbias has strides in elements (batch
+ * entry, head, query; states are adjacent). taser_relative_bias_grad works in
+ * `work` (16-byte aligned, as much as taser_relative_bias_bytes says) and sums
+ * in 32 bits in a fixed order. Both only launch kernels. */
+typedef struct taser_distances {
+    int32_t type, heads, buckets;
+    int64_t batch, queries, keys;
+    const int64_t *bounds, *query_pos, *key_pos;
+    int64_t query_pos_stride, key_pos_stride;
+} taser_distances;
+
+int taser_relative_bias_bytes(const taser_distances* d, uint64_t* work_bytes);
+int taser_relative_bias(const taser_distances* d, const void* table, void* bias, void* hip_stream);
+int taser_relative_bias_grad(const taser_distances* d, const void* dbias, const int64_t dbias_strides[3],
+                             void* dtable, void* work, uint64_t work_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Clipped policy loss with a KL term, forward and backward in one pass over the
+ * logits: the adaptive sampler's choice of n of m candidates (Alg. 1: sel of
+ * taser_select_weighted as the actions), or a token model's of one of many.
+ *
+ * Row r has `width` logits, of which the first count[r] (clamped to [0, width];
+ * all where count is NULL) take part; the rest is not read. For action a =
+ * actions[r][j] with 0 <= a < count[r]:
+ *   logp  = logit[a] - log(sum over the row of exp(logit))
+ *   ratio = exp(logp - old_logp)       (old_logp NULL: ratio is 1, its gradient
+ *                                       logp's, and nothing is clipped)
+ *   apart = ref_logp - logp            (ref_logp NULL: no such term)
+ *   loss  = weight * (-min(ratio * advantage,
+ *                          clip(ratio, 1 - clip_low, 1 + clip_high) * advantage)
+ *                     + kl * (exp(apart) - apart - 1))
+ * and 0 for any other action (-1: none), whose logp is 0 too. weight NULL: 1.
+ * grad[r][c] = the derivative of the sum of all losses (zeros past count[r]);
+ * where ratio * advantage is not the smaller of the two, the first term has none.
+ *   logits  device, type, row r at r * logits_stride elements
+ *   actions int32[rows][picks]; advantage, old_logp, ref_logp, weight, loss, logp
+ *           float[rows][picks]; count int32[rows]; grad dense [rows][width] of
+ *           the logits' type, or NULL                                   device
+ *   width in [1, 2^31), picks in [1, TASER_MAX_PICKS], rows >= 0
+ * Only launches kernels.
+ * ------------------------------------------------------------------------- */
+#define TASER_MAX_PICKS 64
+
+typedef struct taser_policy_batch {
+    int32_t type, picks;
+    int64_t rows, width, logits_stride;
+    const void* logits;
+    const int32_t *count, *actions;
+    const float *advantage, *old_logp, *ref_logp, *weight;
+    float clip_low, clip_high, kl;
+} taser_policy_batch;
+
+int taser_policy_loss(const taser_policy_batch* p, float* loss, float* logp, void* grad, void* hip_stream);
+
 /* Message for the most recent error on the calling thread (static storage). */
 const char* taser_last_error(void);
 

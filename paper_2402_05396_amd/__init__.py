@@ -23,12 +23,15 @@ LIB_PATH = os.path.join(_HERE, "libtaser.so")
 RECENT, UNIFORM, WEIGHTED, INVERSE_TIMESPAN = 0, 1, 2, 3
 INPUT_ON_DEVICE = 1
 MAX_K, MAX_M, MAX_HOPS = 64, 64, 3
+MAX_HEAD_DIM, MAX_BUCKETS, MAX_PICKS = 128, 64, 64
 
 EXPORTS = ("taser_tcsr_build", "taser_tcsr_build_bytes", "taser_tcsr_build_in", "taser_tcsr_size", "taser_tcsr_view", "taser_tcsr_free", "taser_sample_temporal", "taser_sample_temporal_rows",
            "taser_candidate_encodings", "taser_select_weighted", "taser_gather_features", "taser_cache_init", "taser_cache_lookup", "taser_cache_lookup_static", "taser_cache_prefetch", "taser_cache_gather", "taser_cache_tune", "taser_cache_count_accesses", "taser_cache_access_counts",
            "taser_cache_epoch_end", "taser_cache_residents",
            "taser_cache_free", "taser_selector_init", "taser_selector_draw", "taser_selector_update",
-           "taser_selector_scores", "taser_selector_size", "taser_selector_free", "taser_profile_begin", "taser_profile_begin_only", "taser_profile_end", "taser_last_error")
+           "taser_selector_scores", "taser_selector_size", "taser_selector_free",
+           "taser_cross_attention", "taser_cross_attention_bytes", "taser_cross_attention_grad", "taser_relative_bias", "taser_relative_bias_bytes",
+           "taser_relative_bias_grad", "taser_policy_loss", "taser_profile_begin", "taser_profile_begin_only", "taser_profile_end", "taser_last_error")
 
 
 class TaserError(RuntimeError):
@@ -44,6 +47,25 @@ class _KernelTime(ctypes.Structure):
 class _HopOut(ctypes.Structure):
     _fields_ = [("nbr", ctypes.c_void_p), ("eid", ctypes.c_void_p), ("ts", ctypes.c_void_p),
                 ("count", ctypes.c_void_p)]
+
+
+class _Attention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("type", "heads", "kv_heads", "head_dim")] + [(n, ctypes.c_int64) for n in ("batch", "queries", "keys")] +
+                [("scale", ctypes.c_float), ("buckets", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in ("q", "k", "v")] +
+                [(n, ctypes.c_int64 * 3) for n in ("q_strides", "k_strides", "v_strides")] + [("lengths", ctypes.c_void_p), ("mask", ctypes.c_void_p)] +
+                [("mask_stride", ctypes.c_int64)] + [(n, ctypes.c_void_p) for n in ("bias_table", "bounds", "query_pos", "key_pos")] +
+                [("query_pos_stride", ctypes.c_int64), ("key_pos_stride", ctypes.c_int64)])
+
+
+class _Distances(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("type", "heads", "buckets")] + [(n, ctypes.c_int64) for n in ("batch", "queries", "keys")] +
+                [(n, ctypes.c_void_p) for n in ("bounds", "query_pos", "key_pos")] + [("query_pos_stride", ctypes.c_int64), ("key_pos_stride", ctypes.c_int64)])
+
+
+class _PolicyBatch(ctypes.Structure):
+    _fields_ = ([("type", ctypes.c_int32), ("picks", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("rows", "width", "logits_stride")] +
+                [(n, ctypes.c_void_p) for n in ("logits", "count", "actions", "advantage", "old_logp", "ref_logp", "weight")] +
+                [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "kl")])
 
 
 _lib = None
@@ -92,6 +114,14 @@ def lib():
         L.taser_selector_size.argtypes = [vp, ctypes.POINTER(i64)]
         L.taser_selector_free.argtypes = [vp]
         L.taser_selector_free.restype = None
+        A, D, P = ctypes.POINTER(_Attention), ctypes.POINTER(_Distances), ctypes.POINTER(_PolicyBatch)
+        L.taser_cross_attention_bytes.argtypes = [A, ctypes.POINTER(u64), ctypes.POINTER(u64)]
+        L.taser_cross_attention.argtypes = [A, vp, vp, vp, u64, vp]
+        L.taser_cross_attention_grad.argtypes = [A, vp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
+        L.taser_relative_bias_bytes.argtypes = [D, ctypes.POINTER(u64)]
+        L.taser_relative_bias.argtypes = [D, vp, vp, vp]
+        L.taser_relative_bias_grad.argtypes = [D, vp, ctypes.POINTER(i64), vp, vp, u64, vp]
+        L.taser_policy_loss.argtypes = [P, vp, vp, vp, vp]
         L.taser_profile_begin.argtypes = []
         L.taser_profile_begin_only.argtypes = [ctypes.c_char_p]
         L.taser_profile_end.argtypes = [ctypes.POINTER(_KernelTime), i32, ctypes.POINTER(i32)]
@@ -608,6 +638,212 @@ def selector_size(s):
 
 def selector_free(s):
     s.free()
+
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _strided(t, dims, dtype, name, device=None):
+    """A device tensor of `dims` dimensions whose last one is adjacent in memory."""
+    types = (dtype,) if isinstance(dtype, torch.dtype) else tuple(dtype)
+    if t.dtype not in types or t.dim() != dims or not t.is_cuda or (t.shape[-1] > 1 and t.stride(-1) != 1) or (device is not None and t.device != device):
+        raise TypeError(f"{name}: expected a {dims}-dimensional device tensor of {' or '.join(map(str, types))}, elements of the last dimension adjacent")
+    return t
+
+
+def _positions(pos, batch, n, name, device):
+    """int64[batch or 1, n] -> stride of a batch entry in elements."""
+    _strided(pos, 2, torch.int64, name, device)
+    if pos.shape[1] != n or pos.shape[0] not in (1, batch):
+        raise ValueError(f"{name}: expected [{batch} or 1, {n}]")
+    return pos.stride(0) if pos.shape[0] > 1 else 0
+
+
+def _attention_block(q, k, v, lengths, mask, bias, scale):
+    _strided(q, 4, _TYPES, "q")
+    for t, name in ((k, "k"), (v, "v")):
+        _strided(t, 4, q.dtype, name, q.device)
+    batch, queries, heads, dim = q.shape
+    keys, kv_heads = k.shape[1], k.shape[2]
+    if k.shape != v.shape or k.shape[0] != batch or k.shape[3] != dim:
+        raise ValueError("q must be [B, queries, heads, d], k and v [B, keys, kv_heads, d]")
+    a = _Attention(_TYPES[q.dtype], heads, kv_heads, dim, batch, queries, keys, dim ** -0.5 if scale is None and dim else scale or 0.0, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                   q.stride()[:3], k.stride()[:3], v.stride()[:3])
+    if lengths is not None:
+        _want(lengths, torch.int32, "lengths")
+        if lengths.numel() != batch:
+            raise ValueError("lengths must hold a number for each batch entry")
+        a.lengths = lengths.data_ptr()
+    if mask is not None:
+        _strided(mask, 2, (torch.bool, torch.uint8), "mask", q.device)
+        if mask.shape != (batch, keys):
+            raise ValueError("mask must be [B, keys]")
+        a.mask, a.mask_stride = mask.data_ptr(), mask.stride(0)
+    if bias is not None:
+        table, bounds, query_pos, key_pos = bias
+        _want(table, q.dtype, "bias table")
+        _want(bounds, torch.int64, "bias bounds")
+        if table.dim() != 2 or table.shape[0] != heads or bounds.numel() != table.shape[1] - 1:
+            raise ValueError("bias table must be [heads, buckets], bounds one less than buckets")
+        a.query_pos_stride = _positions(query_pos, batch, queries, "query positions", q.device)
+        a.key_pos_stride = _positions(key_pos, batch, keys, "key positions", q.device)
+        a.bias_table, a.bounds, a.query_pos, a.key_pos, a.buckets = table.data_ptr(), bounds.data_ptr(), query_pos.data_ptr(), key_pos.data_ptr(), table.shape[1]
+    return a
+
+
+@contextlib.contextmanager
+def _pool_of(stream):
+    """Memory taken inside is the stream's own: given back after the launch, it goes to work behind it only."""
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        yield
+
+
+def _scratch(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _stats_shape(q):
+    """The library's TASER_ATTENTION_STATS numbers of a row."""
+    return (*q.shape[:3], 2 + (0 if q.dtype == torch.float32 else (q.shape[3] + 1) // 2))
+
+
+def cross_attention_bytes(q, k, v, lengths=None, mask=None, bias=None, scale=None):
+    """taser_cross_attention_bytes -> (workspace bytes of cross_attention, of cross_attention_grad)."""
+    a, work, grad = _attention_block(q, k, v, lengths, mask, bias, scale), ctypes.c_uint64(), ctypes.c_uint64()
+    _check(lib().taser_cross_attention_bytes(ctypes.byref(a), ctypes.byref(work), ctypes.byref(grad)))
+    return work.value, grad.value
+
+
+def cross_attention(q, k, v, lengths=None, mask=None, bias=None, scale=None, want_stats=False, stream=None):
+    """taser_cross_attention. q [B, queries, heads, d], k and v [B, keys, kv_heads, d] of float32, float16 or bfloat16, any strides
+    with adjacent elements; lengths int32[B]; mask bool[B, keys]; bias = (table [heads, buckets] of q's type, bounds int64[buckets - 1],
+    query positions int64[B or 1, queries], key positions int64[B or 1, keys]); scale d ** -0.5 unless given. Returns out (like q,
+    dense), with `want_stats` also stats float32[B, queries, heads, n]: the largest score of a row, the sum of the exponentials
+    over it, and what cross_attention_grad needs besides."""
+    if stream is None:
+        r = (_native or _bind()).attention(q, k, v, lengths, mask, bias, scale, want_stats)
+        if r is not None:
+            return r
+    a, work = _attention_block(q, k, v, lengths, mask, bias, scale), ctypes.c_uint64()
+    _check(lib().taser_cross_attention_bytes(ctypes.byref(a), ctypes.byref(work), None))
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    stats = torch.empty(_stats_shape(q), dtype=torch.float32, device=q.device) if want_stats else None
+    with _pool_of(stream):
+        scratch = _scratch(work.value, q.device)
+    _check(lib().taser_cross_attention(ctypes.byref(a), _ptr(out), _ptr(stats), _ptr(scratch), work.value, _stream(stream)))
+    return (out, stats) if want_stats else out
+
+
+def cross_attention_grad(dout, q, k, v, out, stats, lengths=None, mask=None, bias=None, scale=None, stream=None):
+    """taser_cross_attention_grad: the gradients of cross_attention's sum(out * dout) -> (dq, dk, dv, dtable or None), dense. dout, out:
+    dense like q; out and stats as cross_attention(want_stats=True) gave them for the same arguments."""
+    if stream is None:
+        r = (_native or _bind()).attention_grad(dout, q, k, v, out, stats, lengths, mask, bias, scale)
+        if r is not None:
+            return r
+    a, work = _attention_block(q, k, v, lengths, mask, bias, scale), ctypes.c_uint64()
+    for t, name in ((dout, "dout"), (out, "out")):
+        _want(t, q.dtype, name)
+        if t.shape != q.shape:
+            raise ValueError(f"{name} must have q's shape")
+    _want(stats, torch.float32, "stats")
+    if stats.shape != _stats_shape(q):
+        raise ValueError("stats must be those that cross_attention gave")
+    _check(lib().taser_cross_attention_bytes(ctypes.byref(a), None, ctypes.byref(work)))
+    dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+    dtable = None if bias is None else torch.empty(bias[0].shape, dtype=q.dtype, device=q.device)
+    with _pool_of(stream):
+        scratch = _scratch(work.value, q.device)
+    _check(lib().taser_cross_attention_grad(ctypes.byref(a), _ptr(out), _ptr(stats), _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtable), _ptr(scratch), work.value,
+                                            _stream(stream)))
+    return dq, dk, dv, dtable
+
+
+def _distance_block(dtype, heads, bounds, query_pos, key_pos, batch, device):
+    _want(bounds, torch.int64, "bounds")
+    if query_pos.dim() != 2 or key_pos.dim() != 2:
+        raise TypeError("positions must be [B or 1, n]")
+    queries, keys = query_pos.shape[1], key_pos.shape[1]
+    strides = [_positions(query_pos, batch, queries, "query positions", device), _positions(key_pos, batch, keys, "key positions", device)]
+    return _Distances(_TYPES[dtype], heads, bounds.numel() + 1, batch, queries, keys, bounds.data_ptr(), query_pos.data_ptr(), key_pos.data_ptr(), *strides)
+
+
+def relative_bias(table, bounds, query_pos, key_pos, stream=None):
+    """taser_relative_bias. table [heads, buckets], bounds int64[buckets - 1], positions int64[B or 1, queries] and [B or 1, keys]
+    -> [B, heads, queries, keys] of the table's type, B the larger of the positions'."""
+    if stream is None:
+        r = (_native or _bind()).bias(table, bounds, query_pos, key_pos)
+        if r is not None:
+            return r
+    if table.dtype not in _TYPES:
+        raise TypeError("table: expected float32, float16 or bfloat16")
+    _want(table, table.dtype, "table")
+    batch = max(query_pos.shape[0], key_pos.shape[0])
+    d = _distance_block(table.dtype, table.shape[0], bounds, query_pos, key_pos, batch, table.device)
+    if table.dim() != 2 or table.shape[1] != d.buckets:
+        raise ValueError("table must be [heads, buckets], bounds one less than buckets")
+    out = torch.empty((batch, table.shape[0], d.queries, d.keys), dtype=table.dtype, device=table.device)
+    _check(lib().taser_relative_bias(ctypes.byref(d), _ptr(table), _ptr(out), _stream(stream)))
+    return out
+
+
+def relative_bias_bytes(dbias, bounds, query_pos, key_pos):
+    """taser_relative_bias_bytes -> workspace bytes of relative_bias_grad."""
+    _strided(dbias, 4, _TYPES, "dbias")
+    d, work = _distance_block(dbias.dtype, dbias.shape[1], bounds, query_pos, key_pos, dbias.shape[0], dbias.device), ctypes.c_uint64()
+    _check(lib().taser_relative_bias_bytes(ctypes.byref(d), ctypes.byref(work)))
+    return work.value
+
+
+def relative_bias_grad(dbias, bounds, query_pos, key_pos, stream=None):
+    """taser_relative_bias_grad. dbias [B, heads, queries, keys], any strides with adjacent states -> dtable [heads, buckets]."""
+    if stream is None:
+        r = (_native or _bind()).bias_grad(dbias, bounds, query_pos, key_pos)
+        if r is not None:
+            return r
+    _strided(dbias, 4, _TYPES, "dbias")
+    d, work = _distance_block(dbias.dtype, dbias.shape[1], bounds, query_pos, key_pos, dbias.shape[0], dbias.device), ctypes.c_uint64()
+    if dbias.shape[2:] != (d.queries, d.keys):
+        raise ValueError("dbias must be [B, heads, queries, keys]")
+    _check(lib().taser_relative_bias_bytes(ctypes.byref(d), ctypes.byref(work)))
+    out = torch.empty((dbias.shape[1], d.buckets), dtype=dbias.dtype, device=dbias.device)
+    with _pool_of(stream):
+        scratch = _scratch(work.value, dbias.device)
+    _check(lib().taser_relative_bias_grad(ctypes.byref(d), _ptr(dbias), (ctypes.c_int64 * 3)(*dbias.stride()[:3]), _ptr(out), _ptr(scratch), work.value, _stream(stream)))
+    return out
+
+
+def policy_loss(logits, actions, advantage, old_logp=None, ref_logp=None, count=None, weight=None, clip_low=0.2, clip_high=0.2, kl=0.0, want_grad=True, stream=None):
+    """taser_policy_loss. logits [R, width] of float32, float16 or bfloat16 with contiguous rows; actions int32[R, picks] (-1: none);
+    advantage, old_logp, ref_logp, weight float32[R, picks]; count int32[R]. Returns (loss float32[R, picks], logp float32[R, picks],
+    grad of the sum of all losses, like the logits and dense, or None)."""
+    r = (_native or _bind()).policy(logits, actions, advantage, old_logp, ref_logp, count, weight, clip_low, clip_high, kl, want_grad, stream)
+    if r is not None:
+        return r
+    _strided(logits, 2, _TYPES, "logits")
+    _want(actions, torch.int32, "actions")
+    if actions.dim() != 2 or actions.shape[0] != logits.shape[0]:
+        raise ValueError("logits must be [R, width] and actions [R, picks]")
+    rows, width = logits.shape
+    p = _PolicyBatch(_TYPES[logits.dtype], actions.shape[1], rows, width, logits.stride(0) if rows > 1 else width, logits.data_ptr())
+    p.actions, p.clip_low, p.clip_high, p.kl = actions.data_ptr(), clip_low, clip_high, kl
+    for name, t in (("advantage", advantage), ("old_logp", old_logp), ("ref_logp", ref_logp), ("weight", weight)):
+        if t is not None:
+            _want(t, torch.float32, name)
+            if t.shape != actions.shape:
+                raise ValueError(f"{name} must have the actions' shape")
+            setattr(p, name, t.data_ptr())
+    if count is not None:
+        _want(count, torch.int32, "count")
+        if count.numel() != rows:
+            raise ValueError("count must hold a number for each row")
+        p.count = count.data_ptr()
+    loss, logp = (torch.empty(actions.shape, dtype=torch.float32, device=logits.device) for _ in range(2))
+    grad = torch.empty((rows, width), dtype=logits.dtype, device=logits.device) if want_grad else None
+    _check(lib().taser_policy_loss(ctypes.byref(p), _ptr(loss), _ptr(logp), _ptr(grad), _stream(stream)))
+    return loss, logp, grad
 
 
 def profile_begin():

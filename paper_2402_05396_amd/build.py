@@ -5,6 +5,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -47,18 +48,31 @@ def binding_command():
 
 
 def build(verbose=False):
-    commands = [[HIPCC] + FLAGS + ["-o", LIB] + sources(), binding_command()]
-    running = []
-    for cmd in commands:
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        running.append(subprocess.Popen(cmd))
-    for cmd, p in zip(commands, running):
-        if p.wait() != 0:
-            for other in running:
-                other.wait()
-            raise subprocess.CalledProcessError(p.returncode, cmd)
+    with tempfile.TemporaryDirectory() as objects:   # one object a source, side by side
+        parts = {src: os.path.join(objects, os.path.basename(src) + ".o") for src in sources()}
+        compile_flags = [f for f in FLAGS if f != "-shared"]
+        _run_all([[HIPCC] + compile_flags + ["-c", "-o", obj, src] for src, obj in parts.items()] + [binding_command()], verbose)
+        _run_all([[HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB] + list(parts.values())], verbose)
     return LIB
+
+
+def _run_all(commands, verbose):
+    """Runs the commands, as many at a time as there are processors for (16 at most), and raises for the first that failed."""
+    at_once = max(1, min(16, len(os.sched_getaffinity(0))))
+    waiting, running, failed = list(commands), [], None
+    while waiting or running:
+        while waiting and len(running) < at_once and failed is None:
+            cmd = waiting.pop(0)
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append((cmd, subprocess.Popen(cmd)))
+        if not running:
+            break
+        cmd, p = running.pop(0)
+        if p.wait() != 0 and failed is None:
+            failed = subprocess.CalledProcessError(p.returncode, cmd)
+    if failed is not None:
+        raise failed
 
 
 def stale():

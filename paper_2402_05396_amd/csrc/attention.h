@@ -1,0 +1,257 @@
+// Shared by the translation units of attention to states of another length: argument blocks, tiles in LDS, matrix
+// products and the bias by distance. Not part of the ABI.
+//
+// All products are D = A B + C on tiles of 32 x 32 with a contraction of 16. Lane l holds 8 values of each operand: row
+// (A) or column (B) l % 32, contraction places 8 (l / 32) .. +7. Of the result it holds column l % 32 and the 16 rows
+// 8 g + 4 (l / 32) + i (g, i < 4) in register 4 g + i. So what a product leaves in registers 8 s .. 8 s + 7 is at once a
+// B operand of the next product, whose contraction then runs over rows 16 s + {8 j + 4 (l / 32) + i: j < 2, i < 4}: only
+// the A operand has to be read in that order, and no softmax weight ever leaves its lane.
+#pragma once
+
+#include "taser_internal.h"
+
+typedef float taser_f4 __attribute__((ext_vector_type(4)));
+typedef float taser_f16 __attribute__((ext_vector_type(16)));
+typedef uint32_t taser_u4 __attribute__((ext_vector_type(4)));
+typedef short taser_s4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct TaserFrag { typedef T type __attribute__((ext_vector_type(8))); };
+template <typename T> using taser_frag = typename TaserFrag<T>::type;
+
+// What the kernels of one call share.
+struct TaserAttentionArgs {
+    const void *q, *k, *v;
+    int64_t q_batch, q_token, q_head, k_batch, k_token, k_head, v_batch, v_token, v_head;   // strides in elements
+    int32_t batch, heads, kv_heads, group, dim, queries, keys, rows;                        // group = heads / kv_heads; rows = queries * group
+    float scale;
+    const int32_t* lengths;   // or null
+    const uint8_t* mask;      // or null
+    int64_t mask_batch;
+    const void* table;        // [heads, buckets] or null: no bias
+    const int64_t *bounds, *query_pos, *key_pos;
+    int64_t query_pos_batch, key_pos_batch;
+    int32_t buckets;
+    int32_t splits, row_tiles;
+    int32_t stat_floats;      // of a row: {largest score, sum of exponentials}, then, for 16-bit types, what rounding the output took off
+    int32_t direct;           // states are 16-byte aligned and their heads whole 16-byte pieces: tiles are loaded past the registers
+};
+
+// Checks a call's arguments and lays them out for the kernels.
+int taser_attention_args(const taser_attention* p, const char* what, TaserAttentionArgs* a);
+// Work of taser_cross_attention_grad in bytes.
+uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t type);
+
+// A batch entry's number of states.
+__device__ inline int32_t taser_length(const TaserAttentionArgs& a, int32_t b) {
+    if (!a.lengths) return a.keys;
+    const int32_t n = a.lengths[b];
+    return n < 0 ? 0 : (n > a.keys ? a.keys : n);
+}
+
+// What rounding took off an output element goes beside the statistics (single precision: nothing does). With it <dout, out> is as
+// good as from a 32-bit output: every gradient is that sum's, and where the terms of dtable cancel its error would be all there is.
+template <typename T> __device__ inline T* taser_rest(float* stats, int64_t row, int stat_floats) { return (T*)(stats + row * stat_floats + 2); }
+
+// Up to 8 consecutive elements (n of them; the rest are zeros), at any alignment of the element.
+template <typename T, int N> __device__ inline void taser_load(const T* p, int n, T (&x)[N]) {
+    if (n >= N) {
+        __builtin_memcpy(x, p, N * sizeof(T));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = i < n ? p[i] : (T)0.f;
+    }
+}
+// Four elements, of which the first n are written.
+template <typename T> __device__ inline void taser_store(T* to, int n, const T (&x)[4]) {
+    if (n >= 4) {
+        __builtin_memcpy(to, x, sizeof(x));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) to[i] = x[i];
+    }
+}
+template <typename T> __device__ inline taser_frag<T> taser_load_frag(const T* p, int n) {
+    T x[8];
+    taser_load<T, 8>(p, n, x);
+    taser_frag<T> f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = x[i];
+    return f;
+}
+
+__device__ inline void taser_mma(taser_f16& c, const taser_frag<__bf16>& a, const taser_frag<__bf16>& b) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline void taser_mma(taser_f16& c, const taser_frag<_Float16>& a, const taser_frag<_Float16>& b) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+// Single precision: the instruction contracts 2 places, one a half wave; the 8 values a lane holds take 8 of them.
+__device__ inline void taser_mma(taser_f16& c, const taser_frag<float>& a, const taser_frag<float>& b) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+}
+
+// Registers 8 s .. 8 s + 7 of a result, times `by`, as an operand.
+template <typename T> __device__ inline taser_frag<T> taser_operand(const taser_f16& c, int s, float by = 1.f) {
+    taser_frag<T> f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (T)(c[8 * s + i] * by);
+    return f;
+}
+
+// The value of the lane half a wave away.
+__device__ inline float taser_other_half(float x) {
+    return __shfl_xor(x, 32);
+}
+
+// ---- tiles ----------------------------------------------------------------------------------------------------------
+// A tile holds ROWS rows of DP elements (the head size rounded up, the rest zeros) as 16-byte pieces. Piece c of row r lies
+// at place c ^ taser_swizzle(r): reads of one piece of 16 consecutive rows, and of two neighboring pieces of 4 consecutive
+// rows, then touch every bank of LDS once.
+template <int PIECES> __device__ inline int taser_swizzle(int row) {
+    static_assert(PIECES >= 8, "");
+    const int x = PIECES == 8 ? (row >> 1) & 7 : row & 15;
+    return PIECES == 8 ? ((x & 3) << 1) | (x >> 2) : ((x & 7) << 1) | (x >> 3);
+}
+
+__device__ const uint32_t taser_zero_piece[4] = {0, 0, 0, 0};
+
+// Loads a tile by THREADS threads: row r from row_at(r) where bit r of `keep` is set (zeros elsewhere: nothing is read there).
+// Past the registers (`direct`) it has arrived when vmcnt says so.
+template <typename T, int DP, int ROWS, int THREADS, typename F>
+__device__ inline void taser_load_tile(char* lds, F row_at, uint64_t keep, int dim, bool direct, int thread) {
+    constexpr int PIECES = DP * (int)sizeof(T) / 16, EACH = 16 / (int)sizeof(T);
+    static_assert(ROWS * PIECES % THREADS == 0, "");
+    if (direct) {
+#pragma unroll
+        for (int i = 0; i < ROWS * PIECES / THREADS; ++i) {
+            const int at = i * THREADS + thread, row = at / PIECES, c = (at % PIECES) ^ taser_swizzle<PIECES>(row);
+            const bool there = (keep >> row) & 1 && c * EACH < dim;
+            const void* from = there ? (const void*)(row_at(row) + c * EACH) : (const void*)taser_zero_piece;
+            char* to = lds + (at & ~63) * 16;   // a wave writes 1 KiB from a common address on
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+        }
+    } else {
+#pragma unroll 1
+        for (int i = 0; i < ROWS * PIECES / THREADS; ++i) {
+            const int at = i * THREADS + thread, row = at / PIECES, c = (at % PIECES) ^ taser_swizzle<PIECES>(row);
+            T x[EACH];
+            taser_load<T, EACH>(row_at(row) + c * EACH, (keep >> row) & 1 ? dim - c * EACH : 0, x);
+            taser_u4 u;
+            __builtin_memcpy(&u, x, 16);
+            *(taser_u4*)(lds + at * 16) = u;
+        }
+    }
+}
+
+// Waits for this wave's loads past the registers (and all other loads).
+__device__ inline void taser_loads_arrived() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+}
+
+// Operand of a tile's rows (lane l: row l % 32 of the 32 from `row0` on), contraction over elements 16 kk ..
+template <typename T, int DP> __device__ inline taser_frag<T> taser_rows_operand(const char* lds, int row0, int kk, int lane) {
+    constexpr int PIECES = DP * (int)sizeof(T) / 16;
+    const int row = row0 + (lane & 31), half = lane >> 5;
+    const char* at = lds + row * (DP * (int)sizeof(T));
+    const int s = taser_swizzle<PIECES>(row);
+    taser_frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+        const taser_u4 u = *(const taser_u4*)(at + (((2 * kk + half) ^ s) << 4));
+        __builtin_memcpy(&f, &u, 16);
+    } else {
+        const taser_f4 x = *(const taser_f4*)(at + (((4 * kk + 2 * half) ^ s) << 4)), y = *(const taser_f4*)(at + (((4 * kk + 2 * half + 1) ^ s) << 4));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = x[i];
+            f[4 + i] = y[i];
+        }
+    }
+    return f;
+}
+
+// Operand of a tile's columns (lane l: element 32 dt + l % 32), contraction over rows row0 + {8 j + 4 (l / 32) + i}: the transposed
+// tile in the order in which a product leaves its rows.
+template <typename T, int DP> __device__ inline taser_frag<T> taser_columns_operand(const char* lds, int row0, int dt, int lane) {
+    constexpr int PIECES = DP * (int)sizeof(T) / 16, BYTES = DP * (int)sizeof(T);
+    const int half = lane >> 5;
+    taser_frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+        // 16 lanes read 4 rows of 16 elements, 8 bytes a lane, and get a column of 4 each
+        const int t = lane & 15, c = 4 * dt + 2 * ((lane >> 4) & 1) + ((t & 3) >> 1);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = row0 + 8 * j + 4 * half + (t >> 2);
+            const char* at = lds + row * BYTES + ((c ^ taser_swizzle<PIECES>(row)) << 4) + ((t & 1) << 3);
+            const taser_s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) taser_s4*)at);
+            T y[4];
+            __builtin_memcpy(y, &x, 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[4 * j + i] = y[i];
+        }
+    } else {
+        const int d = 32 * dt + (lane & 31), c = d >> 2;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = row0 + 8 * j + 4 * half + i;
+                f[4 * j + i] = *(const float*)(lds + row * BYTES + ((c ^ taser_swizzle<PIECES>(row)) << 4) + ((d & 3) << 2));
+            }
+    }
+    return f;
+}
+
+// ---- the bias by distance ----------------------------------------------------------------------------------------------
+// Lane l keeps bound l; there are at most 63. A distance common to the wave has as many bounds at most as it as lanes say so.
+__device__ inline int64_t taser_lane_bound(const TaserAttentionArgs& a, int lane) {
+    return lane < a.buckets - 1 ? a.bounds[lane] : INT64_MAX;
+}
+__device__ inline int taser_uniform_bucket(int64_t bound, int64_t distance) {
+    return __popcll(__ballot(bound <= distance));
+}
+__device__ inline int64_t taser_apart(int64_t a, int64_t b) { return (int64_t)((uint64_t)a - (uint64_t)b); }
+__device__ inline int64_t taser_lane_value(int64_t x, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane) |
+                     (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)x >> 32), lane) << 32);
+}
+// Buckets of a lane's distances to the 16 states of a result's registers (state 8 g + i of `pos` in register 4 g + i), known to
+// lie in low .. high.
+__device__ inline void taser_buckets(int (&bucket)[16], int64_t bound, int low, int high, int64_t from, const int64_t* pos) {
+    int64_t apart[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        apart[r] = taser_apart(from, pos[8 * (r >> 2) + (r & 3)]);
+        bucket[r] = low;
+    }
+    for (int i = low; i < high; ++i) {
+        const int64_t x = taser_lane_value(bound, i);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) bucket[r] += x <= apart[r];
+    }
+}
+__device__ inline int64_t taser_wave_min(int64_t x) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int64_t y = __shfl_xor(x, m);
+        x = y < x ? y : x;
+    }
+    return x;
+}
+__device__ inline int64_t taser_wave_max(int64_t x) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int64_t y = __shfl_xor(x, m);
+        x = y > x ? y : x;
+    }
+    return x;
+}
+
+// Workgroups are handed out to the eight L2 partitions in turn: each partition takes a stretch of consecutive work, so that
+// workgroups that read the same states share a cache. -1: nothing to do.
+__device__ inline int64_t taser_stretch_of_work(int64_t id, int64_t all) {
+    const int64_t each = (all + 7) / 8, at = (id & 7) * each + (id >> 3);
+    return (id >> 3) < each && at < all ? at : -1;
+}
+inline int64_t taser_stretched_grid(int64_t all) { return (all + 7) / 8 * 8; }

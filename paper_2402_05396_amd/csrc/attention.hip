@@ -1,0 +1,429 @@
+// Attention to states of another length (taser_cross_attention): one pass over the states with the running maximum and sum of
+// a softmax.
+#include <cmath>
+#include <type_traits>
+
+#include "attention.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// A wave owns 32 query rows (of the queries of one key head: row r is query r / group, head r % group of them), lane l row
+// l % 32 of them. Scores come out transposed, states in registers, so a row's softmax needs one exchange, with the other half of
+// the wave, and its weights are an operand as they are. SHARED: the four waves of a block have 32 rows each and share tiles of 64
+// states. Else the block has 32 rows and each wave every fourth (second) tile of 32 states, joined at the end: for few rows.
+template <typename T, int DP, bool SHARED> struct Shape {
+    static constexpr int kWaves = !SHARED && DP * sizeof(T) > 256 ? 2 : 4, kStates = SHARED && sizeof(T) == 2 ? 64 : 32;
+    static constexpr int kTileBytes = kStates * DP * (int)sizeof(T), kTiles = SHARED ? 1 : kWaves;   // tiles in LDS at a time, of each of four kinds
+    static constexpr int kRows = SHARED ? 32 * kWaves : 32;
+};
+
+template <typename T, int DP, bool SHARED, bool BIAS>
+__global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && sizeof(T) == 2 ? 2 : 1)) void attention_kernel(const TaserAttentionArgs a, T* out, float* stats, float* part_out,
+                                                                                      float* part_stats, int64_t work) {
+    using S = Shape<T, DP, SHARED>;
+    constexpr int KT = S::kStates, NK = KT / 32, ND = DP / 32, NC = DP / 16;
+    __shared__ __attribute__((aligned(1024))) char k0[S::kTiles][S::kTileBytes], v0[S::kTiles][S::kTileBytes], k1[S::kTiles][S::kTileBytes], v1[S::kTiles][S::kTileBytes];
+    __shared__ int64_t pos0[S::kTiles][BIAS ? KT : 1], pos1[S::kTiles][BIAS ? KT : 1], range0[S::kTiles][2], range1[S::kTiles][2];
+    __shared__ float joined[2][S::kWaves][32];
+    extern __shared__ float table[];   // [group][buckets]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int64_t item = taser_stretch_of_work(blockIdx.x, work);
+    if (item < 0) return;
+    const int row_tile = (int)(item % a.row_tiles), split = (int)(item / a.row_tiles % a.splits);
+    const int64_t pair = item / a.row_tiles / a.splits;
+    const int hk = (int)(pair % a.kv_heads), b = (int)(pair / a.kv_heads);
+    const int32_t length = taser_length(a, b);
+    const int all_tiles = (length + KT - 1) / KT, each = (all_tiles + a.splits - 1) / a.splits;
+    const int first = split * each, last = first + each < all_tiles ? first + each : all_tiles;
+
+    const int row = row_tile * S::kRows + (SHARED ? wave * 32 : 0) + (lane & 31);
+    const bool real = row < a.rows;
+    const int query = real ? row / a.group : 0, g = real ? row - query * a.group : 0, head = hk * a.group + g;
+    taser_frag<T> q[NC];
+    {
+        const T* from = (const T*)a.q + b * a.q_batch + query * a.q_token + head * a.q_head;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) q[c] = taser_load_frag<T>(from + 16 * c + 8 * half, real ? a.dim - 16 * c - 8 * half : 0);
+    }
+    int64_t query_pos = 0, bound = 0, query_low = 0, query_high = 0;
+    if constexpr (BIAS) {
+        const T* from = (const T*)a.table + (int64_t)hk * a.group * a.buckets;
+        for (int i = threadIdx.x; i < a.group * a.buckets; i += blockDim.x) table[i] = (float)from[i];
+        query_pos = a.query_pos[b * a.query_pos_batch + query];
+        bound = taser_lane_bound(a, lane);
+        query_low = taser_wave_min(query_pos);
+        query_high = taser_wave_max(query_pos);
+        __syncthreads();
+    }
+    const float* my_table = table + g * a.buckets;
+    const T* const k_from = (const T*)a.k + b * a.k_batch + hk * a.k_head;
+    const T* const v_from = (const T*)a.v + b * a.v_batch + hk * a.v_head;
+
+    // states [KT * tile, ..) that take part
+    auto kept = [&](int tile) -> uint64_t {
+        const int at = tile * KT, n = length - at;
+        uint64_t keep = n >= 64 ? ~0ull : (n <= 0 ? 0 : (1ull << n) - 1);
+        if (KT == 32) keep &= 0xffffffffull;
+        if (a.mask) keep &= __ballot(lane < n && a.mask[b * a.mask_batch + at + (lane < n ? lane : 0)]);
+        return keep;
+    };
+    constexpr int THREADS = SHARED ? 64 * S::kWaves : 64;
+    const int thread = SHARED ? (int)threadIdx.x : lane, slot = SHARED ? 0 : wave;
+    auto fetch = [&](char* k, char* v, int64_t* pos, int64_t* range, int tile, uint64_t keep) {
+        const int64_t at = (int64_t)tile * KT;
+        taser_load_tile<T, DP, KT, THREADS>(k, [&](int r) { return k_from + (at + r) * a.k_token; }, keep, a.dim, a.direct, thread);
+        taser_load_tile<T, DP, KT, THREADS>(v, [&](int r) { return v_from + (at + r) * a.v_token; }, keep, a.dim, a.direct, thread);
+        if constexpr (BIAS) {
+            if (!SHARED || wave == 0) {
+                const bool there = lane < KT && (keep >> lane) & 1;
+                const int64_t p = there ? a.key_pos[b * a.key_pos_batch + at + lane] : 0;
+                if (lane < KT) pos[lane] = p;
+                const int64_t low = taser_wave_min(there ? p : INT64_MAX), high = taser_wave_max(there ? p : INT64_MIN);
+                if (lane == 0) {
+                    range[0] = low;
+                    range[1] = high;
+                }
+            }
+        }
+    };
+
+    // Half precision ends at 6e-8 below 1: there the weights, and all sums of them, are 2^14 times as large until the end.
+    constexpr float lift = std::is_same_v<T, _Float16> ? 14.f : 0.f, drop = std::is_same_v<T, _Float16> ? 1.f / 16384.f : 1.f;
+    float top = -INFINITY, sum = 0.f;
+    taser_f16 o[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+    const float scale2 = a.scale * kLog2e;
+
+    auto compute = [&](const char* k, const char* v, const int64_t* pos, const int64_t* range, uint64_t keep) {
+        taser_f16 s[NK];
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) taser_mma(s[n], taser_rows_operand<T, DP>(k, 32 * n, c, lane), q[c]);
+        }
+        if constexpr (BIAS) {
+            if (keep) {
+                const int low = taser_uniform_bucket(bound, taser_apart(query_low, range[1])), high = taser_uniform_bucket(bound, taser_apart(query_high, range[0]));
+                if (low == high) {
+                    const float bias = my_table[low];
+#pragma unroll
+                    for (int n = 0; n < NK; ++n)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[n][r] = fmaf(s[n][r], a.scale, bias);
+                } else {
+#pragma unroll
+                    for (int n = 0; n < NK; ++n) {
+                        int bucket[16];
+                        taser_buckets(bucket, bound, low, high, query_pos, pos + 32 * n + 4 * half);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[n][r] = fmaf(s[n][r], a.scale, my_table[bucket[r]]);
+                    }
+                }
+            }
+        }
+        if (keep != (KT == 64 ? ~0ull : 0xffffffffull)) {
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                const uint32_t bits = (uint32_t)(keep >> (32 * n)) >> (4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!((bits >> (8 * (r >> 2) + (r & 3))) & 1)) s[n][r] = -INFINITY;
+            }
+        }
+        float now = s[0][0];
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) now = fmaxf(now, s[n][r]);
+        now = fmaxf(now, taser_other_half(now));
+        if (__any(now > top)) {
+            now = fmaxf(now, top);
+            const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - now) * (BIAS ? kLog2e : scale2));
+            top = now;
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
+        }
+        const float base = top == -INFINITY ? 0.f : top, base2 = base * scale2 - lift;
+        float part = 0.f;
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[n][r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(s[n][r] - base, kLog2e, lift) : fmaf(s[n][r], scale2, -base2));
+                part += s[n][r];
+            }
+        sum += part;
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                // the weights are rounded to the type of the states that they multiply; their sum is of the unrounded ones
+                const taser_frag<T> p = taser_operand<T>(s[n], h);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) taser_mma(o[d], taser_columns_operand<T, DP>(v, 32 * n + 16 * h, d, lane), p);
+            }
+    };
+
+    const int step = SHARED ? 1 : S::kWaves;
+    int tile = first + (SHARED ? 0 : wave);
+    uint64_t keep0 = 0, keep1 = 0;
+    auto arrived = [&]() {
+        taser_loads_arrived();
+        if (SHARED) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
+    };
+    if (tile < last) {
+        keep0 = kept(tile);
+        fetch(k0[slot], v0[slot], pos0[slot], range0[slot], tile, keep0);
+    }
+    for (; tile < last; tile += 2 * step) {
+        arrived();
+        if (tile + step < last) {
+            keep1 = kept(tile + step);
+            fetch(k1[slot], v1[slot], pos1[slot], range1[slot], tile + step, keep1);
+        }
+        compute(k0[slot], v0[slot], pos0[slot], range0[slot], keep0);
+        if (tile + step >= last) break;
+        arrived();
+        if (tile + 2 * step < last) {
+            keep0 = kept(tile + 2 * step);
+            fetch(k0[slot], v0[slot], pos0[slot], range0[slot], tile + 2 * step, keep0);
+        }
+        compute(k1[slot], v1[slot], pos1[slot], range1[slot], keep1);
+    }
+
+    sum += taser_other_half(sum);
+    if (!BIAS) top *= a.scale;
+    if constexpr (!SHARED) {   // the waves' shares are joined
+        constexpr int W = S::kWaves;
+        joined[0][wave][lane & 31] = top;
+        joined[1][wave][lane & 31] = sum;
+        // a wave's sums need twice the bytes of a tile of 16-bit elements
+        auto place = [&](int w, int d) -> float* {
+            constexpr int FIRST = sizeof(T) == 2 ? ND / 2 : ND;
+            return (float*)(d < FIRST ? k0[w] + d * 4096 : k1[w] + (d - FIRST) * 4096);
+        };
+        taser_loads_arrived();
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) place(wave, d)[64 * r + lane] = o[d][r];
+        __syncthreads();
+        float best = -INFINITY, by[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) best = fmaxf(best, joined[0][w][lane & 31]);
+        sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            by[w] = best == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((joined[0][w][lane & 31] - best) * kLog2e);
+            sum = fmaf(by[w], joined[1][w][lane & 31], sum);
+        }
+        top = best;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            if (d % W != wave) continue;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                float x = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) x = fmaf(by[w], place(w, d)[64 * r + lane], x);
+                o[d][r] = x;
+            }
+        }
+    }
+    if (!real) return;
+    const int64_t at = ((int64_t)b * a.queries + query) * a.heads + head;
+    if (part_out) {
+        const int64_t all_rows = (int64_t)a.batch * a.queries * a.heads;
+        float* to = part_out + (split * all_rows + at) * a.dim;
+        if (half == 0 && (SHARED || wave == 0)) {
+            part_stats[2 * (split * all_rows + at)] = top;
+            part_stats[2 * (split * all_rows + at) + 1] = sum * drop;
+        }
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+            if (!SHARED && d % S::kWaves != wave) continue;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int e = 32 * d + 8 * (r >> 2) + 4 * half + (r & 3);
+                if (e < a.dim) to[e] = o[d][r] * drop;
+            }
+        }
+        return;
+    }
+    if (stats && half == 0 && (SHARED || wave == 0)) {
+        stats[at * a.stat_floats] = top;
+        stats[at * a.stat_floats + 1] = sum * drop;
+    }
+    const float inverse = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+    T *to = out + at * a.dim, *rest = sizeof(T) == 2 && stats ? taser_rest<T>(stats, at, a.stat_floats) : nullptr;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+        if (!SHARED && d % S::kWaves != wave) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 32 * d + 8 * j + 4 * half;
+            T x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = (T)(o[d][4 * j + i] * inverse);
+                y[i] = (T)(o[d][4 * j + i] * inverse - (float)x[i]);
+            }
+            taser_store(to + e, a.dim - e, x);
+            if (rest) taser_store(rest + e, a.dim - e, y);
+        }
+    }
+}
+
+// Joins the splits: a thread has one element of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(const float* part_out, const float* part_stats, int64_t rows, int32_t dim, int32_t splits, T* out, float* stats,
+                                                             int32_t stat_floats) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * dim) return;
+    const int64_t row = i / dim;
+    const int e = (int)(i - row * dim);
+    float top = -INFINITY, sum = 0.f, x = 0.f;
+    for (int s = 0; s < splits; ++s) top = fmaxf(top, part_stats[2 * (s * rows + row)]);
+    if (top != -INFINITY)
+        for (int s = 0; s < splits; ++s) {
+            const float by = __builtin_amdgcn_exp2f((part_stats[2 * (s * rows + row)] - top) * kLog2e);
+            sum = fmaf(by, part_stats[2 * (s * rows + row) + 1], sum);
+            x = fmaf(by, part_out[(s * rows + row) * dim + e], x);
+        }
+    x = sum != 0.f ? x / sum : 0.f;
+    out[i] = (T)x;
+    if (!stats) return;
+    if (sizeof(T) == 2) taser_rest<T>(stats, row, stat_floats)[e] = (T)(x - (float)(T)x);
+    if (e == 0) {
+        stats[row * stat_floats] = top;
+        stats[row * stat_floats + 1] = sum;
+    }
+}
+
+template <typename T, int DP, bool SHARED>
+int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStream_t stream) {
+    using S = Shape<T, DP, SHARED>;
+    const int64_t rows = (int64_t)a.batch * a.queries * a.heads;
+    float* part_out = a.splits > 1 ? work : nullptr;
+    float* part_stats = a.splits > 1 ? work + a.splits * rows * a.dim : nullptr;
+    a.row_tiles = (a.rows + S::kRows - 1) / S::kRows;
+    const int64_t items = (int64_t)a.batch * a.kv_heads * a.splits * a.row_tiles;
+    const dim3 grid((unsigned)taser_stretched_grid(items)), block(64 * S::kWaves);
+    if (items > INT32_MAX / 2) return taser_fail(TASER_E_RANGE, "cross_attention: too many queries and batch entries for one launch");
+    {
+        TaserProfileSpan span(stream, "attention");
+        if (a.table)
+            attention_kernel<T, DP, SHARED, true><<<grid, block, sizeof(float) * a.group * a.buckets, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
+        else
+            attention_kernel<T, DP, SHARED, false><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
+        TASER_HIP_TRY(hipGetLastError());
+    }
+    if (a.splits > 1) {
+        TaserProfileSpan span(stream, "attention_join");
+        attention_join_kernel<T><<<dim3((unsigned)((rows * a.dim + 255) / 256)), 256, 0, stream>>>(part_out, part_stats, rows, a.dim, a.splits, (T*)out, stats, a.stat_floats);
+        TASER_HIP_TRY(hipGetLastError());
+    }
+    return TASER_OK;
+}
+
+template <typename T> int launch_typed(TaserAttentionArgs& a, bool shared, void* out, float* stats, float* work, hipStream_t stream) {
+    if (a.dim <= 64) return shared ? launch<T, 64, true>(a, out, stats, work, stream) : launch<T, 64, false>(a, out, stats, work, stream);
+    return shared ? launch<T, 128, true>(a, out, stats, work, stream) : launch<T, 128, false>(a, out, stats, work, stream);
+}
+
+bool few_rows(const TaserAttentionArgs& a) { return a.rows <= 64; }
+
+// Parts of the states, so that the chip is full where there are few rows.
+int splits_for(const TaserAttentionArgs& a) {
+    const bool few = few_rows(a);
+    const int64_t blocks = (int64_t)a.batch * a.kv_heads * (few ? (a.rows + 31) / 32 : (a.rows + 127) / 128);
+    if (!blocks) return 1;
+    const int64_t most = a.keys / (few ? 256 : 512), wanted = (512 + blocks - 1) / blocks;
+    const int64_t n = wanted < most ? wanted : most;
+    return n < 1 ? 1 : (n > 256 ? 256 : (int)n);
+}
+
+uint64_t work_bytes(const TaserAttentionArgs& a) {
+    const int splits = splits_for(a);
+    return splits > 1 ? sizeof(float) * (uint64_t)splits * a.batch * a.queries * a.heads * (a.dim + 2) : 0;
+}
+
+}  // namespace
+
+int taser_attention_args(const taser_attention* p, const char* what, TaserAttentionArgs* a) {
+    if (!p) return taser_fail(TASER_E_ARG, "%s: null argument block", what);
+    if (p->type < TASER_F32 || p->type > TASER_BF16) return taser_fail(TASER_E_ARG, "%s: unknown element type %d", what, p->type);
+    if (p->batch < 0 || p->queries < 0 || p->keys < 0 || p->heads < 1 || p->kv_heads < 1 || p->head_dim < 1)
+        return taser_fail(TASER_E_ARG, "%s: negative size, or no heads or elements", what);
+    if (p->heads % p->kv_heads) return taser_fail(TASER_E_ARG, "%s: %d query heads cannot share %d key heads evenly", what, p->heads, p->kv_heads);
+    if (p->head_dim > TASER_MAX_HEAD_DIM) return taser_fail(TASER_E_RANGE, "%s: heads of %d elements (at most %d)", what, p->head_dim, TASER_MAX_HEAD_DIM);
+    const int64_t group = p->heads / p->kv_heads, limit = (int64_t)1 << 31;
+    if (p->batch >= limit || p->queries * group >= limit - 128 || p->keys >= limit - 128 || (p->queries && p->batch * p->heads >= ((int64_t)1 << 39) / p->queries))
+        return taser_fail(TASER_E_RANGE, "%s: too many queries, states or batch entries", what);
+    if (!(p->scale > 0.f) || std::isinf(p->scale)) return taser_fail(TASER_E_ARG, "%s: the scale must be positive and finite", what);
+    const bool queries = p->batch && p->queries;
+    if (queries && !p->q) return taser_fail(TASER_E_ARG, "%s: null queries", what);
+    if (p->batch && p->keys && (!p->k || !p->v)) return taser_fail(TASER_E_ARG, "%s: null states", what);
+    if (p->bias_table) {
+        if (p->buckets < 1 || p->buckets > TASER_MAX_BUCKETS) return taser_fail(TASER_E_RANGE, "%s: %d buckets (1 to %d)", what, p->buckets, TASER_MAX_BUCKETS);
+        if (p->buckets > 1 && !p->bounds) return taser_fail(TASER_E_ARG, "%s: a bias needs its bounds", what);
+        if ((queries && !p->query_pos) || (p->batch && p->keys && !p->key_pos)) return taser_fail(TASER_E_ARG, "%s: a bias needs positions", what);
+        if (group * p->buckets > TASER_MAX_GROUP_BUCKETS)
+            return taser_fail(TASER_E_RANGE, "%s: %lld query heads to a key head with %d buckets (product at most %d)", what, (long long)group, p->buckets, TASER_MAX_GROUP_BUCKETS);
+    }
+    *a = TaserAttentionArgs{};
+    a->q = p->q; a->k = p->k; a->v = p->v;
+    a->q_batch = p->q_strides[0]; a->q_token = p->q_strides[1]; a->q_head = p->q_strides[2];
+    a->k_batch = p->k_strides[0]; a->k_token = p->k_strides[1]; a->k_head = p->k_strides[2];
+    a->v_batch = p->v_strides[0]; a->v_token = p->v_strides[1]; a->v_head = p->v_strides[2];
+    a->batch = (int32_t)p->batch; a->heads = p->heads; a->kv_heads = p->kv_heads; a->group = (int32_t)group; a->dim = p->head_dim;
+    a->queries = (int32_t)p->queries; a->keys = (int32_t)p->keys; a->rows = (int32_t)(p->queries * group);
+    a->scale = p->scale;
+    a->lengths = p->lengths; a->mask = p->mask; a->mask_batch = p->mask_stride;
+    a->table = p->bias_table; a->bounds = p->bounds; a->query_pos = p->query_pos; a->key_pos = p->key_pos;
+    a->query_pos_batch = p->query_pos_stride; a->key_pos_batch = p->key_pos_stride; a->buckets = p->bias_table ? p->buckets : 0;
+    a->splits = a->row_tiles = 1;
+    a->stat_floats = TASER_ATTENTION_STATS(p->type, p->head_dim);
+    const int size = p->type == TASER_F32 ? 4 : 2, whole = 16 / size;
+    bool direct = a->dim % whole == 0 && ((uintptr_t)p->k | (uintptr_t)p->v) % 16 == 0;
+    for (int i = 0; i < 3; ++i) direct = direct && p->k_strides[i] % whole == 0 && p->v_strides[i] % whole == 0;
+    a->direct = direct;
+    return TASER_OK;
+}
+
+extern "C" int taser_cross_attention_bytes(const taser_attention* p, uint64_t* work, uint64_t* grad_work) {
+    TaserAttentionArgs a;
+    if (const int rc = taser_attention_args(p, "cross_attention_bytes", &a)) return rc;
+    if (work) *work = work_bytes(a);
+    if (grad_work) *grad_work = taser_attention_grad_bytes(a, p->type);
+    return TASER_OK;
+}
+
+extern "C" int taser_cross_attention(const taser_attention* p, void* out, float* stats, void* work, uint64_t work_size, void* hip_stream) {
+    TaserAttentionArgs a;
+    if (const int rc = taser_attention_args(p, "cross_attention", &a)) return rc;
+    if (!a.batch || !a.queries) return TASER_OK;
+    if (!out) return taser_fail(TASER_E_ARG, "cross_attention: null output");
+    a.splits = splits_for(a);
+    const uint64_t need = work_bytes(a);
+    if (need > work_size) return taser_fail(TASER_E_RANGE, "cross_attention: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)need);
+    if (need && (!work || (uintptr_t)work % 16)) return taser_fail(TASER_E_ARG, "cross_attention: null or misaligned workspace");
+    hipStream_t stream = (hipStream_t)hip_stream;
+    taser_clear_stale_hip_error();
+    const bool shared = !few_rows(a);
+    if (p->type == TASER_F32) return launch_typed<float>(a, shared, out, stats, (float*)work, stream);
+    if (p->type == TASER_F16) return launch_typed<_Float16>(a, shared, out, stats, (float*)work, stream);
+    return launch_typed<__bf16>(a, shared, out, stats, (float*)work, stream);
+}

@@ -1,0 +1,563 @@
+// The gradients of attention to states of another length (taser_cross_attention_grad).
+//
+// With p = exp(x - top) / sum, dp = <dout, v>, t = <dout, out> of a row: dx = p (dp - t); dv = sum of p dout, dk = scale * sum of
+// dx q, dq = scale * sum of dx k, dtable = sum of dx by bucket. One kernel owns states and goes over the rows (dk, dv), another
+// owns rows and goes over the states (dq, dtable): scores and dp are computed twice (7 products for 5), but nothing is added to
+// memory by more than one block, so all sums have one order and need no second pass over a gradient.
+#include <cmath>
+#include <type_traits>
+
+#include "attention.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// What the passes need of a row: {top, 1 / sum, <dout, out>, log2 of the sum of 2^(x log2 e)}; a row without states has weights of 0.
+// 16 lanes a row.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_grad_rows_kernel(const T* out, const T* dout, const float* stats, int32_t stat_floats, int64_t rows, int32_t dim, taser_f4* info) {
+    const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (row >= rows) return;
+    const int e = 8 * (threadIdx.x & 15);
+    const taser_frag<T> x = taser_load_frag<T>(out + row * dim + e, dim - e), y = taser_load_frag<T>(dout + row * dim + e, dim - e);
+    float t = 0.f;
+    if constexpr (sizeof(T) == 2) {
+        const taser_frag<T> z = taser_load_frag<T>(taser_rest<T>((float*)stats, row, stat_floats) + e, dim - e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t = fmaf((float)x[i] + (float)z[i], (float)y[i], t);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t = fmaf(x[i], y[i], t);
+    }
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) t += __shfl_xor(t, m);
+    if (e) return;
+    const float top = stats[row * stat_floats], sum = stats[row * stat_floats + 1];
+    taser_f4 w;
+    w[0] = sum == 0.f ? INFINITY : top;
+    w[1] = sum == 0.f ? 0.f : 1.f / sum;
+    w[2] = t;
+    w[3] = sum == 0.f ? INFINITY : fmaf(top, kLog2e, log2f(sum));
+    info[row] = w;
+}
+
+// ---- dq, dtable -----------------------------------------------------------------------------------------------------------
+// A wave owns 32 rows, as in the forward pass; four waves share tiles of 32 states.
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_queries_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dq,
+                                                                                               float* part_dq, float* part_table, int64_t work) {
+    constexpr int KT = 32, ND = DP / 32, NC = DP / 16, BYTES = KT * DP * (int)sizeof(T);
+    __shared__ __attribute__((aligned(1024))) char k0[BYTES], v0[BYTES], k1[BYTES], v1[BYTES];
+    __shared__ int64_t pos0[BIAS ? KT : 1], pos1[BIAS ? KT : 1], range0[2], range1[2];
+    extern __shared__ float table[];   // [group][buckets], then [128 rows][buckets]: sums of dx
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int64_t item = taser_stretch_of_work(blockIdx.x, work);
+    if (item < 0) return;
+    const int row_tile = (int)(item % a.row_tiles), split = (int)(item / a.row_tiles % a.splits);
+    const int64_t pair = item / a.row_tiles / a.splits;
+    const int hk = (int)(pair % a.kv_heads), b = (int)(pair / a.kv_heads);
+    const int32_t length = taser_length(a, b);
+    const int all_tiles = (length + KT - 1) / KT, each = (all_tiles + a.splits - 1) / a.splits;
+    const int first = split * each, last = first + each < all_tiles ? first + each : all_tiles;
+
+    const int row = row_tile * 128 + wave * 32 + (lane & 31);
+    const bool real = row < a.rows;
+    const int query = real ? row / a.group : 0, g = real ? row - query * a.group : 0, head = hk * a.group + g;
+    const int64_t at_row = ((int64_t)b * a.queries + query) * a.heads + head;
+    taser_frag<T> q[NC], dy[NC];
+    {
+        const T *from = (const T*)a.q + b * a.q_batch + query * a.q_token + head * a.q_head, *dfrom = dout + at_row * a.dim;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int e = 16 * c + 8 * half, n = real ? a.dim - e : 0;
+            q[c] = taser_load_frag<T>(from + e, n);
+            dy[c] = taser_load_frag<T>(dfrom + e, n);
+        }
+    }
+    taser_f4 mine = {INFINITY, 0.f, 0.f, INFINITY};
+    if (real) mine = info[at_row];
+    int64_t query_pos = 0, bound = 0, query_low = 0, query_high = 0;
+    if constexpr (BIAS) {
+        const T* from = (const T*)a.table + (int64_t)hk * a.group * a.buckets;
+        for (int i = threadIdx.x; i < (a.group + 128) * a.buckets; i += 256) table[i] = i < a.group * a.buckets ? (float)from[i] : 0.f;
+        query_pos = a.query_pos[b * a.query_pos_batch + query];
+        bound = taser_lane_bound(a, lane);
+        query_low = taser_wave_min(query_pos);
+        query_high = taser_wave_max(query_pos);
+        __syncthreads();
+    }
+    const float* my_table = table + g * a.buckets;
+    float* my_sums = table + (a.group + wave * 32 + (lane & 31)) * a.buckets;
+    const T* const k_from = (const T*)a.k + b * a.k_batch + hk * a.k_head;
+    const T* const v_from = (const T*)a.v + b * a.v_batch + hk * a.v_head;
+
+    auto kept = [&](int tile) -> uint32_t {
+        const int at = tile * KT, n = length - at;
+        uint32_t keep = n >= 32 ? ~0u : (1u << n) - 1;
+        if (a.mask) keep &= (uint32_t)__ballot(lane < n && a.mask[b * a.mask_batch + at + (lane < n ? lane : 0)]);
+        return keep;
+    };
+    auto fetch = [&](char* k, char* v, int64_t* pos, int64_t* range, int tile, uint32_t keep) {
+        const int64_t at = (int64_t)tile * KT;
+        taser_load_tile<T, DP, KT, 256>(k, [&](int r) { return k_from + (at + r) * a.k_token; }, keep, a.dim, a.direct, threadIdx.x);
+        taser_load_tile<T, DP, KT, 256>(v, [&](int r) { return v_from + (at + r) * a.v_token; }, keep, a.dim, a.direct, threadIdx.x);
+        if constexpr (BIAS) {
+            if (wave == 0) {
+                const bool there = lane < KT && (keep >> lane) & 1;
+                const int64_t p = there ? a.key_pos[b * a.key_pos_batch + at + lane] : 0;
+                if (lane < KT) pos[lane] = p;
+                const int64_t low = taser_wave_min(there ? p : INT64_MAX), high = taser_wave_max(there ? p : INT64_MIN);
+                if (lane == 0) {
+                    range[0] = low;
+                    range[1] = high;
+                }
+            }
+        }
+    };
+
+    taser_f16 acc[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+    const float scale2 = a.scale * kLog2e;
+
+    auto compute = [&](const char* k, const char* v, const int64_t* pos, const int64_t* range, uint32_t keep) {
+        if (!keep) return;
+        taser_f16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            taser_mma(s, taser_rows_operand<T, DP>(k, 0, c, lane), q[c]);
+            taser_mma(dp, taser_rows_operand<T, DP>(v, 0, c, lane), dy[c]);
+        }
+        const uint32_t bits = keep >> (4 * half);
+        int bucket[16], low = 0, high = 0;
+        if constexpr (BIAS) {
+            low = taser_uniform_bucket(bound, taser_apart(query_low, range[1]));
+            high = taser_uniform_bucket(bound, taser_apart(query_high, range[0]));
+            if (low == high) {
+                const float bias = my_table[low];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale, bias);
+            } else {
+                taser_buckets(bucket, bound, low, high, query_pos, pos + 4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale, my_table[bucket[r]]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            float p = BIAS ? __builtin_amdgcn_exp2f((s[r] - mine[0]) * kLog2e) * mine[1] : __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -mine[3]));
+            if (keep != ~0u && !((bits >> (8 * (r >> 2) + (r & 3))) & 1)) p = 0.f;
+            s[r] = p * (dp[r] - mine[2]);
+        }
+        if constexpr (BIAS) {
+            for (int u = low; u <= high; ++u) {
+                float x = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x += low == high || bucket[r] == u ? s[r] : 0.f;
+                x += taser_other_half(x);
+                if (half == 0) my_sums[u] += x;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const taser_frag<T> x = taser_operand<T>(s, h);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) taser_mma(acc[d], taser_columns_operand<T, DP>(k, 16 * h, d, lane), x);
+        }
+    };
+
+    int tile = first;
+    uint32_t keep0 = 0, keep1 = 0;
+    if (tile < last) {
+        keep0 = kept(tile);
+        fetch(k0, v0, pos0, range0, tile, keep0);
+    }
+    for (; tile < last; tile += 2) {
+        taser_loads_arrived();
+        __syncthreads();
+        if (tile + 1 < last) {
+            keep1 = kept(tile + 1);
+            fetch(k1, v1, pos1, range1, tile + 1, keep1);
+        }
+        compute(k0, v0, pos0, range0, keep0);
+        if (tile + 1 >= last) break;
+        taser_loads_arrived();
+        __syncthreads();
+        if (tile + 2 < last) {
+            keep0 = kept(tile + 2);
+            fetch(k0, v0, pos0, range0, tile + 2, keep0);
+        }
+        compute(k1, v1, pos1, range1, keep1);
+    }
+
+    if constexpr (BIAS) {
+        __syncthreads();
+        float* to = part_table + item * (a.group * a.buckets);
+        const float* sums = table + a.group * a.buckets;
+        const int rows = a.rows - row_tile * 128 < 128 ? a.rows - row_tile * 128 : 128;
+        for (int i = threadIdx.x; i < a.group * a.buckets; i += 256) {
+            const int of = i / a.buckets, u = i - of * a.buckets;
+            int r = (int)((of + a.group - (int64_t)row_tile * 128 % a.group) % a.group);   // the first row of this tile with that head
+            float x = 0.f;
+            for (; r < rows; r += a.group) x += sums[r * a.buckets + u];
+            to[i] = x;
+        }
+    }
+    if (!real) return;
+    float* part = part_dq ? part_dq + (split * (int64_t)a.batch * a.queries * a.heads + at_row) * a.dim : nullptr;
+    T* to = dq + at_row * a.dim;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 32 * d + 8 * j + 4 * half;
+            T x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float y = acc[d][4 * j + i] * a.scale;
+                x[i] = (T)y;
+                if (part && e + i < a.dim) part[e + i] = y;
+            }
+            if (part) continue;
+            taser_store(to + e, a.dim - e, x);
+        }
+}
+
+// ---- dk, dv ---------------------------------------------------------------------------------------------------------------
+// A wave owns 32 states, their keys and values in registers (lane l: state l % 32); four waves share tiles of 32 rows. Rows of all
+// query heads of the key head pass by, so shared heads' gradients are whole.
+template <typename T, int DP, bool BIAS>
+__global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dk, T* dv, float* part_dk,
+                                                                    float* part_dv, int64_t work) {
+    constexpr int RT = 32, ND = DP / 32, NC = DP / 16, BYTES = RT * DP * (int)sizeof(T);
+    __shared__ __attribute__((aligned(1024))) char q0[BYTES], y0[BYTES], q1[BYTES], y1[BYTES];
+    __shared__ taser_f4 info0[4][RT / 4], info1[4][RT / 4];   // a kind of number of 4 rows
+    __shared__ int64_t pos0[BIAS ? RT : 1], pos1[BIAS ? RT : 1], range0[2], range1[2];
+    __shared__ int at0[BIAS ? RT : 1], at1[BIAS ? RT : 1];    // a row's place in the table
+    extern __shared__ float table[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int64_t item = taser_stretch_of_work(blockIdx.x, work);
+    if (item < 0) return;
+    const int state_tile = (int)(item % a.row_tiles), split = (int)(item / a.row_tiles % a.splits);
+    const int64_t pair = item / a.row_tiles / a.splits;
+    const int hk = (int)(pair % a.kv_heads), b = (int)(pair / a.kv_heads);
+    const int32_t length = taser_length(a, b);
+    const int all_tiles = state_tile * 128 < length ? (a.rows + RT - 1) / RT : 0, each = (all_tiles + a.splits - 1) / a.splits;
+    const int first = split * each, last = first + each < all_tiles ? first + each : all_tiles;
+
+    const int state = state_tile * 128 + wave * 32 + (lane & 31);
+    const bool real = state < length && (!a.mask || a.mask[b * a.mask_batch + state]);
+    taser_frag<T> k[NC], v[NC];
+    {
+        const int64_t at = real ? state : 0;
+        const T *k_from = (const T*)a.k + b * a.k_batch + hk * a.k_head + at * a.k_token, *v_from = (const T*)a.v + b * a.v_batch + hk * a.v_head + at * a.v_token;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const int e = 16 * c + 8 * half, n = real ? a.dim - e : 0;
+            k[c] = taser_load_frag<T>(k_from + e, n);
+            v[c] = taser_load_frag<T>(v_from + e, n);
+        }
+    }
+    int64_t key_pos = 0, bound = 0, key_low = 0, key_high = 0;
+    if constexpr (BIAS) {
+        const T* from = (const T*)a.table + (int64_t)hk * a.group * a.buckets;
+        for (int i = threadIdx.x; i < a.group * a.buckets; i += 256) table[i] = (float)from[i];
+        key_pos = real ? a.key_pos[b * a.key_pos_batch + state] : 0;
+        bound = taser_lane_bound(a, lane);
+        key_low = taser_wave_min(real ? key_pos : INT64_MAX);
+        key_high = taser_wave_max(real ? key_pos : INT64_MIN);
+        __syncthreads();
+    }
+    const bool any = __any(real);
+    const T* const q_from = (const T*)a.q + b * a.q_batch;
+    auto fetch = [&](char* q, char* y, taser_f4 (*rows_info)[RT / 4], int64_t* pos, int64_t* range, int* in_table, int tile) {
+        const int at = tile * RT, n = a.rows - at;
+        const uint32_t keep = n >= 32 ? ~0u : (1u << n) - 1;
+        taser_load_tile<T, DP, RT, 256>(q, [&](int r) {
+            const int row = at + r < a.rows ? at + r : 0, query = row / a.group;
+            return q_from + query * a.q_token + (int64_t)(hk * a.group + row - query * a.group) * a.q_head;
+        }, keep, a.dim, a.direct, threadIdx.x);
+        taser_load_tile<T, DP, RT, 256>(y, [&](int r) {
+            const int row = at + r < a.rows ? at + r : 0, query = row / a.group;
+            return dout + (((int64_t)b * a.queries + query) * a.heads + hk * a.group + row - query * a.group) * a.dim;
+        }, keep, a.dim, a.direct, threadIdx.x);
+        if (threadIdx.x < 64) {
+            const bool there = lane < n && lane < RT;
+            const int row = there ? at + lane : 0, query = row / a.group, g = row - query * a.group;
+            taser_f4 w = {INFINITY, 0.f, 0.f, INFINITY};
+            if (there) w = info[((int64_t)b * a.queries + query) * a.heads + hk * a.group + g];
+            if (lane < RT)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ((float*)rows_info[i])[lane] = w[i];
+            if constexpr (BIAS) {
+                const int64_t p = there ? a.query_pos[b * a.query_pos_batch + query] : 0;
+                if (lane < RT) {
+                    pos[lane] = p;
+                    in_table[lane] = g * a.buckets;
+                }
+                const int64_t low = taser_wave_min(there ? p : INT64_MAX), high = taser_wave_max(there ? p : INT64_MIN);
+                if (lane == 0) {
+                    range[0] = low;
+                    range[1] = high;
+                }
+            }
+        }
+    };
+
+    // Weights are at most 1: in half precision they are 2^14 times as large where dv's product takes them.
+    constexpr float lift = std::is_same_v<T, _Float16> ? 16384.f : 1.f;
+    taser_f16 sum_k[ND], sum_v[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum_k[d][r] = sum_v[d][r] = 0.f;
+    const float scale2 = a.scale * kLog2e;
+
+    auto compute = [&](const char* q, const char* y, const taser_f4 (*rows_info)[RT / 4], const int64_t* pos, const int64_t* range, const int* in_table) {
+        if (!any) return;
+        taser_f16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            taser_mma(s, taser_rows_operand<T, DP>(q, 0, c, lane), k[c]);
+            taser_mma(dp, taser_rows_operand<T, DP>(y, 0, c, lane), v[c]);
+        }
+        if constexpr (BIAS) {
+            const int low = taser_uniform_bucket(bound, taser_apart(range[0], key_high)), high = taser_uniform_bucket(bound, taser_apart(range[1], key_low));
+            int bucket[16];
+            if (low == high) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) bucket[r] = low;
+            } else {   // distances count the other way round here: bound <= query - key
+                int64_t apart[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    apart[r] = taser_apart(pos[8 * (r >> 2) + 4 * half + (r & 3)], key_pos);
+                    bucket[r] = low;
+                }
+                for (int i = low; i < high; ++i) {
+                    const int64_t x = taser_lane_value(bound, i);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) bucket[r] += x <= apart[r];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale, table[in_table[8 * (r >> 2) + 4 * half + (r & 3)] + bucket[r]]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const taser_f4 top = rows_info[0][2 * j + half], inverse = rows_info[1][2 * j + half], t = rows_info[2][2 * j + half], whole = rows_info[3][2 * j + half];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 4 * j + i;
+                float p = BIAS ? __builtin_amdgcn_exp2f((s[r] - top[i]) * kLog2e) * inverse[i] : __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -whole[i]));
+                if (!real) p = 0.f;
+                s[r] = p;
+                dp[r] = p * (dp[r] - t[i]);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const taser_frag<T> p = taser_operand<T>(s, h, lift), x = taser_operand<T>(dp, h);
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                taser_mma(sum_v[d], taser_columns_operand<T, DP>(y, 16 * h, d, lane), p);
+                taser_mma(sum_k[d], taser_columns_operand<T, DP>(q, 16 * h, d, lane), x);
+            }
+        }
+    };
+
+    int tile = first;
+    if (tile < last) fetch(q0, y0, info0, pos0, range0, at0, tile);
+    for (; tile < last; tile += 2) {
+        taser_loads_arrived();
+        __syncthreads();
+        if (tile + 1 < last) fetch(q1, y1, info1, pos1, range1, at1, tile + 1);
+        compute(q0, y0, info0, pos0, range0, at0);
+        if (tile + 1 >= last) break;
+        taser_loads_arrived();
+        __syncthreads();
+        if (tile + 2 < last) fetch(q0, y0, info0, pos0, range0, at0, tile + 2);
+        compute(q1, y1, info1, pos1, range1, at1);
+    }
+
+    if (state >= a.keys) return;
+    const int64_t at = (((int64_t)b * a.keys + state) * a.kv_heads + hk) * a.dim, all = (int64_t)a.batch * a.keys * a.kv_heads * a.dim;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 32 * d + 8 * j + 4 * half;
+            T x[4], y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float one = sum_k[d][4 * j + i] * a.scale, two = sum_v[d][4 * j + i] * (1.f / lift);
+                x[i] = (T)one;
+                y[i] = (T)two;
+                if (part_dk && e + i < a.dim) {
+                    part_dk[split * all + at + e + i] = one;
+                    part_dv[split * all + at + e + i] = two;
+                }
+            }
+            if (part_dk) continue;
+            taser_store(dk + at + e, a.dim - e, x);
+            taser_store(dv + at + e, a.dim - e, y);
+        }
+}
+
+// Adds up parts, in their order.
+template <typename T> __global__ __launch_bounds__(256) void attention_grad_add_kernel(const float* parts, int32_t n_parts, int64_t n, T* out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    float x = 0.f;
+    for (int p = 0; p < n_parts; ++p) x += parts[p * n + i];
+    out[i] = (T)x;
+}
+
+// dtable of one head: parts [batch, kv_heads, per_pair][group, buckets], four chains of sums.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_grad_table_kernel(const float* parts, int32_t batch, int32_t kv_heads, int32_t group, int32_t per_pair, int32_t buckets, T* dtable) {
+    __shared__ float sums[4][64];
+    const int head = blockIdx.x, hk = head / group, g = head - hk * group, chain = threadIdx.x >> 6, u = threadIdx.x & 63;
+    float x = 0.f;
+    if (u < buckets)
+        for (int64_t i = chain; i < (int64_t)batch * per_pair; i += 4) {
+            const int64_t item = (i / per_pair * kv_heads + hk) * per_pair + i % per_pair;
+            x += parts[(item * group + g) * buckets + u];
+        }
+    sums[chain][u] = x;
+    __syncthreads();
+    if ((int)threadIdx.x < buckets) dtable[(int64_t)head * buckets + u] = (T)((sums[0][u] + sums[1][u]) + (sums[2][u] + sums[3][u]));
+}
+
+struct Plan {
+    int row_tiles, row_splits, state_tiles, state_splits;   // row_splits: parts of the states that a tile of rows goes over, and the other way round
+    uint64_t info, dq, dk, dv, table, bytes;                // places in the workspace
+};
+
+Plan plan(const TaserAttentionArgs& a) {
+    Plan p = {};
+    const int64_t pairs = (int64_t)a.batch * a.kv_heads;
+    auto parts = [&](int64_t blocks, int64_t most) {
+        const int64_t n = blocks ? (512 + blocks - 1) / blocks : 1;
+        return (int)(n < most ? (n < 1 ? 1 : n) : (most < 1 ? 1 : (most > 64 ? 64 : most)));
+    };
+    p.row_tiles = (int)(((int64_t)a.rows + 127) / 128);
+    p.state_tiles = (int)(((int64_t)a.keys + 127) / 128);
+    p.row_splits = parts(pairs * p.row_tiles, a.keys / 256);
+    p.state_splits = parts(pairs * p.state_tiles, a.rows / 256);
+    auto take = [&](uint64_t bytes) {
+        const uint64_t at = p.bytes;
+        p.bytes += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const uint64_t rows = (uint64_t)a.batch * a.queries * a.heads, states = (uint64_t)a.batch * a.keys * a.kv_heads * a.dim;
+    p.info = take(rows * 16);
+    p.dq = take(p.row_splits > 1 ? p.row_splits * rows * a.dim * 4 : 0);
+    p.dk = take(p.state_splits > 1 ? p.state_splits * states * 4 : 0);
+    p.dv = take(p.state_splits > 1 ? p.state_splits * states * 4 : 0);
+    p.table = take(a.table ? (uint64_t)pairs * p.row_tiles * p.row_splits * a.group * a.buckets * 4 : 0);
+    return p;
+}
+
+template <typename T> int add_up(const float* parts, int n_parts, int64_t n, T* out, hipStream_t stream) {
+    TaserProfileSpan span(stream, "attention_grad_add");
+    attention_grad_add_kernel<T><<<dim3((unsigned)((n + 255) / 256)), 256, 0, stream>>>(parts, n_parts, n, out);
+    TASER_HIP_TRY(hipGetLastError());
+    return TASER_OK;
+}
+
+template <typename T, int DP>
+int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stats, const T* dout, T* dq, T* dk, T* dv, T* dtable, char* work, hipStream_t stream) {
+    const int64_t rows = (int64_t)a.batch * a.queries * a.heads, states = (int64_t)a.batch * a.keys * a.kv_heads * a.dim, pairs = (int64_t)a.batch * a.kv_heads;
+    taser_f4* info = (taser_f4*)(work + p.info);
+    if (rows) {
+        TaserProfileSpan span(stream, "attention_grad_rows");
+        attention_grad_rows_kernel<T><<<dim3((unsigned)((rows + 15) / 16)), 256, 0, stream>>>(out, dout, stats, a.stat_floats, rows, a.dim, info);
+        TASER_HIP_TRY(hipGetLastError());
+    }
+    float* part_table = (float*)(work + p.table);
+    if (rows) {
+        a.row_tiles = p.row_tiles;
+        a.splits = p.row_splits;
+        float* part = p.row_splits > 1 ? (float*)(work + p.dq) : nullptr;
+        const int64_t items = pairs * p.row_tiles * p.row_splits;
+        const dim3 grid((unsigned)taser_stretched_grid(items));
+        {
+            TaserProfileSpan span(stream, "attention_grad_queries");
+            if (a.table)
+                attention_grad_queries_kernel<T, DP, true><<<grid, 256, sizeof(float) * (a.group + 128) * a.buckets, stream>>>(a, info, dout, dq, part, part_table, items);
+            else
+                attention_grad_queries_kernel<T, DP, false><<<grid, 256, 0, stream>>>(a, info, dout, dq, part, part_table, items);
+            TASER_HIP_TRY(hipGetLastError());
+        }
+        if (part)
+            if (const int rc = add_up<T>(part, p.row_splits, rows * a.dim, dq, stream)) return rc;
+    }
+    if (a.table) {
+        TaserProfileSpan span(stream, "attention_grad_table");
+        attention_grad_table_kernel<T><<<dim3((unsigned)a.heads), 256, 0, stream>>>(part_table, rows ? a.batch : 0, a.kv_heads, a.group, p.row_tiles * p.row_splits, a.buckets, dtable);
+        TASER_HIP_TRY(hipGetLastError());
+    }
+    if (states) {
+        a.row_tiles = p.state_tiles;
+        a.splits = p.state_splits;
+        float* part = p.state_splits > 1 ? (float*)(work + p.dk) : nullptr;
+        float* part_v = p.state_splits > 1 ? (float*)(work + p.dv) : nullptr;
+        const int64_t items = pairs * p.state_tiles * p.state_splits;
+        const dim3 grid((unsigned)taser_stretched_grid(items));
+        // rows are loaded here: q and dout have to be aligned for loads past the registers
+        const int whole = 16 / (int)sizeof(T);
+        a.direct = a.dim % whole == 0 && ((uintptr_t)a.q | (uintptr_t)dout) % 16 == 0 && a.q_batch % whole == 0 && a.q_token % whole == 0 && a.q_head % whole == 0;
+        {
+            TaserProfileSpan span(stream, "attention_grad_states");
+            if (a.table)
+                attention_grad_states_kernel<T, DP, true><<<grid, 256, sizeof(float) * a.group * a.buckets, stream>>>(a, info, dout, dk, dv, part, part_v, items);
+            else
+                attention_grad_states_kernel<T, DP, false><<<grid, 256, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
+            TASER_HIP_TRY(hipGetLastError());
+        }
+        if (part) {
+            if (const int rc = add_up<T>(part, p.state_splits, states, dk, stream)) return rc;
+            if (const int rc = add_up<T>(part_v, p.state_splits, states, dv, stream)) return rc;
+        }
+    }
+    return TASER_OK;
+}
+
+template <typename T>
+int launch_typed(TaserAttentionArgs& a, const Plan& p, const void* out, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, char* work, hipStream_t stream) {
+    if (a.dim <= 64) return launch<T, 64>(a, p, (const T*)out, stats, (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (T*)dtable, work, stream);
+    return launch<T, 128>(a, p, (const T*)out, stats, (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (T*)dtable, work, stream);
+}
+
+}  // namespace
+
+uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t) { return plan(a).bytes; }
+
+extern "C" int taser_cross_attention_grad(const taser_attention* arg, const void* out, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, void* work,
+                                          uint64_t work_size, void* hip_stream) {
+    TaserAttentionArgs a;
+    if (const int rc = taser_attention_args(arg, "cross_attention_grad", &a)) return rc;
+    const bool rows = a.batch && a.queries, states = a.batch && a.keys;
+    if (rows && (!out || !stats || !dout || !dq)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null output, statistics or gradient of the queries' side");
+    if (states && (!dk || !dv)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null gradient of the states");
+    if (a.table && !dtable) return taser_fail(TASER_E_ARG, "cross_attention_grad: null gradient of the bias table");
+    const Plan p = plan(a);
+    if (p.bytes > work_size)
+        return taser_fail(TASER_E_RANGE, "cross_attention_grad: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)p.bytes);
+    if (p.bytes && (!work || (uintptr_t)work % 16)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null or misaligned workspace");
+    if ((int64_t)a.batch * a.kv_heads * ((int64_t)p.row_tiles * p.row_splits + (int64_t)p.state_tiles * p.state_splits) > INT32_MAX / 2)
+        return taser_fail(TASER_E_RANGE, "cross_attention_grad: too many queries, states and batch entries for one launch");
+    hipStream_t stream = (hipStream_t)hip_stream;
+    taser_clear_stale_hip_error();
+    if (arg->type == TASER_F32) return launch_typed<float>(a, p, out, stats, dout, dq, dk, dv, dtable, (char*)work, stream);
+    if (arg->type == TASER_F16) return launch_typed<_Float16>(a, p, out, stats, dout, dq, dk, dv, dtable, (char*)work, stream);
+    return launch_typed<__bf16>(a, p, out, stats, dout, dq, dk, dv, dtable, (char*)work, stream);
+}

@@ -11,6 +11,8 @@
 // two kernel launches take about 6; its kernels take 9.
 #include <Python.h>
 
+#include <cmath>
+
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -30,6 +32,13 @@ struct Api {
     decltype(&taser_selector_draw) selector_draw;
     decltype(&taser_selector_update) selector_update;
     decltype(&taser_selector_scores) selector_scores;
+    decltype(&taser_cross_attention_bytes) cross_attention_bytes;
+    decltype(&taser_cross_attention) cross_attention;
+    decltype(&taser_cross_attention_grad) cross_attention_grad;
+    decltype(&taser_relative_bias_bytes) relative_bias_bytes;
+    decltype(&taser_relative_bias) relative_bias;
+    decltype(&taser_relative_bias_grad) relative_bias_grad;
+    decltype(&taser_policy_loss) policy_loss;
     decltype(&taser_last_error) last_error;
 } api;
 PyObject* error_class = nullptr;                                  // TaserError
@@ -363,6 +372,242 @@ PyObject* scores(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- attention, the bias by distance, the policy loss ------------------------------------------
+bool element_type(at::ScalarType t, int32_t* type) {
+    *type = t == at::kFloat ? TASER_F32 : t == at::kHalf ? TASER_F16 : TASER_BF16;
+    return t == at::kFloat || t == at::kHalf || t == at::kBFloat16;
+}
+// A device tensor of `dims` dimensions whose last one is adjacent in memory.
+const at::Tensor* strided(PyObject* o, int64_t dims, at::ScalarType type) {
+    const at::Tensor* t = plain(o);
+    return t && t->scalar_type() == type && t->is_cuda() && t->layout() == at::kStrided && t->dim() == dims && (t->size(dims - 1) <= 1 || t->stride(dims - 1) == 1) ? t : nullptr;
+}
+bool get_float(PyObject* o, float* v) {
+    if (!PyFloat_CheckExact(o)) return false;
+    *v = (float)PyFloat_AS_DOUBLE(o);
+    return true;
+}
+bool positions(const at::Tensor* t, int64_t batch, int64_t n, const int64_t** p, int64_t* stride) {
+    if (!t || t->size(1) != n || (t->size(0) != 1 && t->size(0) != batch)) return false;
+    *p = static_cast<const int64_t*>(t->data_ptr());
+    *stride = t->size(0) > 1 ? t->stride(0) : 0;
+    return true;
+}
+
+// (q, k, v, lengths, mask, bias, scale) -> the argument block
+bool attention_block(PyObject* const* o, taser_attention* a, const at::Tensor** query) {
+    const at::Tensor* q = plain(o[0]);
+    *a = taser_attention{};
+    if (!q || !element_type(q->scalar_type(), &a->type) || !(q = strided(o[0], 4, q->scalar_type()))) return false;
+    const at::Tensor *k = strided(o[1], 4, q->scalar_type()), *v = k ? strided(o[2], 4, q->scalar_type()) : nullptr;
+    if (!v || k->sizes() != v->sizes() || k->size(0) != q->size(0) || k->size(3) != q->size(3)) return false;
+    if (q->size(2) > 65536 || k->size(2) > 65536 || q->size(3) < 1 || q->size(3) > TASER_MAX_HEAD_DIM) return false;
+    a->batch = q->size(0);
+    a->queries = q->size(1);
+    a->heads = (int32_t)q->size(2);
+    a->head_dim = (int32_t)q->size(3);
+    a->keys = k->size(1);
+    a->kv_heads = (int32_t)k->size(2);
+    a->q = q->data_ptr();
+    a->k = k->data_ptr();
+    a->v = v->data_ptr();
+    for (int i = 0; i < 3; ++i) {
+        a->q_strides[i] = q->stride(i);
+        a->k_strides[i] = k->stride(i);
+        a->v_strides[i] = v->stride(i);
+    }
+    if (o[3] != Py_None) {
+        const at::Tensor* t = device_array(o[3], at::kInt);
+        if (!t || t->numel() != a->batch) return false;
+        a->lengths = static_cast<const int32_t*>(t->data_ptr());
+    }
+    if (o[4] != Py_None) {
+        const at::Tensor* t = strided(o[4], 2, at::kBool);
+        if (!t || t->size(0) != a->batch || t->size(1) != a->keys) return false;
+        a->mask = static_cast<const uint8_t*>(t->data_ptr());
+        a->mask_stride = t->stride(0);
+    }
+    if (o[5] != Py_None) {
+        if (!PyTuple_CheckExact(o[5]) || PyTuple_GET_SIZE(o[5]) != 4) return false;
+        const at::Tensor *table = device_array(PyTuple_GET_ITEM(o[5], 0), q->scalar_type()), *bounds = device_array(PyTuple_GET_ITEM(o[5], 1), at::kLong);
+        if (!table || !bounds || table->dim() != 2 || table->size(0) != a->heads || bounds->numel() != table->size(1) - 1 || table->size(1) > TASER_MAX_BUCKETS) return false;
+        if (!positions(strided(PyTuple_GET_ITEM(o[5], 2), 2, at::kLong), a->batch, a->queries, &a->query_pos, &a->query_pos_stride) ||
+            !positions(strided(PyTuple_GET_ITEM(o[5], 3), 2, at::kLong), a->batch, a->keys, &a->key_pos, &a->key_pos_stride))
+            return false;
+        a->buckets = (int32_t)table->size(1);
+        a->bias_table = table->data_ptr();
+        a->bounds = static_cast<const int64_t*>(bounds->data_ptr());
+    }
+    if (o[6] == Py_None) a->scale = (float)(1.0 / std::sqrt((double)a->head_dim));
+    else if (!get_float(o[6], &a->scale)) return false;
+    *query = q;
+    return true;
+}
+at::Tensor scratch(uint64_t bytes, const at::Tensor& like) { return bytes ? make({(int64_t)bytes}, at::kByte, like.device()) : at::Tensor(); }
+
+// (q, k, v, lengths, mask, bias, scale, want_stats), on torch's current stream
+PyObject* attention(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_attention a;
+    const at::Tensor* q;
+    void* stream;
+    uint64_t bytes = 0;
+    if (n_args != 8 || !PyBool_Check(o[7]) || !attention_block(o, &a, &q) || !get_stream(Py_None, &stream)) return not_plain();
+    if (const int rc = api.cross_attention_bytes(&a, &bytes, nullptr)) return raise(rc);
+    const at::Tensor out = make(q->sizes(), q->scalar_type(), q->device()), work = scratch(bytes, *q);
+    at::Tensor stats;
+    if (o[7] == Py_True) stats = make({a.batch, a.queries, a.heads, TASER_ATTENTION_STATS(a.type, a.head_dim)}, at::kFloat, q->device());
+    void *p_out = out.data_ptr(), *p_stats = stats.defined() ? stats.data_ptr() : nullptr, *p_work = bytes ? work.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.cross_attention(&a, p_out, static_cast<float*>(p_stats), p_work, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    if (o[7] != Py_True) return THPVariable_Wrap(out);
+    Ref x(THPVariable_Wrap(out)), y(THPVariable_Wrap(stats));
+    return x.p && y.p ? PyTuple_Pack(2, x.p, y.p) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// (dout, q, k, v, out, stats, lengths, mask, bias, scale), on torch's current stream
+PyObject* attention_grad(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_attention a;
+    const at::Tensor* q;
+    void* stream;
+    uint64_t bytes = 0;
+    if (n_args != 10) return not_plain();
+    PyObject* const block[7] = {o[1], o[2], o[3], o[6], o[7], o[8], o[9]};
+    if (!attention_block(block, &a, &q) || !get_stream(Py_None, &stream)) return not_plain();
+    const at::Tensor *dout = device_array(o[0], q->scalar_type()), *out = device_array(o[4], q->scalar_type()), *stats = device_array(o[5], at::kFloat);
+    if (!dout || !out || !stats || dout->sizes() != q->sizes() || out->sizes() != q->sizes() || stats->sizes() != at::IntArrayRef({a.batch, a.queries, a.heads, TASER_ATTENTION_STATS(a.type, a.head_dim)}))
+        return not_plain();
+    if (const int rc = api.cross_attention_bytes(&a, nullptr, &bytes)) return raise(rc);
+    const at::IntArrayRef states = plain(o[2])->sizes();
+    const at::Tensor dq = make(q->sizes(), q->scalar_type(), q->device()), dk = make(states, q->scalar_type(), q->device()), dv = make(states, q->scalar_type(), q->device()),
+                     work = scratch(bytes, *q);
+    at::Tensor dtable;
+    if (a.bias_table) dtable = make({a.heads, a.buckets}, q->scalar_type(), q->device());
+    const void *p_out = out->data_ptr(), *p_stats = stats->data_ptr(), *p_dout = dout->data_ptr();
+    void *p_dq = dq.data_ptr(), *p_dk = dk.data_ptr(), *p_dv = dv.data_ptr(), *p_dtable = dtable.defined() ? dtable.data_ptr() : nullptr, *p_work = bytes ? work.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.cross_attention_grad(&a, p_out, static_cast<const float*>(p_stats), p_dout, p_dq, p_dk, p_dv, p_dtable, p_work, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    Ref x(THPVariable_Wrap(dq)), y(THPVariable_Wrap(dk)), z(THPVariable_Wrap(dv)), t(dtable.defined() ? THPVariable_Wrap(dtable) : nullptr);
+    if (!x.p || !y.p || !z.p || (dtable.defined() && !t.p)) return nullptr;
+    return PyTuple_Pack(4, x.p, y.p, z.p, t.p ? t.p : Py_None);
+    END_HANDLE_TH_ERRORS
+}
+
+// (bounds, query positions, key positions) of a bias over `batch` entries (-1: the larger of the positions')
+bool distance_block(PyObject* const* o, int64_t batch, taser_distances* d) {
+    const at::Tensor *bounds = device_array(o[0], at::kLong), *from = strided(o[1], 2, at::kLong), *to = strided(o[2], 2, at::kLong);
+    if (!bounds || !from || !to || bounds->numel() >= TASER_MAX_BUCKETS) return false;
+    d->batch = batch >= 0 ? batch : (from->size(0) > to->size(0) ? from->size(0) : to->size(0));
+    d->queries = from->size(1);
+    d->keys = to->size(1);
+    d->buckets = (int32_t)bounds->numel() + 1;
+    d->bounds = static_cast<const int64_t*>(bounds->data_ptr());
+    return positions(from, d->batch, d->queries, &d->query_pos, &d->query_pos_stride) && positions(to, d->batch, d->keys, &d->key_pos, &d->key_pos_stride);
+}
+
+// (table, bounds, query positions, key positions), on torch's current stream
+PyObject* bias(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_distances d = {};
+    void* stream;
+    const at::Tensor* table = n_args == 4 ? plain(o[0]) : nullptr;
+    if (!table || !element_type(table->scalar_type(), &d.type) || !(table = device_array(o[0], table->scalar_type())) || table->dim() != 2 || table->size(0) > 65535 ||
+        !distance_block(o + 1, -1, &d) || table->size(1) != d.buckets || !get_stream(Py_None, &stream))
+        return not_plain();
+    d.heads = (int32_t)table->size(0);
+    const at::Tensor out = make({d.batch, d.heads, d.queries, d.keys}, table->scalar_type(), table->device());
+    const void* p_table = table->data_ptr();
+    void* p_out = out.data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.relative_bias(&d, p_table, p_out, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (dbias, bounds, query positions, key positions), on torch's current stream
+PyObject* bias_grad(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_distances d = {};
+    void* stream;
+    uint64_t bytes = 0;
+    const at::Tensor* dbias = n_args == 4 ? plain(o[0]) : nullptr;
+    if (!dbias || !element_type(dbias->scalar_type(), &d.type) || !(dbias = strided(o[0], 4, dbias->scalar_type())) || dbias->size(1) > 65535 ||
+        !distance_block(o + 1, dbias->size(0), &d) || dbias->size(2) != d.queries || dbias->size(3) != d.keys || !get_stream(Py_None, &stream))
+        return not_plain();
+    d.heads = (int32_t)dbias->size(1);
+    if (const int rc = api.relative_bias_bytes(&d, &bytes)) return raise(rc);
+    const at::Tensor out = make({d.heads, d.buckets}, dbias->scalar_type(), dbias->device()), work = scratch(bytes, *dbias);
+    const int64_t strides[3] = {dbias->stride(0), dbias->stride(1), dbias->stride(2)};
+    const void* p_dbias = dbias->data_ptr();
+    void *p_out = out.data_ptr(), *p_work = bytes ? work.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.relative_bias_grad(&d, p_dbias, strides, p_out, p_work, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    return THPVariable_Wrap(out);
+    END_HANDLE_TH_ERRORS
+}
+
+// (logits, actions, advantage, old_logp, ref_logp, count, weight, clip_low, clip_high, kl, want_grad, stream)
+PyObject* policy(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_policy_batch p = {};
+    void* stream;
+    const at::Tensor* logits = n_args == 12 ? plain(o[0]) : nullptr;
+    if (!logits || !element_type(logits->scalar_type(), &p.type) || !(logits = strided(o[0], 2, logits->scalar_type()))) return not_plain();
+    const at::Tensor* actions = device_array(o[1], at::kInt);
+    if (!actions || actions->dim() != 2 || actions->size(0) != logits->size(0) || actions->size(1) > TASER_MAX_PICKS) return not_plain();
+    const float* given[4] = {};   // advantage, old_logp, ref_logp, weight
+    PyObject* const of[4] = {o[2], o[3], o[4], o[6]};
+    for (int i = 0; i < 4; ++i) {
+        if (i && of[i] == Py_None) continue;
+        const at::Tensor* t = device_array(of[i], at::kFloat);
+        if (!t || t->sizes() != actions->sizes()) return not_plain();
+        given[i] = static_cast<const float*>(t->data_ptr());
+    }
+    p.rows = logits->size(0);
+    p.width = logits->size(1);
+    p.logits_stride = p.rows > 1 ? logits->stride(0) : p.width;
+    p.picks = (int32_t)actions->size(1);
+    p.logits = logits->data_ptr();
+    p.actions = static_cast<const int32_t*>(actions->data_ptr());
+    p.advantage = given[0];
+    p.old_logp = given[1];
+    p.ref_logp = given[2];
+    p.weight = given[3];
+    if (o[5] != Py_None) {
+        const at::Tensor* t = device_array(o[5], at::kInt);
+        if (!t || t->numel() != p.rows) return not_plain();
+        p.count = static_cast<const int32_t*>(t->data_ptr());
+    }
+    if (!get_float(o[7], &p.clip_low) || !get_float(o[8], &p.clip_high) || !get_float(o[9], &p.kl) || !PyBool_Check(o[10]) || !get_stream(o[11], &stream)) return not_plain();
+    const at::Tensor loss = make(actions->sizes(), at::kFloat, logits->device()), logp = make(actions->sizes(), at::kFloat, logits->device());
+    at::Tensor grad;
+    if (o[10] == Py_True) grad = make({p.rows, p.width}, logits->scalar_type(), logits->device());
+    void *p_loss = loss.data_ptr(), *p_logp = logp.data_ptr(), *p_grad = grad.defined() ? grad.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.policy_loss(&p, static_cast<float*>(p_loss), static_cast<float*>(p_logp), p_grad, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    Ref x(THPVariable_Wrap(loss)), y(THPVariable_Wrap(logp)), z(grad.defined() ? THPVariable_Wrap(grad) : nullptr);
+    if (!x.p || !y.p || (grad.defined() && !z.p)) return nullptr;
+    return PyTuple_Pack(3, x.p, y.p, z.p ? z.p : Py_None);
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(TaserError, {entry point: address})
 template <typename F> bool entry(PyObject* addresses, const char* name, F* to) {
     PyObject* o = PyDict_GetItemString(addresses, name);
@@ -379,7 +624,11 @@ PyObject* bind(PyObject*, PyObject* args) {
         !entry(addresses, "taser_gather_features", &to.gather_features) || !entry(addresses, "taser_candidate_encodings", &to.candidate_encodings) ||
         !entry(addresses, "taser_select_weighted", &to.select_weighted) || !entry(addresses, "taser_cache_lookup", &to.cache_lookup) ||
         !entry(addresses, "taser_selector_draw", &to.selector_draw) || !entry(addresses, "taser_selector_update", &to.selector_update) ||
-        !entry(addresses, "taser_selector_scores", &to.selector_scores) || !entry(addresses, "taser_last_error", &to.last_error))
+        !entry(addresses, "taser_selector_scores", &to.selector_scores) ||
+        !entry(addresses, "taser_cross_attention_bytes", &to.cross_attention_bytes) || !entry(addresses, "taser_cross_attention", &to.cross_attention) ||
+        !entry(addresses, "taser_cross_attention_grad", &to.cross_attention_grad) || !entry(addresses, "taser_relative_bias_bytes", &to.relative_bias_bytes) ||
+        !entry(addresses, "taser_relative_bias", &to.relative_bias) || !entry(addresses, "taser_relative_bias_grad", &to.relative_bias_grad) ||
+        !entry(addresses, "taser_policy_loss", &to.policy_loss) || !entry(addresses, "taser_last_error", &to.last_error))
         return nullptr;
     api = to;
     Py_INCREF(cls);
@@ -390,6 +639,7 @@ PyObject* bind(PyObject*, PyObject* args) {
 #define FAST(name, function) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(function)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, FAST("sample", sample), FAST("gather", gather), FAST("encodings", encodings),
                          FAST("select", select), FAST("lookup", lookup), FAST("draw", draw), FAST("update", update), FAST("scores", scores),
+                         FAST("attention", attention), FAST("attention_grad", attention_grad), FAST("bias", bias), FAST("bias_grad", bias_grad), FAST("policy", policy),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Native half of the Python binding, built for " TASER_BINDING_TAG ".", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,214 @@
+// Clipped policy loss with a KL term and its gradient (taser_policy_loss): one softmax a row, of which a few places are looked at.
+//
+// With l = logp of an action: d loss / d l = weight * (-ratio * advantage where that is the smaller term, + kl (1 - exp(ref - l))), and
+// d l / d logit[c] = (c is the action) - softmax[c]. So a row's gradient is minus the sum of its actions' slopes times the softmax,
+// plus each slope at its action.
+#include "attention.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Batch {
+    int32_t picks, width;
+    int64_t rows, stride;
+    const int32_t *count, *actions;
+    const float *advantage, *old_logp, *ref_logp, *weight;
+    float low, high, kl;
+};
+
+__device__ inline int32_t taking_part(const Batch& p, int64_t row) {
+    if (!p.count) return p.width;
+    const int32_t n = p.count[row];
+    return n < 0 ? 0 : (n > p.width ? p.width : n);
+}
+
+// Loss of the action at place `at` of the row's, and its slope. An action of weight 0 has neither, whatever else is given for it.
+__device__ inline void action_loss(const Batch& p, int64_t at, float logp, float* loss, float* slope) {
+    const float w = p.weight ? p.weight[at] : 1.f, a = p.advantage[at];
+    const float ratio = p.old_logp ? expf(logp - p.old_logp[at]) : 1.f;
+    const float whole = ratio * a, cut = p.old_logp ? fminf(fmaxf(ratio, 1.f - p.low), 1.f + p.high) * a : whole;
+    float x = -(cut < whole ? cut : whole), y = whole <= cut ? -whole : 0.f;
+    if (whole != whole) x = y = whole;
+    if (p.ref_logp) {
+        const float apart = p.ref_logp[at] - logp, e = expf(apart);
+        x += p.kl * (e - apart - 1.f);
+        y += p.kl * (1.f - e);
+    }
+    *loss = w != 0.f ? w * x : 0.f;
+    *slope = w != 0.f ? w * y : 0.f;
+}
+
+// Rows of at most 64 candidates and actions: G lanes a row, a candidate and an action a lane.
+template <typename T, int G>
+__global__ __launch_bounds__(256) void policy_window_kernel(const Batch p, const T* logits, float* loss, float* logp_out, T* grad) {
+    const int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    const int lane = threadIdx.x % G;
+    if (row >= p.rows) return;   // the lanes of a row leave together
+    const int n = taking_part(p, row);
+    const float x = lane < n ? (float)logits[row * p.stride + lane] : -INFINITY;
+    float top = x;
+#pragma unroll
+    for (int m = 1; m < G; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, G));
+    if (top == -INFINITY) top = 0.f;
+    const float e = lane < n ? expf(x - top) : 0.f;
+    float sum = e;
+#pragma unroll
+    for (int m = 1; m < G; m <<= 1) sum += __shfl_xor(sum, m, G);
+    const float logsum = logf(sum);
+    const int64_t at = row * p.picks + lane;
+    const int action = lane < p.picks ? p.actions[at] : -1;
+    const bool real = action >= 0 && action < n;
+    const float chosen = __shfl(x, real ? action : 0, G);
+    float l = 0.f, mine = 0.f, slope = 0.f;
+    if (real) {
+        l = (chosen - top) - logsum;
+        action_loss(p, at, l, &mine, &slope);
+    }
+    if (lane < p.picks) {
+        loss[at] = mine;
+        logp_out[at] = l;
+    }
+    if (!grad) return;
+    float all = slope;
+#pragma unroll
+    for (int m = 1; m < G; m <<= 1) all += __shfl_xor(all, m, G);
+    float g = sum > 0.f ? e / sum * -all : e * -all;
+    for (int j = 0; j < p.picks; ++j) {
+        const int a = __shfl(real ? action : -1, j, G);
+        const float y = __shfl(slope, j, G);
+        if (a == lane) g += y;
+    }
+    if (lane < p.width) grad[row * p.width + lane] = (T)(lane < n ? g : 0.f);
+}
+
+// The larger of two running (maximum, sum of exponentials).
+__device__ inline void join(float& top, float& sum, float other_top, float other_sum) {
+    const float best = fmaxf(top, other_top);
+    if (best == -INFINITY) return;
+    sum = sum * __builtin_amdgcn_exp2f((top - best) * kLog2e) + other_sum * __builtin_amdgcn_exp2f((other_top - best) * kLog2e);
+    top = best;
+}
+
+// Any row: a block goes over it twice.
+template <typename T>
+__global__ __launch_bounds__(1024) void policy_row_kernel(const Batch p, const T* logits, float* loss, float* logp_out, T* grad) {
+    constexpr int EACH = 16 / sizeof(T);
+    __shared__ float tops[16], sums[16], slopes[TASER_MAX_PICKS];
+    __shared__ int places[TASER_MAX_PICKS];
+    __shared__ float whole;
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = taking_part(p, row), waves = blockDim.x >> 6;
+    const T* from = logits + row * p.stride;
+    float top = -INFINITY, sum = 0.f;
+    for (int64_t c = threadIdx.x * EACH; c < n; c += blockDim.x * EACH) {
+        T x[EACH];
+        const int m = n - c < EACH ? (int)(n - c) : EACH;
+        taser_load<T, EACH>(from + c, m, x);
+        float best = -INFINITY, part = 0.f;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) best = i < m ? fmaxf(best, (float)x[i]) : best;
+        const float base = best == -INFINITY ? 0.f : best;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) part += i < m ? __builtin_amdgcn_exp2f(((float)x[i] - base) * kLog2e) : 0.f;
+        if (best == -INFINITY) sum += part;   // 0, or NaN
+        else join(top, sum, best, part);
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const float t = __shfl_xor(top, m), s = __shfl_xor(sum, m);
+        join(top, sum, t, s);
+    }
+    if (lane == 0) {
+        tops[wave] = top;
+        sums[wave] = sum;
+    }
+    __syncthreads();
+    top = tops[0];
+    sum = sums[0];
+    for (int w = 1; w < waves; ++w) join(top, sum, tops[w], sums[w]);
+    if (top == -INFINITY) top = 0.f;
+    if (wave == 0) {
+        const int64_t at = row * p.picks + lane;
+        const int action = lane < p.picks ? p.actions[at] : -1;
+        const bool real = action >= 0 && action < n;
+        float l = 0.f, mine = 0.f, slope = 0.f;
+        if (real) {
+            l = ((float)from[action] - top) - logf(sum);
+            action_loss(p, at, l, &mine, &slope);
+        }
+        if (lane < p.picks) {
+            loss[at] = mine;
+            logp_out[at] = l;
+            places[lane] = real ? action : -1;
+            slopes[lane] = slope;
+        }
+        float all = slope;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) all += __shfl_xor(all, m);
+        if (lane == 0) whole = all;
+    }
+    if (!grad) return;
+    __syncthreads();
+    const float by = sum > 0.f ? -whole / sum : -whole;
+    T* to = grad + row * p.width;
+    for (int64_t c = threadIdx.x * EACH; c < p.width; c += blockDim.x * EACH) {
+        T x[EACH], y[EACH];
+        const int m = n - c < EACH ? (n > c ? (int)(n - c) : 0) : EACH, writes = p.width - c < EACH ? (int)(p.width - c) : EACH;
+        taser_load<T, EACH>(from + c, m, x);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) y[i] = (T)(i < m ? __builtin_amdgcn_exp2f(((float)x[i] - top) * kLog2e) * by : 0.f);
+        if (writes == EACH) {
+            __builtin_memcpy(to + c, y, sizeof(y));
+        } else {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i)
+                if (i < writes) to[c + i] = y[i];
+        }
+    }
+    __syncthreads();   // the row is written: its actions' places are now put right
+    if ((int)threadIdx.x < p.picks && places[threadIdx.x] >= 0) {
+        const int a = places[threadIdx.x];
+        float g = __builtin_amdgcn_exp2f(((float)from[a] - top) * kLog2e) * by;
+        for (int j = 0; j < p.picks; ++j) g += places[j] == a ? slopes[j] : 0.f;
+        to[a] = (T)g;
+    }
+}
+
+template <typename T> int launch(const Batch& p, const void* logits, float* loss, float* logp, void* grad, hipStream_t stream) {
+    const int most = p.width > p.picks ? p.width : p.picks;
+    TaserProfileSpan span(stream, "policy_loss");
+    if (most <= 64) {
+        const int g = most <= 16 ? 16 : (most <= 32 ? 32 : 64);
+        const int64_t each = 256 / g;
+        const dim3 grid((unsigned)((p.rows + each - 1) / each));
+        if (g == 16) policy_window_kernel<T, 16><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
+        else if (g == 32) policy_window_kernel<T, 32><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
+        else policy_window_kernel<T, 64><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
+    } else {
+        const int threads = p.width <= 4096 ? 256 : 1024;
+        policy_row_kernel<T><<<dim3((unsigned)p.rows), threads, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
+    }
+    TASER_HIP_TRY(hipGetLastError());
+    return TASER_OK;
+}
+
+}  // namespace
+
+extern "C" int taser_policy_loss(const taser_policy_batch* b, float* loss, float* logp, void* grad, void* hip_stream) {
+    if (!b) return taser_fail(TASER_E_ARG, "policy_loss: null argument block");
+    if (b->type < TASER_F32 || b->type > TASER_BF16) return taser_fail(TASER_E_ARG, "policy_loss: unknown element type %d", b->type);
+    if (b->rows < 0 || b->width < 1 || b->picks < 1) return taser_fail(TASER_E_ARG, "policy_loss: negative number of rows, or no candidates or actions");
+    if (b->picks > TASER_MAX_PICKS || b->width >= (int64_t)1 << 31 || b->rows >= (int64_t)1 << 31)
+        return taser_fail(TASER_E_RANGE, "policy_loss: more than %d actions a row, or too many rows or candidates", TASER_MAX_PICKS);
+    if (!(b->clip_low >= 0.f) || !(b->clip_high >= 0.f) || !(b->kl >= 0.f)) return taser_fail(TASER_E_ARG, "policy_loss: clip_low, clip_high and kl must not be negative");
+    if (!b->rows) return TASER_OK;
+    if (!b->logits || !b->actions || !b->advantage || !loss || !logp) return taser_fail(TASER_E_ARG, "policy_loss: null logits, actions, advantages or outputs");
+    if (b->logits_stride < b->width && b->rows > 1) return taser_fail(TASER_E_ARG, "policy_loss: rows of logits overlap");
+    const Batch p{b->picks, (int32_t)b->width, b->rows, b->logits_stride, b->count, b->actions, b->advantage, b->old_logp, b->ref_logp, b->weight, b->clip_low, b->clip_high, b->kl};
+    hipStream_t stream = (hipStream_t)hip_stream;
+    taser_clear_stale_hip_error();
+    if (b->type == TASER_F32) return launch<float>(p, b->logits, loss, logp, grad, stream);
+    if (b->type == TASER_F16) return launch<_Float16>(p, b->logits, loss, logp, grad, stream);
+    return launch<__bf16>(p, b->logits, loss, logp, grad, stream);
+}
