@@ -41,6 +41,12 @@ int taser_attention_args(const taser_attention* p, const char* what, TaserAttent
 // Work of taser_cross_attention_grad in bytes.
 uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t type);
 
+// Windows of few states and rows: kernels of their own.
+bool taser_window_fits(const TaserAttentionArgs& a);
+int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out, float* stats, hipStream_t stream);
+uint64_t taser_window_grad_bytes(const TaserAttentionArgs& a);
+int taser_window_attention_grad(const TaserAttentionArgs& a, int32_t type, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, float* work, hipStream_t stream);
+
 // A batch entry's number of states.
 __device__ inline int32_t taser_length(const TaserAttentionArgs& a, int32_t b) {
     if (!a.lengths) return a.keys;

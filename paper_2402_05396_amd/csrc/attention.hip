@@ -348,6 +348,7 @@ bool few_rows(const TaserAttentionArgs& a) { return a.rows <= 64; }
 // Parts of the states, so that the chip is full where there are few rows.
 int splits_for(const TaserAttentionArgs& a) {
     const bool few = few_rows(a);
+    if (taser_window_fits(a)) return 1;
     const int64_t blocks = (int64_t)a.batch * a.kv_heads * (few ? (a.rows + 31) / 32 : (a.rows + 127) / 128);
     if (!blocks) return 1;
     const int64_t most = a.keys / (few ? 256 : 512), wanted = (512 + blocks - 1) / blocks;
@@ -422,6 +423,7 @@ extern "C" int taser_cross_attention(const taser_attention* p, void* out, float*
     if (need && (!work || (uintptr_t)work % 16)) return taser_fail(TASER_E_ARG, "cross_attention: null or misaligned workspace");
     hipStream_t stream = (hipStream_t)hip_stream;
     taser_clear_stale_hip_error();
+    if (taser_window_fits(a)) return taser_window_attention(a, p->type, out, stats, stream);
     const bool shared = !few_rows(a);
     if (p->type == TASER_F32) return launch_typed<float>(a, shared, out, stats, (float*)work, stream);
     if (p->type == TASER_F16) return launch_typed<_Float16>(a, shared, out, stats, (float*)work, stream);

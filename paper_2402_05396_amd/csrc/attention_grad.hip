@@ -539,7 +539,10 @@ int launch_typed(TaserAttentionArgs& a, const Plan& p, const void* out, const fl
 
 }  // namespace
 
-uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t) { return plan(a).bytes; }
+// Windows go their own way where there is anything to do.
+static bool window(const TaserAttentionArgs& a) { return taser_window_fits(a) && a.batch && a.queries; }
+
+uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t) { return window(a) ? taser_window_grad_bytes(a) : plan(a).bytes; }
 
 extern "C" int taser_cross_attention_grad(const taser_attention* arg, const void* out, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, void* work,
                                           uint64_t work_size, void* hip_stream) {
@@ -550,13 +553,15 @@ extern "C" int taser_cross_attention_grad(const taser_attention* arg, const void
     if (states && (!dk || !dv)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null gradient of the states");
     if (a.table && !dtable) return taser_fail(TASER_E_ARG, "cross_attention_grad: null gradient of the bias table");
     const Plan p = plan(a);
-    if (p.bytes > work_size)
-        return taser_fail(TASER_E_RANGE, "cross_attention_grad: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)p.bytes);
-    if (p.bytes && (!work || (uintptr_t)work % 16)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null or misaligned workspace");
+    const uint64_t need = taser_attention_grad_bytes(a, arg->type);
+    if (need > work_size)
+        return taser_fail(TASER_E_RANGE, "cross_attention_grad: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)need);
+    if (need && (!work || (uintptr_t)work % 16)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null or misaligned workspace");
     if ((int64_t)a.batch * a.kv_heads * ((int64_t)p.row_tiles * p.row_splits + (int64_t)p.state_tiles * p.state_splits) > INT32_MAX / 2)
         return taser_fail(TASER_E_RANGE, "cross_attention_grad: too many queries, states and batch entries for one launch");
     hipStream_t stream = (hipStream_t)hip_stream;
     taser_clear_stale_hip_error();
+    if (window(a)) return taser_window_attention_grad(a, arg->type, stats, dout, dq, dk, dv, dtable, (float*)work, stream);
     if (arg->type == TASER_F32) return launch_typed<float>(a, p, out, stats, dout, dq, dk, dv, dtable, (char*)work, stream);
     if (arg->type == TASER_F16) return launch_typed<_Float16>(a, p, out, stats, dout, dq, dk, dv, dtable, (char*)work, stream);
     return launch_typed<__bf16>(a, p, out, stats, dout, dq, dk, dv, dtable, (char*)work, stream);

@@ -1,0 +1,490 @@
+// Attention over windows: at most 64 states and four rows (queries and heads that share a key head) an item, thousands of items. It
+// is bound by memory: an item's keys and values are read once, all of them on their way before the first is used.
+//
+// A wavefront has an item. L lanes hold a row of the states, 16 bytes each, so 64 / L states are read at a time, in N turns; state
+// s L' + g (L' = 64 / L) is group g's in turn s. A score is a sum over a group; then lane (g, c) takes the score of turn c: each
+// state has one lane, whose softmax weight costs one exponential, and where its bucket, its gradient and the sums over all states
+// are found. The weights go back to the groups for the sums over the states.
+#include "attention.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// x of the lane whose number differs in bit M (for M < 16, among lanes that agree in the bits below: they hold the same value).
+template <int M> __device__ inline float other(float x) {
+    const int v = __builtin_bit_cast(int, x);
+    int y;
+    if constexpr (M == 1) y = __builtin_amdgcn_update_dpp(0, v, 0xb1, 0xf, 0xf, false);         // quad_perm 1 0 3 2
+    else if constexpr (M == 2) y = __builtin_amdgcn_update_dpp(0, v, 0x4e, 0xf, 0xf, false);    // quad_perm 2 3 0 1
+    else if constexpr (M == 4) y = __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false);   // row_half_mirror
+    else if constexpr (M == 8) y = __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false);   // row_ror 8
+    else return __shfl_xor(x, M);
+    return __builtin_bit_cast(float, y);
+}
+struct Pair { float a, b; };
+// {a of the lane with bit M clear, b of it} where the bit is clear ... : the two halves of a pair of values change places, so that
+// a + b is a's sum over the bit where it is clear, and b's where it is set.
+template <int M> __device__ inline Pair swapped(float a, float b, int lane) {
+    if constexpr (M == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+        const unsigned x = r[0], y = r[1];   // (a cast of r[1] itself would take element 0)
+        return {__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)};
+    } else if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+        const unsigned x = r[0], y = r[1];   // (a cast of r[1] itself would take element 0)
+        return {__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)};
+    } else {
+        const bool set = lane & M;
+        return {set ? b : a, other<M>(set ? a : b)};
+    }
+}
+template <int M> __device__ inline float add_other(float x) {
+    if constexpr (M >= 16) {
+        const Pair p = swapped<M>(x, x, 0);
+        return p.a + p.b;
+    } else {
+        return x + other<M>(x);
+    }
+}
+template <int M> __device__ inline float max_other(float x) {
+    if constexpr (M >= 16) {
+        const Pair p = swapped<M>(x, x, 0);
+        return fmaxf(p.a, p.b);
+    } else {
+        return fmaxf(x, other<M>(x));
+    }
+}
+template <int LANES> __device__ inline float group_sum(float x) {   // over LANES neighboring lanes
+    x = add_other<1>(x);
+    x = add_other<2>(x);
+    if constexpr (LANES >= 8) x = add_other<4>(x);
+    if constexpr (LANES >= 16) x = add_other<8>(x);
+    if constexpr (LANES >= 32) x = add_other<16>(x);
+    if constexpr (LANES >= 64) x = add_other<32>(x);
+    return x;
+}
+__device__ inline float wave_max(float x) {
+    x = max_other<1>(x);
+    x = max_other<2>(x);
+    x = max_other<4>(x);
+    x = max_other<8>(x);
+    x = max_other<16>(x);
+    return max_other<32>(x);
+}
+
+// Sums of E values over the groups, each lane left with the sums of E / groups of them (at least one), from element first(lane) on.
+template <int L, int E> struct Spread {
+    static constexpr int kGroups = 64 / L, kLeft = E > kGroups ? E / kGroups : 1;
+    template <int M, int N> __device__ static void step(float* x, int lane) {
+        if constexpr (M >= L) {
+            if constexpr (N > 1) {
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    const Pair p = swapped<M>(x[i], x[i + N / 2], lane);
+                    x[i] = p.a + p.b;
+                }
+                step<M / 2, N / 2>(x, lane);
+            } else {
+                x[0] = M >= 16 ? add_other<M>(x[0]) : x[0] + other<M>(x[0]);
+                step<M / 2, 1>(x, lane);
+            }
+        }
+    }
+    __device__ static void sums(float* x, int lane) { step<32, E>(x, lane); }
+    __device__ static int first(int lane) {
+        int at = 0, n = E;
+#pragma unroll
+        for (int m = 32; m >= L; m >>= 1)
+            if (n > 1) {
+                n /= 2;
+                at += lane & m ? n : 0;
+            }
+        return at;
+    }
+};
+
+template <typename T, int E> struct Chunk { T x[E]; };
+
+// A lane's 16 bytes of a row: where the row ends inside them they are its last 16 (elements of the lane before it come twice, and
+// count once, as zeros of `q`); a row shorter than 16 bytes is read element by element.
+template <typename T, int E> __device__ inline Chunk<T, E> load_chunk(const T* row, int at, int dim, bool there) {
+    Chunk<T, E> c;
+    if (dim >= E) {
+        if (there) {
+            __builtin_memcpy(c.x, row + at, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < E; ++i) c.x[i] = (T)0.f;
+        }
+    } else {
+        taser_load<T, E>(row, there ? dim : 0, c.x);
+    }
+    return c;
+}
+template <typename T, int N> __device__ inline void store_values(T* row, int at, int dim, const float (&x)[N]) {
+    T y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = (T)x[i];
+    if (at + N <= dim) {
+        __builtin_memcpy(row + at, y, sizeof(y));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (at + i < dim) row[at + i] = y[i];
+    }
+}
+
+__device__ inline int bucket_of(const int64_t* bounds, int64_t apart) {   // 64 bounds, those past the last INT64_MAX
+    int at = 0;
+#pragma unroll
+    for (int step = 32; step; step >>= 1)
+        if (bounds[at + step - 1] <= apart) at += step;
+    return at;
+}
+
+// What a wave knows of its item.
+template <typename T, int L, int N, int R> struct Item {
+    static constexpr int E = 16 / (int)sizeof(T), kGroups = 64 / L;
+    int lane, group, c, at, b, hk, state;   // at: the lane's first element; state: the lane's own
+    bool inside;                            // the lane holds elements
+    uint64_t seen;                          // by lane: its state takes part
+    const T *k, *v;
+
+    __device__ void open(const TaserAttentionArgs& a, int64_t item, int lane_) {
+        lane = lane_;
+        group = lane / L;
+        c = lane % L;
+        hk = (int)(item % a.kv_heads);
+        b = (int)(item / a.kv_heads);
+        inside = c * E < a.dim;
+        at = a.dim < E ? 0 : (c * E + E <= a.dim ? c * E : a.dim - E);
+        state = c * kGroups + group;
+        const int32_t length = taser_length(a, b);
+        seen = __ballot(c < N && state < length && (!a.mask || a.mask[b * a.mask_batch + state]));
+        k = (const T*)a.k + b * a.k_batch + hk * a.k_head;
+        v = (const T*)a.v + b * a.v_batch + hk * a.v_head;
+    }
+    __device__ int turn_state(int turn) const { return turn * kGroups + group; }
+    __device__ bool turn_seen(int turn) const { return inside && (seen >> (group * L + turn)) & 1; }
+    __device__ void load_states(const TaserAttentionArgs& a, Chunk<T, E> (&kc)[N], Chunk<T, E> (&vc)[N]) const {
+#pragma unroll
+        for (int s = 0; s < N; ++s) kc[s] = load_chunk<T, E>(k + turn_state(s) * a.k_token, at, a.dim, turn_seen(s));
+#pragma unroll
+        for (int s = 0; s < N; ++s) vc[s] = load_chunk<T, E>(v + turn_state(s) * a.v_token, at, a.dim, turn_seen(s));
+    }
+    // Row r's elements, those that the lane before has too as zeros.
+    __device__ void load_row(const T* row, int dim, bool there, float (&x)[E]) const {
+        const Chunk<T, E> y = load_chunk<T, E>(row, at, dim, there && inside);
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = at + i >= c * E ? (float)y.x[i] : 0.f;
+    }
+    __device__ float dot(const float (&x)[E], const Chunk<T, E>& y) const {
+        float d = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) d = fmaf(x[i], (float)y.x[i], d);
+        return group_sum<L>(d);
+    }
+    // The value of turn c, which is the lane's own state's.
+    __device__ float own(const float (&x)[N]) const {
+        float y = x[0];
+#pragma unroll
+        for (int s = 1; s < N; ++s) y = c == s ? x[s] : y;
+        return y;
+    }
+    __device__ float of_turn(float x, int turn) const { return __shfl(x, (lane & ~(L - 1)) + turn); }
+};
+
+// The bias table of the whole call in LDS where it fits (it does: at most 16 heads, else it is read from memory), bounds beside it.
+__device__ inline void load_bounds(const TaserAttentionArgs& a, int64_t* bounds) {
+    if (threadIdx.x < 64) bounds[threadIdx.x] = (int)threadIdx.x < a.buckets - 1 ? a.bounds[threadIdx.x] : INT64_MAX;
+    __syncthreads();
+}
+
+template <typename T, int L, int N, int R>
+__global__ __launch_bounds__(256) void window_kernel(const TaserAttentionArgs a, T* out, float* stats, int64_t items) {
+    using I = Item<T, L, N, R>;
+    constexpr int E = I::E, LEFT = Spread<L, E>::kLeft;
+    __shared__ int64_t bounds[64];
+    if (a.table) load_bounds(a, bounds);
+    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (item >= items) return;
+    I w;
+    w.open(a, item, threadIdx.x & 63);
+    Chunk<T, E> k[N], v[N];
+    w.load_states(a, k, v);
+    float q[R][E];
+    int query[R], head[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = r < a.rows ? r : 0;
+        query[r] = row / a.group;
+        head[r] = w.hk * a.group + row - query[r] * a.group;
+        w.load_row((const T*)a.q + w.b * a.q_batch + query[r] * a.q_token + head[r] * a.q_head, a.dim, r < a.rows, q[r]);
+    }
+    const bool mine = (w.seen >> w.lane) & 1;
+    const int64_t key_pos = a.table && mine ? a.key_pos[w.b * a.key_pos_batch + w.state] : 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (r >= a.rows) break;
+        float s[N];
+#pragma unroll
+        for (int t = 0; t < N; ++t) s[t] = w.dot(q[r], k[t]);
+        float x = w.own(s) * a.scale;
+        if (a.table) {
+            const int bucket = bucket_of(bounds, taser_apart(a.query_pos[w.b * a.query_pos_batch + query[r]], key_pos));
+            x += (float)((const T*)a.table)[(int64_t)head[r] * a.buckets + bucket];
+        }
+        if (!mine) x = -INFINITY;
+        const float top = wave_max(x), p = __builtin_amdgcn_exp2f((x - (top == -INFINITY ? 0.f : top)) * kLog2e), sum = group_sum<64>(p);
+        float o[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            const float y = w.of_turn(p, t);
+#pragma unroll
+            for (int i = 0; i < E; ++i) o[i] = fmaf(y, (float)v[t].x[i], o[i]);
+        }
+        Spread<L, E>::sums(o, w.lane);
+        const float inverse = sum != 0.f ? 1.f / sum : 0.f;
+        float left[LEFT];
+#pragma unroll
+        for (int i = 0; i < LEFT; ++i) left[i] = o[i] * inverse;
+        const int64_t row = ((int64_t)w.b * a.queries + query[r]) * a.heads + head[r];
+        if (w.inside) store_values<T, LEFT>(out + row * a.dim, w.at + Spread<L, E>::first(w.lane), a.dim, left);
+        if (!stats) continue;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < LEFT; ++i) left[i] -= (float)(T)left[i];
+            if (w.inside) store_values<T, LEFT>(taser_rest<T>(stats, row, a.stat_floats), w.at + Spread<L, E>::first(w.lane), a.dim, left);
+        }
+        if (w.lane == 0) {
+            stats[row * a.stat_floats] = top;
+            stats[row * a.stat_floats + 1] = sum;
+        }
+    }
+}
+
+// A wave takes every waves-th item (their number is a multiple of the key heads': a wave's items have one) and keeps the table's
+// gradient of its R rows, lane u bucket u.
+template <typename T, int L, int N, int R>
+__global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionArgs a, const T* dout, const float* stats, T* dq, T* dk, T* dv, float* part_table, int64_t items, int64_t waves) {
+    using I = Item<T, L, N, R>;
+    constexpr int E = I::E, LEFT = Spread<L, E>::kLeft;
+    __shared__ int64_t bounds[64];
+    if (a.table) load_bounds(a, bounds);
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (wave >= waves) return;
+    float table_sums[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) table_sums[r] = 0.f;
+    for (int64_t item = wave; item < items; item += waves) {
+        I w;
+        w.open(a, item, threadIdx.x & 63);
+        Chunk<T, E> k[N], v[N];
+        w.load_states(a, k, v);
+        float q[R][E], y[R][E], p[R], dx[R];
+        int64_t row[R];
+        const bool mine = (w.seen >> w.lane) & 1;
+        const int64_t key_pos = a.table && mine ? a.key_pos[w.b * a.key_pos_batch + w.state] : 0;
+        int query[R], head[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int at = r < a.rows ? r : 0;
+            query[r] = at / a.group;
+            head[r] = w.hk * a.group + at - query[r] * a.group;
+            row[r] = ((int64_t)w.b * a.queries + query[r]) * a.heads + head[r];
+            w.load_row((const T*)a.q + w.b * a.q_batch + query[r] * a.q_token + head[r] * a.q_head, a.dim, r < a.rows, q[r]);
+            w.load_row(dout + row[r] * a.dim, a.dim, r < a.rows, y[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            p[r] = dx[r] = 0.f;
+            if (r >= a.rows) continue;
+            float s[N], d[N];
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                s[t] = w.dot(q[r], k[t]);
+                d[t] = w.dot(y[r], v[t]);
+            }
+            float x = w.own(s) * a.scale;
+            const float dp = w.own(d);
+            int bucket = 0;
+            if (a.table) {
+                bucket = bucket_of(bounds, taser_apart(a.query_pos[w.b * a.query_pos_batch + query[r]], key_pos));
+                x += (float)((const T*)a.table)[(int64_t)head[r] * a.buckets + bucket];
+            }
+            const float top = stats[row[r] * a.stat_floats], sum = stats[row[r] * a.stat_floats + 1];
+            p[r] = mine && sum != 0.f ? __builtin_amdgcn_exp2f((x - top) * kLog2e) / sum : 0.f;
+            const float t = group_sum<64>(mine ? p[r] * dp : 0.f);
+            dx[r] = mine ? p[r] * (dp - t) : 0.f;
+            if (a.table) {
+                for (uint64_t left = w.seen; left; left &= left - 1) {
+                    const int l = __builtin_ctzll(left);
+                    const float one = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, dx[r]), l));
+                    table_sums[r] += __builtin_amdgcn_readlane(bucket, l) == w.lane ? one : 0.f;
+                }
+            }
+        }
+        float sums[R][E];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < E; ++i) sums[r][i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            float one[E], two[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) one[i] = two[i] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float g = w.of_turn(dx[r], t) * a.scale, f = w.of_turn(p[r], t);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    one[i] = fmaf(g, q[r][i], one[i]);
+                    two[i] = fmaf(f, y[r][i], two[i]);
+                    sums[r][i] = fmaf(g, (float)k[t].x[i], sums[r][i]);
+                }
+            }
+            // A lane whose 16 bytes reach back into the lane's before has zeros there: it writes its own elements.
+            if (w.inside && w.turn_state(t) < a.keys) {
+                const int64_t to = (((int64_t)w.b * a.keys + w.turn_state(t)) * a.kv_heads + w.hk) * a.dim;
+                if (w.at == w.c * E) {
+                    store_values<T, E>(dk + to, w.at, a.dim, one);
+                    store_values<T, E>(dv + to, w.at, a.dim, two);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < E; ++i)
+                        if (w.at + i >= w.c * E) {
+                            dk[to + w.at + i] = (T)one[i];
+                            dv[to + w.at + i] = (T)two[i];
+                        }
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            Spread<L, E>::sums(sums[r], w.lane);
+            float left[LEFT];
+#pragma unroll
+            for (int i = 0; i < LEFT; ++i) left[i] = sums[r][i];
+            if (r < a.rows && w.inside) store_values<T, LEFT>(dq + row[r] * a.dim, w.at + Spread<L, E>::first(w.lane), a.dim, left);
+        }
+    }
+    if (a.table) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < a.rows && lane < a.buckets) part_table[(wave * a.rows + r) * a.buckets + lane] = table_sums[r];
+    }
+}
+
+// dtable of one head: 16 chains of sums over the waves of its key head and their rows.
+template <typename T>
+__global__ __launch_bounds__(1024) void window_table_kernel(const float* parts, int64_t waves, int32_t kv_heads, int32_t group, int32_t rows, int32_t buckets, T* dtable) {
+    __shared__ float sums[16][64];
+    const int head = blockIdx.x, hk = head / group, g = head - hk * group, chain = threadIdx.x >> 6, u = threadIdx.x & 63;
+    float x = 0.f;
+    if (u < buckets)
+        for (int64_t i = hk + (int64_t)chain * kv_heads; i < waves; i += 16 * kv_heads)
+            for (int r = g; r < rows; r += group) x += parts[(i * rows + r) * buckets + u];
+    sums[chain][u] = x;
+    __syncthreads();
+    if ((int)threadIdx.x >= buckets) return;
+    x = 0.f;
+    for (int i = 0; i < 16; ++i) x += sums[i][u];
+    dtable[(int64_t)head * buckets + u] = (T)x;
+}
+
+struct Call {   // one of the two kernels' arguments
+    void* out;
+    float* stats;
+    const void* dout;
+    void *dq, *dk, *dv;
+    float* part_table;
+    int64_t waves;
+    hipStream_t stream;
+};
+
+template <typename T, int L, int N, int R> int run(const TaserAttentionArgs& a, const Call& c) {
+    const int64_t items = (int64_t)a.batch * a.kv_heads;
+    if (c.dout) {
+        TaserProfileSpan span(c.stream, "attention_window_grad");
+        window_grad_kernel<T, L, N, R><<<dim3((unsigned)((c.waves + 3) / 4)), 256, 0, c.stream>>>(a, (const T*)c.dout, c.stats, (T*)c.dq, (T*)c.dk, (T*)c.dv, c.part_table, items, c.waves);
+    } else {
+        TaserProfileSpan span(c.stream, "attention_window");
+        window_kernel<T, L, N, R><<<dim3((unsigned)((items + 3) / 4)), 256, 0, c.stream>>>(a, (T*)c.out, c.stats, items);
+    }
+    TASER_HIP_TRY(hipGetLastError());
+    return TASER_OK;
+}
+template <typename T, int L, int N> int run_rows(const TaserAttentionArgs& a, const Call& c) {
+    if (a.rows <= 1) return run<T, L, N, 1>(a, c);
+    if (a.rows <= 2) return run<T, L, N, 2>(a, c);
+    return run<T, L, N, 4>(a, c);
+}
+// Lanes of a row as few as hold it, turns as few as the states need, out of three.
+template <typename T, int L> int run_turns(const TaserAttentionArgs& a, const Call& c) {
+    const int turns = (a.keys + 64 / L - 1) / (64 / L);
+    if (turns <= L / 4) return run_rows<T, L, L / 4>(a, c);
+    if (turns <= L / 2) return run_rows<T, L, L / 2>(a, c);
+    return run_rows<T, L, L>(a, c);
+}
+template <typename T> int run_typed(const TaserAttentionArgs& a, const Call& c) {
+    constexpr int E = 16 / (int)sizeof(T);
+    if (a.dim <= 8 * E) return run_turns<T, 8>(a, c);
+    if constexpr (sizeof(T) == 4)
+        if (a.dim > 16 * E) return run_turns<T, 32>(a, c);
+    return run_turns<T, 16>(a, c);
+}
+int run_any(const TaserAttentionArgs& a, int32_t type, const Call& c) {
+    if (type == TASER_F32) return run_typed<float>(a, c);
+    if (type == TASER_F16) return run_typed<_Float16>(a, c);
+    return run_typed<__bf16>(a, c);
+}
+
+// Waves of the gradient: enough for the chip, a multiple of the key heads.
+int64_t grad_waves(const TaserAttentionArgs& a) {
+    const int64_t items = (int64_t)a.batch * a.kv_heads;
+    if (!a.table || items <= 4096) return items;
+    const int64_t n = 4096 / a.kv_heads * a.kv_heads;
+    return n ? n : a.kv_heads;
+}
+
+}  // namespace
+
+bool taser_window_fits(const TaserAttentionArgs& a) { return a.keys >= 1 && a.keys <= 64 && a.rows <= 4; }
+
+int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out, float* stats, hipStream_t stream) {
+    Call c = {};
+    c.out = out;
+    c.stats = stats;
+    c.stream = stream;
+    return run_any(a, type, c);
+}
+
+uint64_t taser_window_grad_bytes(const TaserAttentionArgs& a) {
+    return a.table ? (uint64_t)grad_waves(a) * a.rows * a.buckets * sizeof(float) : 0;
+}
+
+int taser_window_attention_grad(const TaserAttentionArgs& a, int32_t type, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, float* work, hipStream_t stream) {
+    Call c = {};
+    c.stats = const_cast<float*>(stats);
+    c.dout = dout;
+    c.dq = dq;
+    c.dk = dk;
+    c.dv = dv;
+    c.part_table = work;
+    c.waves = grad_waves(a);
+    c.stream = stream;
+    if (const int rc = run_any(a, type, c)) return rc;
+    if (!a.table) return TASER_OK;
+    TaserProfileSpan span(stream, "attention_window_table");
+    const dim3 grid((unsigned)a.heads);
+    if (type == TASER_F32) window_table_kernel<float><<<grid, 1024, 0, stream>>>(work, c.waves, a.kv_heads, a.group, a.rows, a.buckets, (float*)dtable);
+    else if (type == TASER_F16) window_table_kernel<_Float16><<<grid, 1024, 0, stream>>>(work, c.waves, a.kv_heads, a.group, a.rows, a.buckets, (_Float16*)dtable);
+    else window_table_kernel<__bf16><<<grid, 1024, 0, stream>>>(work, c.waves, a.kv_heads, a.group, a.rows, a.buckets, (__bf16*)dtable);
+    TASER_HIP_TRY(hipGetLastError());
+    return TASER_OK;
+}
