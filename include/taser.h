@@ -477,8 +477,9 @@ void taser_selector_free(taser_selector* s);
  *
  * taser_cross_attention: out dense [batch][queries][heads][head_dim]; stats
  *   float[batch][queries][heads][TASER_ATTENTION_STATS(type, head_dim)] or NULL:
- *   the largest x of a row (minus infinity: none), the sum of exp(x - largest),
- *   then what only the gradient reads (how far 16-bit outputs were rounded).
+ *   for each row a reference near its largest x (minus infinity: no states), the
+ *   sum of exp(x - reference), then what only the gradient reads (how far 16-bit
+ *   outputs were rounded).
  * taser_cross_attention_grad: the gradients of sum(out * dout): dq dense like
  *   out, dk and dv dense [batch][keys][kv_heads][head_dim] (zeros for states
  *   that took no part), dtable [heads][buckets] (NULL without a bias). q .. v,

@@ -720,8 +720,8 @@ def cross_attention(q, k, v, lengths=None, mask=None, bias=None, scale=None, wan
     """taser_cross_attention. q [B, queries, heads, d], k and v [B, keys, kv_heads, d] of float32, float16 or bfloat16, any strides
     with adjacent elements; lengths int32[B]; mask bool[B, keys]; bias = (table [heads, buckets] of q's type, bounds int64[buckets - 1],
     query positions int64[B or 1, queries], key positions int64[B or 1, keys]); scale d ** -0.5 unless given. Returns out (like q,
-    dense), with `want_stats` also stats float32[B, queries, heads, n]: the largest score of a row, the sum of the exponentials
-    over it, and what cross_attention_grad needs besides."""
+    dense), with `want_stats` also stats float32[B, queries, heads, n]: a reference near the row's largest score, the sum of the
+    exponentials over it, and what cross_attention_grad needs besides."""
     if stream is None:
         r = (_native or _bind()).attention(q, k, v, lengths, mask, bias, scale, want_stats)
         if r is not None:

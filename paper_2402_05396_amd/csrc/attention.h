@@ -106,9 +106,16 @@ template <typename T> __device__ inline taser_frag<T> taser_operand(const taser_
     return f;
 }
 
-// The value of the lane half a wave away.
-__device__ inline float taser_other_half(float x) {
-    return __shfl_xor(x, 32);
+// Sum and maximum over the two halves of a wave: the halves of two copies change places.
+__device__ inline float taser_halves_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned a = r[0], b = r[1];   // (a cast of r[1] itself would take element 0)
+    return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+__device__ inline float taser_halves_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+    const unsigned a = r[0], b = r[1];
+    return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------
@@ -121,93 +128,121 @@ template <int PIECES> __device__ inline int taser_swizzle(int row) {
     return PIECES == 8 ? ((x & 3) << 1) | (x >> 2) : ((x & 7) << 1) | (x >> 3);
 }
 
-__device__ const uint32_t taser_zero_piece[4] = {0, 0, 0, 0};
+// Loads tiles of ROWS rows by THREADS threads. Past the registers (`direct`) through a buffer descriptor of the tile: a lane's places
+// are the same in every tile, rows and elements that are not there lie outside the descriptor and arrive as zeros; vmcnt says when.
+// Else element by element through the registers.
+constexpr int kTaserNowhere = 0x7ffffff0, kTaserTileBytes = 0x7ff00000;   // a place outside every descriptor; more than any tile may span
+template <typename T, int DP, int ROWS, int THREADS> struct TaserTileLoader {
+    static constexpr int PIECES = DP * (int)sizeof(T) / 16, EACH = 16 / (int)sizeof(T), N = ROWS * PIECES / THREADS;
+    static_assert(ROWS * PIECES % THREADS == 0 && THREADS % 64 == 0, "");
+    int thread, dim, place[N];
+    bool direct;
+    __device__ int row(int i) const { return (i * THREADS + thread) / PIECES; }
+    __device__ int element(int i) const { return ((i * THREADS + thread) % PIECES ^ taser_swizzle<PIECES>(row(i))) * EACH; }
 
-// Loads a tile by THREADS threads: row r from row_at(r) where bit r of `keep` is set (zeros elsewhere: nothing is read there).
-// Past the registers (`direct`) it has arrived when vmcnt says so.
-template <typename T, int DP, int ROWS, int THREADS, typename F>
-__device__ inline void taser_load_tile(char* lds, F row_at, uint64_t keep, int dim, bool direct, int thread) {
-    constexpr int PIECES = DP * (int)sizeof(T) / 16, EACH = 16 / (int)sizeof(T);
-    static_assert(ROWS * PIECES % THREADS == 0, "");
-    if (direct) {
+    __device__ TaserTileLoader(int thread_, int dim_, bool direct_) : thread(thread_), dim(dim_), direct(direct_) {}
+    // row_at(r): elements from the tile's base to row r.
+    template <typename F> __device__ void set(F row_at) {
 #pragma unroll
-        for (int i = 0; i < ROWS * PIECES / THREADS; ++i) {
-            const int at = i * THREADS + thread, row = at / PIECES, c = (at % PIECES) ^ taser_swizzle<PIECES>(row);
-            const bool there = (keep >> row) & 1 && c * EACH < dim;
-            const void* from = there ? (const void*)(row_at(row) + c * EACH) : (const void*)taser_zero_piece;
-            char* to = lds + (at & ~63) * 16;   // a wave writes 1 KiB from a common address on
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-        }
-    } else {
+        for (int i = 0; i < N; ++i) place[i] = element(i) < dim ? (int)((row_at(row(i)) + element(i)) * (int)sizeof(T)) : kTaserNowhere;
+    }
+    // `bytes` from base on belong to rows that are there (direct), of which those without their bit of `keep` are left out (if `some`
+    // are); row_at as for set.
+    template <typename F> __device__ void load(char* lds, const T* base, int bytes, uint64_t keep, bool some, F row_at) const {
+        if (direct) {
+            const auto tile = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int at = place[i];
+                if (some) at = (keep >> row(i)) & 1 ? at : kTaserNowhere;
+                char* to = lds + (((i * THREADS + thread) & ~63) << 4);   // a wave writes 1 KiB from a common address on
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(tile, (__attribute__((address_space(3))) void*)to, 16, at, 0, 0, 0);
+            }
+        } else {
 #pragma unroll 1
-        for (int i = 0; i < ROWS * PIECES / THREADS; ++i) {
-            const int at = i * THREADS + thread, row = at / PIECES, c = (at % PIECES) ^ taser_swizzle<PIECES>(row);
-            T x[EACH];
-            taser_load<T, EACH>(row_at(row) + c * EACH, (keep >> row) & 1 ? dim - c * EACH : 0, x);
-            taser_u4 u;
-            __builtin_memcpy(&u, x, 16);
-            *(taser_u4*)(lds + at * 16) = u;
+            for (int i = 0; i < N; ++i) {
+                T x[EACH];
+                taser_load<T, EACH>(base + row_at(row(i)) + element(i), (keep >> row(i)) & 1 ? dim - element(i) : 0, x);
+                taser_u4 u;
+                __builtin_memcpy(&u, x, 16);
+                *(taser_u4*)(lds + ((i * THREADS + thread) << 4)) = u;
+            }
         }
     }
-}
+};
+// Bytes of n rows that are `stride` bytes apart, of which the last is `row` bytes.
+__device__ inline int taser_span(int n, int64_t stride, int row) { return n > 0 ? (int)((n - 1) * stride) + row : 0; }
 
 // Waits for this wave's loads past the registers (and all other loads).
 __device__ inline void taser_loads_arrived() {
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
 }
 
-// Operand of a tile's rows (lane l: row l % 32 of the 32 from `row0` on), contraction over elements 16 kk ..
-template <typename T, int DP> __device__ inline taser_frag<T> taser_rows_operand(const char* lds, int row0, int kk, int lane) {
-    constexpr int PIECES = DP * (int)sizeof(T) / 16;
-    const int row = row0 + (lane & 31), half = lane >> 5;
-    const char* at = lds + row * (DP * (int)sizeof(T));
-    const int s = taser_swizzle<PIECES>(row);
-    taser_frag<T> f;
-    if constexpr (sizeof(T) == 2) {
-        const taser_u4 u = *(const taser_u4*)(at + (((2 * kk + half) ^ s) << 4));
-        __builtin_memcpy(&f, &u, 16);
-    } else {
-        const taser_f4 x = *(const taser_f4*)(at + (((4 * kk + 2 * half) ^ s) << 4)), y = *(const taser_f4*)(at + (((4 * kk + 2 * half + 1) ^ s) << 4));
+// Where a lane's part of a tile lies, once for all tiles: 32 rows further on, everything is 32 rows of bytes further on.
+// Operand of the tile's rows (lane l: row l % 32), contraction over elements 16 c ..
+template <typename T, int DP> struct TaserRowsAt {
+    static constexpr int PIECES = DP * (int)sizeof(T) / 16, BYTES = DP * (int)sizeof(T);
+    int at[DP / 16];
+    __device__ explicit TaserRowsAt(int lane) {
+        const int row = lane & 31, half = lane >> 5, s = taser_swizzle<PIECES>(row);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[i] = x[i];
-            f[4 + i] = y[i];
-        }
+        for (int c = 0; c < DP / 16; ++c) at[c] = row * BYTES + (((sizeof(T) == 2 ? 2 * c + half : 4 * c + 2 * half) ^ s) << 4);
     }
-    return f;
-}
-
-// Operand of a tile's columns (lane l: element 32 dt + l % 32), contraction over rows row0 + {8 j + 4 (l / 32) + i}: the transposed
-// tile in the order in which a product leaves its rows.
-template <typename T, int DP> __device__ inline taser_frag<T> taser_columns_operand(const char* lds, int row0, int dt, int lane) {
-    constexpr int PIECES = DP * (int)sizeof(T) / 16, BYTES = DP * (int)sizeof(T);
-    const int half = lane >> 5;
-    taser_frag<T> f;
-    if constexpr (sizeof(T) == 2) {
-        // 16 lanes read 4 rows of 16 elements, 8 bytes a lane, and get a column of 4 each
-        const int t = lane & 15, c = 4 * dt + 2 * ((lane >> 4) & 1) + ((t & 3) >> 1);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int row = row0 + 8 * j + 4 * half + (t >> 2);
-            const char* at = lds + row * BYTES + ((c ^ taser_swizzle<PIECES>(row)) << 4) + ((t & 1) << 3);
-            const taser_s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) taser_s4*)at);
-            T y[4];
-            __builtin_memcpy(y, &x, 8);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[4 * j + i] = y[i];
-        }
-    } else {
-        const int d = 32 * dt + (lane & 31), c = d >> 2;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
+    __device__ taser_frag<T> operand(const char* lds, int row0, int c) const {
+        taser_frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            const taser_u4 u = *(const taser_u4*)(lds + at[c] + row0 * BYTES);
+            __builtin_memcpy(&f, &u, 16);
+        } else {
+            const taser_f4 x = *(const taser_f4*)(lds + at[c] + row0 * BYTES), y = *(const taser_f4*)(lds + (at[c] ^ 16) + row0 * BYTES);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int row = row0 + 8 * j + 4 * half + i;
-                f[4 * j + i] = *(const float*)(lds + row * BYTES + ((c ^ taser_swizzle<PIECES>(row)) << 4) + ((d & 3) << 2));
+                f[i] = x[i];
+                f[4 + i] = y[i];
+            }
+        }
+        return f;
+    }
+};
+
+// Operand of the tile's columns (lane l: element 32 d + l % 32), contraction over rows row0 + {8 j + 4 (l / 32) + i}, row0 a multiple
+// of 16: the transposed tile in the order in which a product leaves its rows.
+template <typename T, int DP> struct TaserColumnsAt {
+    static constexpr int PIECES = DP * (int)sizeof(T) / 16, BYTES = DP * (int)sizeof(T), PLACES = sizeof(T) == 2 ? 2 : 8;
+    int at[DP / 32][PLACES];
+    __device__ explicit TaserColumnsAt(int lane) {
+        const int half = lane >> 5;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int j = 0; j < PLACES; ++j) {
+                if constexpr (sizeof(T) == 2) {   // 16 lanes read 4 rows of 16 elements, 8 bytes a lane, and get a column of 4 each
+                    const int t = lane & 15, c = 4 * d + 2 * ((lane >> 4) & 1) + ((t & 3) >> 1), row = 8 * j + 4 * half + (t >> 2);
+                    at[d][j] = row * BYTES + ((c ^ taser_swizzle<PIECES>(row)) << 4) + ((t & 1) << 3);
+                } else {
+                    const int e = 32 * d + (lane & 31), row = 8 * (j >> 2) + 4 * half + (j & 3);
+                    at[d][j] = row * BYTES + (((e >> 2) ^ taser_swizzle<PIECES>(row)) << 4) + ((e & 3) << 2);
+                }
             }
     }
-    return f;
-}
+    __device__ taser_frag<T> operand(const char* lds, int row0, int d) const {
+        taser_frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const taser_s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) taser_s4*)(lds + at[d][j] + row0 * BYTES));
+                T y[4];
+                __builtin_memcpy(y, &x, 8);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[4 * j + i] = y[i];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = *(const float*)(lds + at[d][j] + row0 * BYTES);
+        }
+        return f;
+    }
+};
 
 // ---- the bias by distance ----------------------------------------------------------------------------------------------
 // Lane l keeps bound l; there are at most 63. A distance common to the wave has as many bounds at most as it as lanes say so.

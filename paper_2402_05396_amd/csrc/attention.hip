@@ -28,7 +28,7 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
     __shared__ int64_t pos0[S::kTiles][BIAS ? KT : 1], pos1[S::kTiles][BIAS ? KT : 1], range0[S::kTiles][2], range1[S::kTiles][2];
     __shared__ float joined[2][S::kWaves][32];
     extern __shared__ float table[];   // [group][buckets]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t item = taser_stretch_of_work(blockIdx.x, work);
     if (item < 0) return;
     const int row_tile = (int)(item % a.row_tiles), split = (int)(item / a.row_tiles % a.splits);
@@ -71,10 +71,14 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
     };
     constexpr int THREADS = SHARED ? 64 * S::kWaves : 64;
     const int thread = SHARED ? (int)threadIdx.x : lane, slot = SHARED ? 0 : wave;
+    TaserTileLoader<T, DP, KT, THREADS> load_k(thread, a.dim, a.direct), load_v(thread, a.dim, a.direct);
+    load_k.set([&](int r) { return r * a.k_token; });
+    load_v.set([&](int r) { return r * a.v_token; });
     auto fetch = [&](char* k, char* v, int64_t* pos, int64_t* range, int tile, uint64_t keep) {
         const int64_t at = (int64_t)tile * KT;
-        taser_load_tile<T, DP, KT, THREADS>(k, [&](int r) { return k_from + (at + r) * a.k_token; }, keep, a.dim, a.direct, thread);
-        taser_load_tile<T, DP, KT, THREADS>(v, [&](int r) { return v_from + (at + r) * a.v_token; }, keep, a.dim, a.direct, thread);
+        const int n = length - tile * KT < KT ? length - tile * KT : KT, size = (int)sizeof(T);
+        load_k.load(k, k_from + at * a.k_token, taser_span(n, a.k_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.k_token; });
+        load_v.load(v, v_from + at * a.v_token, taser_span(n, a.v_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.v_token; });
         if constexpr (BIAS) {
             if (!SHARED || wave == 0) {
                 const bool there = lane < KT && (keep >> lane) & 1;
@@ -89,15 +93,19 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
         }
     };
 
-    // Half precision ends at 6e-8 below 1: there the weights, and all sums of them, are 2^14 times as large until the end.
-    constexpr float lift = std::is_same_v<T, _Float16> ? 14.f : 0.f, drop = std::is_same_v<T, _Float16> ? 1.f / 16384.f : 1.f;
+    // Half precision ends at 6e-8 below 1: there the weights, and all sums of them, are 2^10 times as large until the end.
+    constexpr float lift = std::is_same_v<T, _Float16> ? 10.f : 0.f, drop = std::is_same_v<T, _Float16> ? 1.f / 1024.f : 1.f;
+    // The reference of a row follows its largest score only when that is 2^kSlack weights away: most tiles leave the sums as they are.
+    constexpr float kSlack = 5.f;
+    const TaserRowsAt<T, DP> rows_at(lane);
+    const TaserColumnsAt<T, DP> columns_at(lane);
     float top = -INFINITY, sum = 0.f;
     taser_f16 o[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    const float scale2 = a.scale * kLog2e;
+    const float scale2 = a.scale * kLog2e, slack = kSlack / (BIAS ? kLog2e : scale2);
 
     auto compute = [&](const char* k, const char* v, const int64_t* pos, const int64_t* range, uint64_t keep) {
         taser_f16 s[NK];
@@ -106,7 +114,7 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[n][r] = 0.f;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) taser_mma(s[n], taser_rows_operand<T, DP>(k, 32 * n, c, lane), q[c]);
+            for (int c = 0; c < NC; ++c) taser_mma(s[n], rows_at.operand(k, 32 * n, c), q[c]);
         }
         if constexpr (BIAS) {
             if (keep) {
@@ -131,7 +139,8 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
         if (keep != (KT == 64 ? ~0ull : 0xffffffffull)) {
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
-                const uint32_t bits = (uint32_t)(keep >> (32 * n)) >> (4 * half);
+                uint32_t bits = (uint32_t)(keep >> (32 * n)) >> (4 * half);
+                asm volatile("" : "+v"(bits));   // keeps this a branch: most tiles are whole
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (!((bits >> (8 * (r >> 2) + (r & 3))) & 1)) s[n][r] = -INFINITY;
@@ -142,8 +151,8 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
         for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) now = fmaxf(now, s[n][r]);
-        now = fmaxf(now, taser_other_half(now));
-        if (__any(now > top)) {
+        now = taser_halves_max(now);
+        if (__any(now > top + slack)) {
             now = fmaxf(now, top);
             const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - now) * (BIAS ? kLog2e : scale2));
             top = now;
@@ -170,7 +179,7 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
                 // the weights are rounded to the type of the states that they multiply; their sum is of the unrounded ones
                 const taser_frag<T> p = taser_operand<T>(s[n], h);
 #pragma unroll
-                for (int d = 0; d < ND; ++d) taser_mma(o[d], taser_columns_operand<T, DP>(v, 32 * n + 16 * h, d, lane), p);
+                for (int d = 0; d < ND; ++d) taser_mma(o[d], columns_at.operand(v, 32 * n + 16 * h, d), p);
             }
     };
 
@@ -202,7 +211,7 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
         compute(k1[slot], v1[slot], pos1[slot], range1[slot], keep1);
     }
 
-    sum += taser_other_half(sum);
+    sum = taser_halves_sum(sum);
     if (!BIAS) top *= a.scale;
     if constexpr (!SHARED) {   // the waves' shares are joined
         constexpr int W = S::kWaves;
@@ -400,6 +409,8 @@ int taser_attention_args(const taser_attention* p, const char* what, TaserAttent
     const int size = p->type == TASER_F32 ? 4 : 2, whole = 16 / size;
     bool direct = a->dim % whole == 0 && ((uintptr_t)p->k | (uintptr_t)p->v) % 16 == 0;
     for (int i = 0; i < 3; ++i) direct = direct && p->k_strides[i] % whole == 0 && p->v_strides[i] % whole == 0;
+    // a tile of 64 states within the reach of its descriptor
+    direct = direct && p->k_strides[1] >= 0 && p->v_strides[1] >= 0 && p->k_strides[1] < kTaserTileBytes / 64 / size && p->v_strides[1] < kTaserTileBytes / 64 / size;
     a->direct = direct;
     return TASER_OK;
 }

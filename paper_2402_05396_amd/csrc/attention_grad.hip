@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
     __shared__ __attribute__((aligned(1024))) char k0[BYTES], v0[BYTES], k1[BYTES], v1[BYTES];
     __shared__ int64_t pos0[BIAS ? KT : 1], pos1[BIAS ? KT : 1], range0[2], range1[2];
     extern __shared__ float table[];   // [group][buckets], then [128 rows][buckets]: sums of dx
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t item = taser_stretch_of_work(blockIdx.x, work);
     if (item < 0) return;
     const int row_tile = (int)(item % a.row_tiles), split = (int)(item / a.row_tiles % a.splits);
@@ -98,10 +98,14 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
         if (a.mask) keep &= (uint32_t)__ballot(lane < n && a.mask[b * a.mask_batch + at + (lane < n ? lane : 0)]);
         return keep;
     };
+    TaserTileLoader<T, DP, KT, 256> load_k(threadIdx.x, a.dim, a.direct), load_v(threadIdx.x, a.dim, a.direct);
+    load_k.set([&](int r) { return r * a.k_token; });
+    load_v.set([&](int r) { return r * a.v_token; });
     auto fetch = [&](char* k, char* v, int64_t* pos, int64_t* range, int tile, uint32_t keep) {
         const int64_t at = (int64_t)tile * KT;
-        taser_load_tile<T, DP, KT, 256>(k, [&](int r) { return k_from + (at + r) * a.k_token; }, keep, a.dim, a.direct, threadIdx.x);
-        taser_load_tile<T, DP, KT, 256>(v, [&](int r) { return v_from + (at + r) * a.v_token; }, keep, a.dim, a.direct, threadIdx.x);
+        const int n = length - tile * KT < KT ? length - tile * KT : KT, size = (int)sizeof(T);
+        load_k.load(k, k_from + at * a.k_token, taser_span(n, a.k_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.k_token; });
+        load_v.load(v, v_from + at * a.v_token, taser_span(n, a.v_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.v_token; });
         if constexpr (BIAS) {
             if (wave == 0) {
                 const bool there = lane < KT && (keep >> lane) & 1;
@@ -116,6 +120,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
         }
     };
 
+    const TaserRowsAt<T, DP> rows_at(lane);
+    const TaserColumnsAt<T, DP> columns_at(lane);
     taser_f16 acc[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -130,8 +136,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
         for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            taser_mma(s, taser_rows_operand<T, DP>(k, 0, c, lane), q[c]);
-            taser_mma(dp, taser_rows_operand<T, DP>(v, 0, c, lane), dy[c]);
+            taser_mma(s, rows_at.operand(k, 0, c), q[c]);
+            taser_mma(dp, rows_at.operand(v, 0, c), dy[c]);
         }
         const uint32_t bits = keep >> (4 * half);
         int bucket[16], low = 0, high = 0;
@@ -159,7 +165,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
                 float x = 0.f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x += low == high || bucket[r] == u ? s[r] : 0.f;
-                x += taser_other_half(x);
+                x = taser_halves_sum(x);
                 if (half == 0) my_sums[u] += x;
             }
         }
@@ -167,7 +173,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
         for (int h = 0; h < 2; ++h) {
             const taser_frag<T> x = taser_operand<T>(s, h);
 #pragma unroll
-            for (int d = 0; d < ND; ++d) taser_mma(acc[d], taser_columns_operand<T, DP>(k, 16 * h, d, lane), x);
+            for (int d = 0; d < ND; ++d) taser_mma(acc[d], columns_at.operand(k, 16 * h, d), x);
         }
     };
 
@@ -240,7 +246,7 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
     __shared__ int64_t pos0[BIAS ? RT : 1], pos1[BIAS ? RT : 1], range0[2], range1[2];
     __shared__ int at0[BIAS ? RT : 1], at1[BIAS ? RT : 1];    // a row's place in the table
     extern __shared__ float table[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t item = taser_stretch_of_work(blockIdx.x, work);
     if (item < 0) return;
     const int state_tile = (int)(item % a.row_tiles), split = (int)(item / a.row_tiles % a.splits);
@@ -274,18 +280,28 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
         __syncthreads();
     }
     const bool any = __any(real);
-    const T* const q_from = (const T*)a.q + b * a.q_batch;
+    const T* const q_from = (const T*)a.q + b * a.q_batch + (int64_t)hk * a.group * a.q_head;
+    const T* const y_from = dout + ((int64_t)b * a.queries * a.heads + hk * a.group) * a.dim;
+    const int64_t y_token = (int64_t)a.heads * a.dim;
+    // Where the heads of a query end with a tile, rows have the same places in every tile.
+    const bool even = RT % a.group == 0;
+    TaserTileLoader<T, DP, RT, 256> load_q(threadIdx.x, a.dim, a.direct), load_y(threadIdx.x, a.dim, a.direct);
     auto fetch = [&](char* q, char* y, taser_f4 (*rows_info)[RT / 4], int64_t* pos, int64_t* range, int* in_table, int tile) {
-        const int at = tile * RT, n = a.rows - at;
+        const int at = tile * RT, n = a.rows - at < RT ? a.rows - at : RT, query0 = at / a.group;
         const uint32_t keep = n >= 32 ? ~0u : (1u << n) - 1;
-        taser_load_tile<T, DP, RT, 256>(q, [&](int r) {
-            const int row = at + r < a.rows ? at + r : 0, query = row / a.group;
-            return q_from + query * a.q_token + (int64_t)(hk * a.group + row - query * a.group) * a.q_head;
-        }, keep, a.dim, a.direct, threadIdx.x);
-        taser_load_tile<T, DP, RT, 256>(y, [&](int r) {
-            const int row = at + r < a.rows ? at + r : 0, query = row / a.group;
-            return dout + (((int64_t)b * a.queries + query) * a.heads + hk * a.group + row - query * a.group) * a.dim;
-        }, keep, a.dim, a.direct, threadIdx.x);
+        auto row_at = [&](int64_t token, int64_t head) {
+            return [=](int r) -> int64_t {   // past the last row: the last one's place, outside `keep`
+                const int row = at + (r < n ? r : n - 1), query = row / a.group;
+                return (query - query0) * token + (row - query * a.group) * head;
+            };
+        };
+        const auto q_at = row_at(a.q_token, a.q_head), y_at = row_at(y_token, a.dim);
+        if (!even || tile == first || n < RT) {
+            load_q.set(q_at);
+            load_y.set(y_at);
+        }
+        load_q.load(q, q_from + query0 * a.q_token, kTaserTileBytes, keep, n < RT, q_at);
+        load_y.load(y, y_from + query0 * y_token, kTaserTileBytes, keep, n < RT, y_at);
         if (threadIdx.x < 64) {
             const bool there = lane < n && lane < RT;
             const int row = there ? at + lane : 0, query = row / a.group, g = row - query * a.group;
@@ -311,6 +327,8 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
 
     // Weights are at most 1: in half precision they are 2^14 times as large where dv's product takes them.
     constexpr float lift = std::is_same_v<T, _Float16> ? 16384.f : 1.f;
+    const TaserRowsAt<T, DP> rows_at(lane);
+    const TaserColumnsAt<T, DP> columns_at(lane);
     taser_f16 sum_k[ND], sum_v[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -325,8 +343,8 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
         for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            taser_mma(s, taser_rows_operand<T, DP>(q, 0, c, lane), k[c]);
-            taser_mma(dp, taser_rows_operand<T, DP>(y, 0, c, lane), v[c]);
+            taser_mma(s, rows_at.operand(q, 0, c), k[c]);
+            taser_mma(dp, rows_at.operand(y, 0, c), v[c]);
         }
         if constexpr (BIAS) {
             const int low = taser_uniform_bucket(bound, taser_apart(range[0], key_high)), high = taser_uniform_bucket(bound, taser_apart(range[1], key_low));
@@ -367,8 +385,8 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
             const taser_frag<T> p = taser_operand<T>(s, h, lift), x = taser_operand<T>(dp, h);
 #pragma unroll
             for (int d = 0; d < ND; ++d) {
-                taser_mma(sum_v[d], taser_columns_operand<T, DP>(y, 16 * h, d, lane), p);
-                taser_mma(sum_k[d], taser_columns_operand<T, DP>(q, 16 * h, d, lane), x);
+                taser_mma(sum_v[d], columns_at.operand(y, 16 * h, d), p);
+                taser_mma(sum_k[d], columns_at.operand(q, 16 * h, d), x);
             }
         }
     };
@@ -515,6 +533,9 @@ int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stat
         // rows are loaded here: q and dout have to be aligned for loads past the registers
         const int whole = 16 / (int)sizeof(T);
         a.direct = a.dim % whole == 0 && ((uintptr_t)a.q | (uintptr_t)dout) % 16 == 0 && a.q_batch % whole == 0 && a.q_token % whole == 0 && a.q_head % whole == 0;
+        // the rows of a tile within the reach of its descriptor
+        const int64_t reach = kTaserTileBytes / 64 / (int)sizeof(T);
+        a.direct = a.direct && a.q_token >= 0 && a.q_head >= 0 && a.q_token < reach && a.q_head < reach / a.group && (int64_t)a.heads * a.dim < reach;
         {
             TaserProfileSpan span(stream, "attention_grad_states");
             if (a.table)
