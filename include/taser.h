@@ -496,7 +496,7 @@ enum taser_type { TASER_F32 = 0, TASER_F16 = 1, TASER_BF16 = 2 };
 
 #define TASER_MAX_HEAD_DIM 128
 #define TASER_MAX_BUCKETS 64
-#define TASER_MAX_GROUP_BUCKETS 4096
+#define TASER_MAX_GROUP_BUCKETS 2048
 #define TASER_ATTENTION_STATS(type, head_dim) (2 + ((type) == TASER_F32 ? 0 : ((head_dim) + 1) / 2))
 
 typedef struct taser_attention {

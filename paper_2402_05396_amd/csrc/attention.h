@@ -120,12 +120,12 @@ __device__ inline float taser_halves_max(float x) {
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------
 // A tile holds ROWS rows of DP elements (the head size rounded up, the rest zeros) as 16-byte pieces. Piece c of row r lies
-// at place c ^ taser_swizzle(r): reads of one piece of 16 consecutive rows, and of two neighboring pieces of 4 consecutive
-// rows, then touch every bank of LDS once.
+// at place c ^ taser_swizzle(r). 256 bytes of LDS are read at a time: one piece of 16 neighboring rows (or two neighboring pieces of 8),
+// or four neighboring pieces of 4 rows, in both cases from every bank once.
 template <int PIECES> __device__ inline int taser_swizzle(int row) {
     static_assert(PIECES >= 8, "");
-    const int x = PIECES == 8 ? (row >> 1) & 7 : row & 15;
-    return PIECES == 8 ? ((x & 3) << 1) | (x >> 2) : ((x & 7) << 1) | (x >> 3);
+    if (PIECES == 8) return ((row >> 1) & 1) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1);
+    return (row & 3) << 2 | ((row >> 2) & 1) << 1 | ((row >> 3) & 1);
 }
 
 // Loads tiles of ROWS rows by THREADS threads. Past the registers (`direct`) through a buffer descriptor of the tile: a lane's places
@@ -176,6 +176,11 @@ __device__ inline int taser_span(int n, int64_t stride, int row) { return n > 0 
 // Waits for this wave's loads past the registers (and all other loads).
 __device__ inline void taser_loads_arrived() {
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+}
+
+// A barrier for what was written to LDS by instructions: loads past the registers may still be on their way.
+__device__ inline void taser_lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // Where a lane's part of a tile lies, once for all tiles: 32 rows further on, everything is 32 rows of bytes further on.
@@ -244,49 +249,132 @@ template <typename T, int DP> struct TaserColumnsAt {
     }
 };
 
+// The order of a stretch of products that stands alone between branches: AHEAD reads of LDS first, then READS_EACH under each product
+// while there are any: enough on the way for the latency of LDS, without a register for all of them.
+template <int AHEAD, int READS_EACH, int PRODUCTS> __device__ inline void taser_order() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < PRODUCTS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (AHEAD + i * READS_EACH < PRODUCTS * READS_EACH) __builtin_amdgcn_sched_group_barrier(0x100, READS_EACH, 0);
+    }
+}
+
 // ---- the bias by distance ----------------------------------------------------------------------------------------------
 // Lane l keeps bound l; there are at most 63. A distance common to the wave has as many bounds at most as it as lanes say so.
 __device__ inline int64_t taser_lane_bound(const TaserAttentionArgs& a, int lane) {
     return lane < a.buckets - 1 ? a.bounds[lane] : INT64_MAX;
 }
-__device__ inline int taser_uniform_bucket(int64_t bound, int64_t distance) {
-    return __popcll(__ballot(bound <= distance));
+__device__ inline int taser_uniform_bucket(int64_t bound, int64_t distance, int buckets) {
+    const int n = __popcll(__ballot(bound <= distance));
+    return n < buckets ? n : buckets - 1;
 }
+constexpr float kTaserFoldable = 8192.f;   // the largest bias that may be added to a row's constant rather than to its scores
 __device__ inline int64_t taser_apart(int64_t a, int64_t b) { return (int64_t)((uint64_t)a - (uint64_t)b); }
 __device__ inline int64_t taser_lane_value(int64_t x, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane) |
                      (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)x >> 32), lane) << 32);
 }
-// Buckets of a lane's distances to the 16 states of a result's registers (state 8 g + i of `pos` in register 4 g + i), known to
-// lie in low .. high.
-__device__ inline void taser_buckets(int (&bucket)[16], int64_t bound, int low, int high, int64_t from, const int64_t* pos) {
-    int64_t apart[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        apart[r] = taser_apart(from, pos[8 * (r >> 2) + (r & 3)]);
-        bucket[r] = low;
+// Buckets of single distances. Where all bounds lie within a thousand of one another, as those of token distances do, a table in LDS
+// has the bucket of each distance between them, and a distance costs a read. Others are compared with the bounds in question.
+constexpr int kTaserNear = 1024;
+struct TaserNear {
+    int64_t base;   // the table's first entry: just below the first bound
+    int last;       // its last; -1: there is no table
+    __device__ TaserNear() : base(0), last(-1) {}
+    // By all threads of a block, before a barrier.
+    __device__ TaserNear(const TaserAttentionArgs& a, uint8_t* near) : base(0), last(-1) {
+        if (a.buckets < 2) return;
+        base = a.bounds[0] - 1;
+        const uint64_t span = (uint64_t)a.bounds[a.buckets - 2] - (uint64_t)base;
+        if (span >= (uint64_t)kTaserNear) return;
+        last = (int)span;
+        for (int e = threadIdx.x; e <= last; e += blockDim.x) {
+            int n = 0;
+            for (int u = 0; u < a.buckets - 1; ++u) n += a.bounds[u] - base <= e;
+            near[e] = (uint8_t)n;
+        }
     }
-    for (int i = low; i < high; ++i) {
-        const int64_t x = taser_lane_value(bound, i);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) bucket[r] += x <= apart[r];
+};
+struct TaserBuckets {
+    const uint8_t* near;
+    int64_t bound;
+    int low, high, last;
+    uint32_t base;
+    bool read;
+    // Distances of the tile lie in least .. most, their buckets in low .. high.
+    __device__ TaserBuckets(const TaserNear& n, const uint8_t* near_, int64_t bound_, int low_, int high_, int64_t least, int64_t most)
+        : near(near_), bound(bound_), low(low_), high(high_), last(n.last), base((uint32_t)(uint64_t)n.base) {
+        const int64_t reach = 1 << 30;
+        read = last >= 0 && least > n.base - reach && most < n.base + reach;
     }
+    // from - to[i], or to[i] - from. (Masked states may lie anywhere: theirs is any bucket of the table.)
+    template <bool BACK> __device__ void find(int (&bucket)[4], int64_t from, const int64_t* to) const {
+        if (read) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = (uint32_t)(uint64_t)from, y = (uint32_t)(uint64_t)to[i];
+                int at = (int)((BACK ? y - x : x - y) - base);
+                at = at < 0 ? 0 : (at > last ? last : at);
+                bucket[i] = near[at];
+            }
+        } else {
+            int64_t apart[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                apart[i] = BACK ? taser_apart(to[i], from) : taser_apart(from, to[i]);
+                bucket[i] = low;
+            }
+            for (int u = low; u < high; ++u) {
+                const int64_t x = taser_lane_value(bound, u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bucket[i] += x <= apart[i];
+            }
+        }
+    }
+};
+// Buckets whose biases of all `group` heads of a table [buckets][group] may be folded, as bits.
+__device__ inline uint64_t taser_foldable(const float* table, int buckets, int group, int lane) {
+    bool all = lane < buckets;
+    if (all)
+        for (int g = 0; g < group; ++g) all = all && fabsf(table[lane * group + g]) <= kTaserFoldable;
+    return __ballot(all);
 }
-__device__ inline int64_t taser_wave_min(int64_t x) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int64_t y = __shfl_xor(x, m);
-        x = y < x ? y : x;
-    }
-    return x;
+// The smaller of x and what the lane takes from another one.
+__device__ inline int64_t taser_min64(int64_t x, int64_t y) { return y < x ? y : x; }
+template <int CONTROL> __device__ inline int64_t taser_min_dpp(int64_t x) {
+    const int low = (int)(uint32_t)(uint64_t)x, high = (int)((uint64_t)x >> 32);
+    const uint32_t a = (uint32_t)__builtin_amdgcn_update_dpp(0, low, CONTROL, 0xf, 0xf, false), b = (uint32_t)__builtin_amdgcn_update_dpp(0, high, CONTROL, 0xf, 0xf, false);
+    return taser_min64(x, (int64_t)((uint64_t)b << 32 | a));
 }
-__device__ inline int64_t taser_wave_max(int64_t x) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const int64_t y = __shfl_xor(x, m);
-        x = y > x ? y : x;
-    }
-    return x;
+// Smallest of each half wave's values, in all its lanes.
+__device__ inline int64_t taser_half_min(int64_t x) {
+    x = taser_min_dpp<0x121>(x);   // rotations within 16 lanes
+    x = taser_min_dpp<0x122>(x);
+    x = taser_min_dpp<0x124>(x);
+    x = taser_min_dpp<0x128>(x);
+    const uint32_t low = (uint32_t)(uint64_t)x, high = (uint32_t)((uint64_t)x >> 32);
+    const auto l = __builtin_amdgcn_permlane16_swap(low, low, false, false), h = __builtin_amdgcn_permlane16_swap(high, high, false, false);
+    const uint32_t l0 = l[0], l1 = l[1], h0 = h[0], h1 = h[1];
+    return taser_min64((int64_t)((uint64_t)h0 << 32 | l0), (int64_t)((uint64_t)h1 << 32 | l1));
+}
+// {smallest of all lanes' `low`, smallest of all lanes' `high`}, the one in the lower half's lanes and the other in the upper's.
+__device__ inline int64_t taser_two_mins(int64_t low, int64_t high) {
+    const auto l = __builtin_amdgcn_permlane32_swap((uint32_t)(uint64_t)low, (uint32_t)(uint64_t)high, false, false);
+    const auto h = __builtin_amdgcn_permlane32_swap((uint32_t)((uint64_t)low >> 32), (uint32_t)((uint64_t)high >> 32), false, false);
+    const uint32_t l0 = l[0], l1 = l[1], h0 = h[0], h1 = h[1];
+    return taser_half_min(taser_min64((int64_t)((uint64_t)h0 << 32 | l0), (int64_t)((uint64_t)h1 << 32 | l1)));
+}
+// Range of the positions of the lanes that have one: ends[0] the smallest, ends[1] the largest (INT64_MAX, -INT64_MAX: none).
+__device__ inline void taser_store_range(int64_t pos, bool there, int lane, int64_t* ends) {
+    const int64_t x = taser_two_mins(there ? pos : INT64_MAX, there ? -pos : INT64_MAX);
+    if (lane == 0) ends[0] = x;
+    if (lane == 32) ends[1] = -x;
+}
+__device__ inline void taser_range(int64_t pos, bool there, int64_t* low, int64_t* high) {
+    const int64_t x = taser_two_mins(there ? pos : INT64_MAX, there ? -pos : INT64_MAX);
+    *low = taser_lane_value(x, 0);
+    *high = -taser_lane_value(x, 32);
 }
 
 // Workgroups are handed out to the eight L2 partitions in turn: each partition takes a stretch of consecutive work, so that

@@ -25,9 +25,10 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
     using S = Shape<T, DP, SHARED>;
     constexpr int KT = S::kStates, NK = KT / 32, ND = DP / 32, NC = DP / 16;
     __shared__ __attribute__((aligned(1024))) char k0[S::kTiles][S::kTileBytes], v0[S::kTiles][S::kTileBytes], k1[S::kTiles][S::kTileBytes], v1[S::kTiles][S::kTileBytes];
-    __shared__ int64_t pos0[S::kTiles][BIAS ? KT : 1], pos1[S::kTiles][BIAS ? KT : 1], range0[S::kTiles][2], range1[S::kTiles][2];
+    __shared__ int64_t pos0[S::kTiles][BIAS ? KT : 1], pos1[S::kTiles][BIAS ? KT : 1], ranges[S::kTiles][4][2];
     __shared__ float joined[2][S::kWaves][32];
-    extern __shared__ float table[];   // [group][buckets]
+    __shared__ uint8_t near[BIAS ? kTaserNear : 1];
+    __shared__ float table[BIAS ? TASER_MAX_GROUP_BUCKETS : 1];   // [buckets][group]; of its own, so that no read of it waits for a tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t item = taser_stretch_of_work(blockIdx.x, work);
     if (item < 0) return;
@@ -48,25 +49,40 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
         for (int c = 0; c < NC; ++c) q[c] = taser_load_frag<T>(from + 16 * c + 8 * half, real ? a.dim - 16 * c - 8 * half : 0);
     }
     int64_t query_pos = 0, bound = 0, query_low = 0, query_high = 0;
+    uint64_t foldable = 0;
+    TaserNear map;
     if constexpr (BIAS) {
         const T* from = (const T*)a.table + (int64_t)hk * a.group * a.buckets;
-        for (int i = threadIdx.x; i < a.group * a.buckets; i += blockDim.x) table[i] = (float)from[i];
-        query_pos = a.query_pos[b * a.query_pos_batch + query];
+        for (int i = threadIdx.x; i < a.group * a.buckets; i += blockDim.x) table[i] = (float)from[i % a.group * a.buckets + i / a.group];
+        query_pos = a.query_pos[b * a.query_pos_batch + (row < a.rows ? row : a.rows - 1) / a.group];
         bound = taser_lane_bound(a, lane);
-        query_low = taser_wave_min(query_pos);
-        query_high = taser_wave_max(query_pos);
+        taser_range(query_pos, true, &query_low, &query_high);
+        map = TaserNear(a, near);
         __syncthreads();
+        foldable = taser_foldable(table, a.buckets, a.group, lane);
     }
-    const float* my_table = table + g * a.buckets;
+    const float* my_table = table + g;   // by bucket, `group` apart
     const T* const k_from = (const T*)a.k + b * a.k_batch + hk * a.k_head;
     const T* const v_from = (const T*)a.v + b * a.v_batch + hk * a.v_head;
 
+    // A lane's mask byte of a tile's states is on its way a tile ahead, their positions are two tiles ahead: which buckets a tile can
+    // need is known before it begins.
+    uint8_t ahead_mask = 1;
+    int64_t next_pos = 0, after_pos = 0;
+    auto state_pos = [&](int tile) -> int64_t {
+        const int64_t at = (int64_t)tile * KT + lane;
+        return BIAS && (!SHARED || wave == 0) && lane < KT && at < length ? a.key_pos[b * a.key_pos_batch + at] : 0;
+    };
+    auto look = [&](int tile) {
+        const int64_t at = (int64_t)tile * KT + lane;
+        if (a.mask) ahead_mask = lane < KT && at < length ? a.mask[b * a.mask_batch + at] : 0;
+    };
     // states [KT * tile, ..) that take part
     auto kept = [&](int tile) -> uint64_t {
-        const int at = tile * KT, n = length - at;
+        const int n = length - tile * KT;
         uint64_t keep = n >= 64 ? ~0ull : (n <= 0 ? 0 : (1ull << n) - 1);
         if (KT == 32) keep &= 0xffffffffull;
-        if (a.mask) keep &= __ballot(lane < n && a.mask[b * a.mask_batch + at + (lane < n ? lane : 0)]);
+        if (a.mask) keep &= __ballot(ahead_mask != 0);
         return keep;
     };
     constexpr int THREADS = SHARED ? 64 * S::kWaves : 64;
@@ -74,29 +90,19 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
     TaserTileLoader<T, DP, KT, THREADS> load_k(thread, a.dim, a.direct), load_v(thread, a.dim, a.direct);
     load_k.set([&](int r) { return r * a.k_token; });
     load_v.set([&](int r) { return r * a.v_token; });
-    auto fetch = [&](char* k, char* v, int64_t* pos, int64_t* range, int tile, uint64_t keep) {
+    auto fetch = [&](char* k, char* v, int64_t* pos, int tile, uint64_t keep) {
         const int64_t at = (int64_t)tile * KT;
         const int n = length - tile * KT < KT ? length - tile * KT : KT, size = (int)sizeof(T);
         load_k.load(k, k_from + at * a.k_token, taser_span(n, a.k_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.k_token; });
         load_v.load(v, v_from + at * a.v_token, taser_span(n, a.v_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.v_token; });
-        if constexpr (BIAS) {
-            if (!SHARED || wave == 0) {
-                const bool there = lane < KT && (keep >> lane) & 1;
-                const int64_t p = there ? a.key_pos[b * a.key_pos_batch + at + lane] : 0;
-                if (lane < KT) pos[lane] = p;
-                const int64_t low = taser_wave_min(there ? p : INT64_MAX), high = taser_wave_max(there ? p : INT64_MIN);
-                if (lane == 0) {
-                    range[0] = low;
-                    range[1] = high;
-                }
-            }
-        }
+        if constexpr (BIAS)
+            if ((!SHARED || wave == 0) && lane < KT) pos[lane] = next_pos;
     };
 
     // Half precision ends at 6e-8 below 1: there the weights, and all sums of them, are 2^10 times as large until the end.
     constexpr float lift = std::is_same_v<T, _Float16> ? 10.f : 0.f, drop = std::is_same_v<T, _Float16> ? 1.f / 1024.f : 1.f;
-    // The reference of a row follows its largest score only when that is 2^kSlack weights away: most tiles leave the sums as they are.
-    constexpr float kSlack = 5.f;
+    // The reference of a row follows its largest score only when that is e^kSlack weights away: most tiles leave the sums as they are.
+    constexpr float kSlack = 3.5f;
     const TaserRowsAt<T, DP> rows_at(lane);
     const TaserColumnsAt<T, DP> columns_at(lane);
     float top = -INFINITY, sum = 0.f;
@@ -105,9 +111,26 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
-    const float scale2 = a.scale * kLog2e, slack = kSlack / (BIAS ? kLog2e : scale2);
+    const float scale2 = a.scale * kLog2e;
 
-    auto compute = [&](const char* k, const char* v, const int64_t* pos, const int64_t* range, uint64_t keep) {
+    // Scores stay products while one bias holds for the whole tile: it goes into the row's constant. Elsewhere, and where a bias is so
+    // large that the sum's rounding decides (the lowest value swallows all products), they become sums.
+    float tile_bias = 0.f;
+    bool tile_sums = false;
+    int tile_low = 0, tile_high = 0;
+    auto prepare = [&](int turn) {
+        const int64_t* range = ranges[slot][turn & 3];
+        tile_low = taser_uniform_bucket(bound, taser_apart(query_low, range[1]), a.buckets);
+        tile_high = taser_uniform_bucket(bound, taser_apart(query_high, range[0]), a.buckets);
+        tile_sums = tile_low != tile_high || !((foldable >> tile_low) & 1);
+        tile_bias = tile_sums ? 0.f : my_table[tile_low * a.group];
+    };
+
+    auto compute = [&](const char* k, const char* v, const int64_t* pos, int turn, uint64_t keep) {
+        float bias = tile_bias;
+        const bool sums = tile_sums;
+        const int low = tile_low, high = tile_high;
+        if constexpr (BIAS) prepare(turn + 1);
         taser_f16 s[NK];
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
@@ -117,23 +140,18 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
             for (int c = 0; c < NC; ++c) taser_mma(s[n], rows_at.operand(k, 32 * n, c), q[c]);
         }
         if constexpr (BIAS) {
-            if (keep) {
-                const int low = taser_uniform_bucket(bound, taser_apart(query_low, range[1])), high = taser_uniform_bucket(bound, taser_apart(query_high, range[0]));
-                if (low == high) {
-                    const float bias = my_table[low];
+            if (sums) {
+                const int64_t* range = ranges[slot][turn & 3];
+                const TaserBuckets buckets(map, near, bound, low, high, taser_apart(query_low, range[1]), taser_apart(query_high, range[0]));
 #pragma unroll
-                    for (int n = 0; n < NK; ++n)
+                for (int n = 0; n < NK; ++n)
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) s[n][r] = fmaf(s[n][r], a.scale, bias);
-                } else {
+                    for (int j = 0; j < 4; ++j) {
+                        int bucket[4];
+                        buckets.find<false>(bucket, query_pos, pos + 32 * n + 8 * j + 4 * half);
 #pragma unroll
-                    for (int n = 0; n < NK; ++n) {
-                        int bucket[16];
-                        taser_buckets(bucket, bound, low, high, query_pos, pos + 32 * n + 4 * half);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) s[n][r] = fmaf(s[n][r], a.scale, my_table[bucket[r]]);
+                        for (int i = 0; i < 4; ++i) s[n][4 * j + i] = fmaf(s[n][4 * j + i], a.scale, my_table[bucket[i] * a.group]);
                     }
-                }
             }
         }
         if (keep != (KT == 64 ? ~0ull : 0xffffffffull)) {
@@ -152,9 +170,10 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
 #pragma unroll
             for (int r = 0; r < 16; ++r) now = fmaxf(now, s[n][r]);
         now = taser_halves_max(now);
-        if (__any(now > top + slack)) {
+        if (!sums) now = fmaf(now, a.scale, bias);
+        if (__any(now > top + kSlack)) {
             now = fmaxf(now, top);
-            const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - now) * (BIAS ? kLog2e : scale2));
+            const float shrink = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((top - now) * kLog2e);
             top = now;
             sum *= shrink;
 #pragma unroll
@@ -162,13 +181,22 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[d][r] *= shrink;
         }
-        const float base = top == -INFINITY ? 0.f : top, base2 = base * scale2 - lift;
+        const float base = top == -INFINITY ? 0.f : top;
+        float by = scale2, plus = fmaf(bias - base, kLog2e, lift);
+        if (BIAS && sums) {
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[n][r] -= base;
+            by = kLog2e;
+            plus = lift;
+        }
         float part = 0.f;
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[n][r] = __builtin_amdgcn_exp2f(BIAS ? fmaf(s[n][r] - base, kLog2e, lift) : fmaf(s[n][r], scale2, -base2));
+                s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], by, plus));
                 part += s[n][r];
             }
         sum += part;
@@ -191,28 +219,41 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
         if (SHARED) __syncthreads();
         else __builtin_amdgcn_wave_barrier();
     };
-    if (tile < last) {
-        keep0 = kept(tile);
-        fetch(k0[slot], v0[slot], pos0[slot], range0[slot], tile, keep0);
-    }
-    for (; tile < last; tile += 2 * step) {
-        arrived();
-        if (tile + step < last) {
-            keep1 = kept(tile + step);
-            fetch(k1[slot], v1[slot], pos1[slot], range1[slot], tile + step, keep1);
+    auto store_range = [&](int64_t pos, int at, int turn) {
+        if (!SHARED || wave == 0) taser_store_range(pos, lane < KT && (int64_t)at * KT + lane < length, lane, ranges[slot][turn & 3]);
+    };
+    auto open = [&](char* k, char* v, int64_t* pos, int at, int turn, uint64_t& keep) {
+        if (at >= last) return;
+        keep = kept(at);
+        fetch(k, v, pos, at, keep);
+        look(at + step);
+        if constexpr (BIAS) {
+            store_range(after_pos, at + step, turn + 1);
+            next_pos = after_pos;
+            after_pos = state_pos(at + 2 * step);
         }
-        compute(k0[slot], v0[slot], pos0[slot], range0[slot], keep0);
+    };
+    look(tile);
+    int turn = 0;
+    if constexpr (BIAS) {
+        next_pos = state_pos(tile);
+        after_pos = state_pos(tile + step);
+        store_range(next_pos, tile, 0);
+    }
+    open(k0[slot], v0[slot], pos0[slot], tile, 0, keep0);
+    for (; tile < last; tile += 2 * step, turn += 2) {
+        arrived();
+        if constexpr (BIAS)
+            if (turn == 0) prepare(0);
+        open(k1[slot], v1[slot], pos1[slot], tile + step, turn + 1, keep1);
+        compute(k0[slot], v0[slot], pos0[slot], turn, keep0);
         if (tile + step >= last) break;
         arrived();
-        if (tile + 2 * step < last) {
-            keep0 = kept(tile + 2 * step);
-            fetch(k0[slot], v0[slot], pos0[slot], range0[slot], tile + 2 * step, keep0);
-        }
-        compute(k1[slot], v1[slot], pos1[slot], range1[slot], keep1);
+        open(k0[slot], v0[slot], pos0[slot], tile + 2 * step, turn + 2, keep0);
+        compute(k1[slot], v1[slot], pos1[slot], turn + 1, keep1);
     }
 
     sum = taser_halves_sum(sum);
-    if (!BIAS) top *= a.scale;
     if constexpr (!SHARED) {   // the waves' shares are joined
         constexpr int W = S::kWaves;
         joined[0][wave][lane & 31] = top;
@@ -334,7 +375,7 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
     {
         TaserProfileSpan span(stream, "attention");
         if (a.table)
-            attention_kernel<T, DP, SHARED, true><<<grid, block, sizeof(float) * a.group * a.buckets, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
+            attention_kernel<T, DP, SHARED, true><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
         else
             attention_kernel<T, DP, SHARED, false><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
         TASER_HIP_TRY(hipGetLastError());

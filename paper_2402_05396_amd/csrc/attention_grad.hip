@@ -13,7 +13,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// What the passes need of a row: {top, 1 / sum, <dout, out>, log2 of the sum of 2^(x log2 e)}; a row without states has weights of 0.
+// What the passes need of a row: {reference of its scores, log2 of its sum, <dout, out>}; a row without states has weights of 0.
 // 16 lanes a row.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_grad_rows_kernel(const T* out, const T* dout, const float* stats, int32_t stat_floats, int64_t rows, int32_t dim, taser_f4* info) {
@@ -36,11 +36,19 @@ __global__ __launch_bounds__(256) void attention_grad_rows_kernel(const T* out, 
     const float top = stats[row * stat_floats], sum = stats[row * stat_floats + 1];
     taser_f4 w;
     w[0] = sum == 0.f ? INFINITY : top;
-    w[1] = sum == 0.f ? 0.f : 1.f / sum;
+    w[1] = sum == 0.f ? 0.f : log2f(sum);
     w[2] = t;
-    w[3] = sum == 0.f ? INFINITY : fmaf(top, kLog2e, log2f(sum));
+    w[3] = 0.f;
     info[row] = w;
 }
+
+// Adds to LDS and goes on: written out, as the compiler would first wait for every load that is on its way to LDS. A lane's adds keep
+// their order; lds_adds_done() comes before another wave reads.
+__device__ inline void lds_add(float* to, float x) {
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)to;
+    asm volatile("ds_add_f32 %0, %1" ::"v"(at), "v"(x) : "memory");
+}
+__device__ inline void lds_adds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // ---- dq, dtable -----------------------------------------------------------------------------------------------------------
 // A wave owns 32 rows, as in the forward pass; four waves share tiles of 32 states.
@@ -49,8 +57,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
                                                                                                float* part_dq, float* part_table, int64_t work) {
     constexpr int KT = 32, ND = DP / 32, NC = DP / 16, BYTES = KT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(1024))) char k0[BYTES], v0[BYTES], k1[BYTES], v1[BYTES];
-    __shared__ int64_t pos0[BIAS ? KT : 1], pos1[BIAS ? KT : 1], range0[2], range1[2];
-    extern __shared__ float table[];   // [group][buckets], then [128 rows][buckets]: sums of dx
+    __shared__ int64_t pos0[BIAS ? KT : 1], pos1[BIAS ? KT : 1], ranges[4][2];
+    __shared__ uint8_t near[BIAS ? kTaserNear : 1];
+    __shared__ float table[BIAS ? TASER_MAX_GROUP_BUCKETS : 1];                             // [buckets][group]
+    __shared__ float table_sums[BIAS ? 4 : 1][BIAS ? TASER_MAX_BUCKETS : 1][32];             // of dx, by a wave's buckets and rows
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t item = taser_stretch_of_work(blockIdx.x, work);
     if (item < 0) return;
@@ -75,49 +85,54 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
             dy[c] = taser_load_frag<T>(dfrom + e, n);
         }
     }
-    taser_f4 mine = {INFINITY, 0.f, 0.f, INFINITY};
+    taser_f4 mine = {INFINITY, 0.f, 0.f, 0.f};
     if (real) mine = info[at_row];
     int64_t query_pos = 0, bound = 0, query_low = 0, query_high = 0;
+    uint64_t foldable = 0;
+    TaserNear map;
     if constexpr (BIAS) {
         const T* from = (const T*)a.table + (int64_t)hk * a.group * a.buckets;
-        for (int i = threadIdx.x; i < (a.group + 128) * a.buckets; i += 256) table[i] = i < a.group * a.buckets ? (float)from[i] : 0.f;
-        query_pos = a.query_pos[b * a.query_pos_batch + query];
+        for (int i = threadIdx.x; i < a.group * a.buckets; i += 256) table[i] = (float)from[i % a.group * a.buckets + i / a.group];
+        for (int i = threadIdx.x; i < 4 * TASER_MAX_BUCKETS * 32; i += 256) (&table_sums[0][0][0])[i] = 0.f;
+        query_pos = a.query_pos[b * a.query_pos_batch + (row < a.rows ? row : a.rows - 1) / a.group];
         bound = taser_lane_bound(a, lane);
-        query_low = taser_wave_min(query_pos);
-        query_high = taser_wave_max(query_pos);
+        taser_range(query_pos, true, &query_low, &query_high);
+        map = TaserNear(a, near);
         __syncthreads();
+        foldable = taser_foldable(table, a.buckets, a.group, lane);
     }
-    const float* my_table = table + g * a.buckets;
-    float* my_sums = table + (a.group + wave * 32 + (lane & 31)) * a.buckets;
+    const float* my_table = table + g;   // by bucket, `group` apart
+    float (*my_sums)[32] = table_sums[wave];
     const T* const k_from = (const T*)a.k + b * a.k_batch + hk * a.k_head;
     const T* const v_from = (const T*)a.v + b * a.v_batch + hk * a.v_head;
 
+    // A lane's mask byte of a tile's states is on its way a tile ahead, their positions are two tiles ahead (as in the forward pass).
+    uint8_t ahead_mask = 1;
+    int64_t next_pos = 0, after_pos = 0;
+    auto state_pos = [&](int tile) -> int64_t {
+        const int64_t at = (int64_t)tile * KT + lane;
+        return BIAS && wave == 0 && lane < KT && at < length ? a.key_pos[b * a.key_pos_batch + at] : 0;
+    };
+    auto look = [&](int tile) {
+        const int64_t at = (int64_t)tile * KT + lane;
+        if (a.mask) ahead_mask = lane < KT && at < length ? a.mask[b * a.mask_batch + at] : 0;
+    };
     auto kept = [&](int tile) -> uint32_t {
-        const int at = tile * KT, n = length - at;
+        const int n = length - tile * KT;
         uint32_t keep = n >= 32 ? ~0u : (1u << n) - 1;
-        if (a.mask) keep &= (uint32_t)__ballot(lane < n && a.mask[b * a.mask_batch + at + (lane < n ? lane : 0)]);
+        if (a.mask) keep &= (uint32_t)__ballot(ahead_mask != 0);
         return keep;
     };
     TaserTileLoader<T, DP, KT, 256> load_k(threadIdx.x, a.dim, a.direct), load_v(threadIdx.x, a.dim, a.direct);
     load_k.set([&](int r) { return r * a.k_token; });
     load_v.set([&](int r) { return r * a.v_token; });
-    auto fetch = [&](char* k, char* v, int64_t* pos, int64_t* range, int tile, uint32_t keep) {
+    auto fetch = [&](char* k, char* v, int64_t* pos, int tile, uint32_t keep) {
         const int64_t at = (int64_t)tile * KT;
         const int n = length - tile * KT < KT ? length - tile * KT : KT, size = (int)sizeof(T);
         load_k.load(k, k_from + at * a.k_token, taser_span(n, a.k_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.k_token; });
         load_v.load(v, v_from + at * a.v_token, taser_span(n, a.v_token * size, a.dim * size), keep, a.mask, [&](int r) { return r * a.v_token; });
-        if constexpr (BIAS) {
-            if (wave == 0) {
-                const bool there = lane < KT && (keep >> lane) & 1;
-                const int64_t p = there ? a.key_pos[b * a.key_pos_batch + at + lane] : 0;
-                if (lane < KT) pos[lane] = p;
-                const int64_t low = taser_wave_min(there ? p : INT64_MAX), high = taser_wave_max(there ? p : INT64_MIN);
-                if (lane == 0) {
-                    range[0] = low;
-                    range[1] = high;
-                }
-            }
-        }
+        if constexpr (BIAS)
+            if (wave == 0 && lane < KT) pos[lane] = next_pos;
     };
 
     const TaserRowsAt<T, DP> rows_at(lane);
@@ -129,8 +144,25 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
         for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
     const float scale2 = a.scale * kLog2e;
 
-    auto compute = [&](const char* k, const char* v, const int64_t* pos, const int64_t* range, uint32_t keep) {
+    // As in the forward pass: one bias for the tile goes into the row's constant, others into the scores.
+    float tile_bias = 0.f;
+    bool tile_sums = false;
+    int tile_low = 0, tile_high = 0;
+    auto prepare = [&](int turn) {
+        const int64_t* range = ranges[turn & 3];
+        tile_low = taser_uniform_bucket(bound, taser_apart(query_low, range[1]), a.buckets);
+        tile_high = taser_uniform_bucket(bound, taser_apart(query_high, range[0]), a.buckets);
+        tile_sums = tile_low != tile_high || !((foldable >> tile_low) & 1);
+        tile_bias = my_table[tile_low * a.group];
+    };
+    auto compute = [&](const char* k, const char* v, const int64_t* pos, int turn, uint32_t keep) {
+        float bias = tile_bias, by = scale2, minus = mine[0];
+        const bool sums = tile_sums;
+        const int low = tile_low, high = tile_high;
+        if constexpr (BIAS) prepare(turn + 1);
         if (!keep) return;
+        float sum_before = 0.f;
+        if constexpr (BIAS) sum_before = my_sums[low][lane & 31];
         taser_f16 s, dp;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
@@ -139,34 +171,55 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
             taser_mma(s, rows_at.operand(k, 0, c), q[c]);
             taser_mma(dp, rows_at.operand(v, 0, c), dy[c]);
         }
-        const uint32_t bits = keep >> (4 * half);
-        int bucket[16], low = 0, high = 0;
+        if constexpr (sizeof(T) == 2) taser_order<6, 1, 2 * NC>();
         if constexpr (BIAS) {
-            low = taser_uniform_bucket(bound, taser_apart(query_low, range[1]));
-            high = taser_uniform_bucket(bound, taser_apart(query_high, range[0]));
-            if (low == high) {
-                const float bias = my_table[low];
+            if (sums) {
+                const int64_t* range = ranges[turn & 3];
+                const TaserBuckets of(map, near, bound, low, high, taser_apart(query_low, range[1]), taser_apart(query_high, range[0]));
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale, bias);
-            } else {
-                taser_buckets(bucket, bound, low, high, query_pos, pos + 4 * half);
+                for (int j = 0; j < 4; ++j) {
+                    int bucket[4];
+                    of.find<false>(bucket, query_pos, pos + 8 * j + 4 * half);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale, my_table[bucket[r]]);
+                    for (int i = 0; i < 4; ++i) s[4 * j + i] = fmaf(s[4 * j + i], a.scale, my_table[bucket[i] * a.group]) - mine[0];
+                }
+                bias = minus = 0.f;
+                by = kLog2e;
             }
+        }
+        const float plus = fmaf(bias - minus, kLog2e, -mine[1]);
+        if (keep != ~0u) {
+            uint32_t bits = keep >> (4 * half);
+            asm volatile("" : "+v"(bits));   // keeps this a branch: most tiles are whole
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (!((bits >> (8 * (r >> 2) + (r & 3))) & 1)) s[r] = -INFINITY;
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            float p = BIAS ? __builtin_amdgcn_exp2f((s[r] - mine[0]) * kLog2e) * mine[1] : __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -mine[3]));
-            if (keep != ~0u && !((bits >> (8 * (r >> 2) + (r & 3))) & 1)) p = 0.f;
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[r], by, plus));
             s[r] = p * (dp[r] - mine[2]);
         }
         if constexpr (BIAS) {
-            for (int u = low; u <= high; ++u) {
+            if (low != high) {   // a row's two lanes add one after the other: the sums have one order
+                const int64_t* range = ranges[turn & 3];
+                const TaserBuckets of(map, near, bound, low, high, taser_apart(query_low, range[1]), taser_apart(query_high, range[0]));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    int bucket[4];
+                    of.find<false>(bucket, query_pos, pos + 8 * j + 4 * half);
+#pragma unroll
+                    for (int side = 0; side < 2; ++side)
+                        if (half == side)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) lds_add(&my_sums[bucket[i]][lane & 31], s[4 * j + i]);
+                }
+            } else {
                 float x = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) x += low == high || bucket[r] == u ? s[r] : 0.f;
+                for (int r = 0; r < 16; ++r) x += s[r];
                 x = taser_halves_sum(x);
-                if (half == 0) my_sums[u] += x;
+                if (half == 0) my_sums[low][lane] = sum_before + x;
             }
         }
 #pragma unroll
@@ -179,38 +232,52 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
 
     int tile = first;
     uint32_t keep0 = 0, keep1 = 0;
-    if (tile < last) {
-        keep0 = kept(tile);
-        fetch(k0, v0, pos0, range0, tile, keep0);
+    auto store_range = [&](int64_t pos, int at, int turn) {
+        if (wave == 0) taser_store_range(pos, lane < KT && (int64_t)at * KT + lane < length, lane, ranges[turn & 3]);
+    };
+    auto open = [&](char* k, char* v, int64_t* pos, int at, int turn, uint32_t& keep) {
+        if (at >= last) return;
+        keep = kept(at);
+        fetch(k, v, pos, at, keep);
+        look(at + 1);
+        if constexpr (BIAS) {
+            store_range(after_pos, at + 1, turn + 1);
+            next_pos = after_pos;
+            after_pos = state_pos(at + 2);
+        }
+    };
+    look(tile);
+    int turn = 0;
+    if constexpr (BIAS) {
+        next_pos = state_pos(tile);
+        after_pos = state_pos(tile + 1);
+        store_range(next_pos, tile, 0);
     }
-    for (; tile < last; tile += 2) {
+    open(k0, v0, pos0, tile, 0, keep0);
+    for (; tile < last; tile += 2, turn += 2) {
         taser_loads_arrived();
         __syncthreads();
-        if (tile + 1 < last) {
-            keep1 = kept(tile + 1);
-            fetch(k1, v1, pos1, range1, tile + 1, keep1);
-        }
-        compute(k0, v0, pos0, range0, keep0);
+        if constexpr (BIAS)
+            if (turn == 0) prepare(0);
+        open(k1, v1, pos1, tile + 1, turn + 1, keep1);
+        compute(k0, v0, pos0, turn, keep0);
         if (tile + 1 >= last) break;
         taser_loads_arrived();
         __syncthreads();
-        if (tile + 2 < last) {
-            keep0 = kept(tile + 2);
-            fetch(k0, v0, pos0, range0, tile + 2, keep0);
-        }
-        compute(k1, v1, pos1, range1, keep1);
+        open(k0, v0, pos0, tile + 2, turn + 2, keep0);
+        compute(k1, v1, pos1, turn + 1, keep1);
     }
 
     if constexpr (BIAS) {
+        lds_adds_done();
         __syncthreads();
         float* to = part_table + item * (a.group * a.buckets);
-        const float* sums = table + a.group * a.buckets;
         const int rows = a.rows - row_tile * 128 < 128 ? a.rows - row_tile * 128 : 128;
         for (int i = threadIdx.x; i < a.group * a.buckets; i += 256) {
             const int of = i / a.buckets, u = i - of * a.buckets;
             int r = (int)((of + a.group - (int64_t)row_tile * 128 % a.group) % a.group);   // the first row of this tile with that head
             float x = 0.f;
-            for (; r < rows; r += a.group) x += sums[r * a.buckets + u];
+            for (; r < rows; r += a.group) x += table_sums[r >> 5][u][r & 31];
             to[i] = x;
         }
     }
@@ -235,49 +302,55 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
 }
 
 // ---- dk, dv ---------------------------------------------------------------------------------------------------------------
-// A wave owns 32 states, their keys and values in registers (lane l: state l % 32); four waves share tiles of 32 rows. Rows of all
-// query heads of the key head pass by, so shared heads' gradients are whole.
+// Two waves own 32 states (lane l: state l % 32), four such pairs share tiles of 64 rows (32 in single precision). The first of a pair
+// has the keys in registers: scores, weights, dv. The second has the values: dp, dx, dk; the weights come to it through LDS. Each of a
+// tile's two steps is as many products for the one as for the other, and neither holds more than half of the sums: a wave with both
+// has too many registers for a second one on its SIMD (measured: 610 TFLOP/s so at 2 x 4096 x 4096, 16 heads of 128). Rows of all query
+// heads of the key head pass by, so shared heads' gradients are whole.
 template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dk, T* dv, float* part_dk,
+__global__ __launch_bounds__(512, (DP == 64 && sizeof(T) == 2 ? 4 : 2)) void attention_grad_states_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dk, T* dv, float* part_dk,
                                                                     float* part_dv, int64_t work) {
-    constexpr int RT = 32, ND = DP / 32, NC = DP / 16, BYTES = RT * DP * (int)sizeof(T);
+    constexpr int RT = sizeof(T) == 2 ? 64 : 32, NS = RT / 32, ND = DP / 32, NC = DP / 16, BYTES = RT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(1024))) char q0[BYTES], y0[BYTES], q1[BYTES], y1[BYTES];
-    __shared__ taser_f4 info0[4][RT / 4], info1[4][RT / 4];   // a kind of number of 4 rows
-    __shared__ int64_t pos0[BIAS ? RT : 1], pos1[BIAS ? RT : 1], range0[2], range1[2];
+    __shared__ taser_f4 passed[4][NS][4][64];                 // a pair's weights, by registers and lane
+    __shared__ taser_f4 info0[3][RT / 4], info1[3][RT / 4];   // a kind of number of 4 rows
+    __shared__ taser_f4 constants[BIAS ? 4 : 1][2][RT / 4];   // a pair's: what the exponents of 4 rows get added, of this tile and the next
+    __shared__ int64_t pos0[BIAS ? RT : 1], pos1[BIAS ? RT : 1], range0[NS][2], range1[NS][2];
     __shared__ int at0[BIAS ? RT : 1], at1[BIAS ? RT : 1];    // a row's place in the table
-    extern __shared__ float table[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    __shared__ uint8_t near[BIAS ? kTaserNear : 1];
+    __shared__ float table[BIAS ? TASER_MAX_GROUP_BUCKETS : 1];   // [buckets][group]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, pair = wave & 3;
+    const bool second = wave >= 4;
     const int64_t item = taser_stretch_of_work(blockIdx.x, work);
     if (item < 0) return;
     const int state_tile = (int)(item % a.row_tiles), split = (int)(item / a.row_tiles % a.splits);
-    const int64_t pair = item / a.row_tiles / a.splits;
-    const int hk = (int)(pair % a.kv_heads), b = (int)(pair / a.kv_heads);
+    const int64_t head_of = item / a.row_tiles / a.splits;
+    const int hk = (int)(head_of % a.kv_heads), b = (int)(head_of / a.kv_heads);
     const int32_t length = taser_length(a, b);
     const int all_tiles = state_tile * 128 < length ? (a.rows + RT - 1) / RT : 0, each = (all_tiles + a.splits - 1) / a.splits;
     const int first = split * each, last = first + each < all_tiles ? first + each : all_tiles;
 
-    const int state = state_tile * 128 + wave * 32 + (lane & 31);
+    const int state = state_tile * 128 + pair * 32 + (lane & 31);
     const bool real = state < length && (!a.mask || a.mask[b * a.mask_batch + state]);
-    taser_frag<T> k[NC], v[NC];
+    taser_frag<T> own[NC];   // the states' keys, or values
     {
         const int64_t at = real ? state : 0;
-        const T *k_from = (const T*)a.k + b * a.k_batch + hk * a.k_head + at * a.k_token, *v_from = (const T*)a.v + b * a.v_batch + hk * a.v_head + at * a.v_token;
+        const T* from = second ? (const T*)a.v + b * a.v_batch + hk * a.v_head + at * a.v_token : (const T*)a.k + b * a.k_batch + hk * a.k_head + at * a.k_token;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const int e = 16 * c + 8 * half, n = real ? a.dim - e : 0;
-            k[c] = taser_load_frag<T>(k_from + e, n);
-            v[c] = taser_load_frag<T>(v_from + e, n);
-        }
+        for (int c = 0; c < NC; ++c) own[c] = taser_load_frag<T>(from + 16 * c + 8 * half, real ? a.dim - 16 * c - 8 * half : 0);
     }
     int64_t key_pos = 0, bound = 0, key_low = 0, key_high = 0;
+    uint64_t foldable = 0;
+    TaserNear map;
     if constexpr (BIAS) {
         const T* from = (const T*)a.table + (int64_t)hk * a.group * a.buckets;
-        for (int i = threadIdx.x; i < a.group * a.buckets; i += 256) table[i] = (float)from[i];
+        for (int i = threadIdx.x; i < a.group * a.buckets; i += 512) table[i] = (float)from[i % a.group * a.buckets + i / a.group];
         key_pos = real ? a.key_pos[b * a.key_pos_batch + state] : 0;
         bound = taser_lane_bound(a, lane);
-        key_low = taser_wave_min(real ? key_pos : INT64_MAX);
-        key_high = taser_wave_max(real ? key_pos : INT64_MIN);
+        taser_range(key_pos, real, &key_low, &key_high);
+        map = TaserNear(a, near);
         __syncthreads();
+        foldable = taser_foldable(table, a.buckets, a.group, lane);
     }
     const bool any = __any(real);
     const T* const q_from = (const T*)a.q + b * a.q_batch + (int64_t)hk * a.group * a.q_head;
@@ -285,10 +358,27 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
     const int64_t y_token = (int64_t)a.heads * a.dim;
     // Where the heads of a query end with a tile, rows have the same places in every tile.
     const bool even = RT % a.group == 0;
-    TaserTileLoader<T, DP, RT, 256> load_q(threadIdx.x, a.dim, a.direct), load_y(threadIdx.x, a.dim, a.direct);
-    auto fetch = [&](char* q, char* y, taser_f4 (*rows_info)[RT / 4], int64_t* pos, int64_t* range, int* in_table, int tile) {
+    TaserTileLoader<T, DP, RT, 512> load_q(threadIdx.x, a.dim, a.direct), load_y(threadIdx.x, a.dim, a.direct);
+    // What one wave writes down of a tile's rows, a lane a row, is on its way a tile ahead.
+    taser_f4 ahead_info = {INFINITY, 0.f, 0.f, 0.f};
+    int64_t ahead_pos = 0;
+    int ahead_head = 0;
+    auto look = [&](int tile) {
+        if (wave != 4) return;
+        const int64_t at = (int64_t)tile * RT + lane;
+        const bool there = lane < RT && at < a.rows;
+        const int row = there ? (int)at : 0, query = row / a.group, g = row - query * a.group;
+        taser_f4 w = {INFINITY, 0.f, 0.f, 0.f};
+        if (there) w = info[((int64_t)b * a.queries + query) * a.heads + hk * a.group + g];
+        ahead_info = w;
+        if constexpr (BIAS) {
+            ahead_head = g;
+            ahead_pos = there ? a.query_pos[b * a.query_pos_batch + query] : 0;
+        }
+    };
+    auto fetch = [&](char* q, char* y, taser_f4 (*rows_info)[RT / 4], int64_t* pos, int64_t (*range)[2], int* in_table, int tile) {
         const int at = tile * RT, n = a.rows - at < RT ? a.rows - at : RT, query0 = at / a.group;
-        const uint32_t keep = n >= 32 ? ~0u : (1u << n) - 1;
+        const uint64_t keep = n >= 64 ? ~0ull : (1ull << n) - 1;
         auto row_at = [&](int64_t token, int64_t head) {
             return [=](int r) -> int64_t {   // past the last row: the last one's place, outside `keep`
                 const int row = at + (r < n ? r : n - 1), query = row / a.group;
@@ -302,24 +392,20 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
         }
         load_q.load(q, q_from + query0 * a.q_token, kTaserTileBytes, keep, n < RT, q_at);
         load_y.load(y, y_from + query0 * y_token, kTaserTileBytes, keep, n < RT, y_at);
-        if (threadIdx.x < 64) {
-            const bool there = lane < n && lane < RT;
-            const int row = there ? at + lane : 0, query = row / a.group, g = row - query * a.group;
-            taser_f4 w = {INFINITY, 0.f, 0.f, INFINITY};
-            if (there) w = info[((int64_t)b * a.queries + query) * a.heads + hk * a.group + g];
+        if (wave == 4) {
             if (lane < RT)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ((float*)rows_info[i])[lane] = w[i];
+                for (int i = 0; i < 3; ++i) ((float*)rows_info[i])[lane] = i == 0 && !BIAS ? fmaf(-ahead_info[0], kLog2e, -ahead_info[1]) : ahead_info[i];   // (without a bias: the constant itself)
             if constexpr (BIAS) {
-                const int64_t p = there ? a.query_pos[b * a.query_pos_batch + query] : 0;
+                const bool there = lane < n && lane < RT;
                 if (lane < RT) {
-                    pos[lane] = p;
-                    in_table[lane] = g * a.buckets;
+                    pos[lane] = ahead_pos;
+                    in_table[lane] = ahead_head;
                 }
-                const int64_t low = taser_wave_min(there ? p : INT64_MAX), high = taser_wave_max(there ? p : INT64_MIN);
-                if (lane == 0) {
-                    range[0] = low;
-                    range[1] = high;
+                const int64_t low = taser_half_min(there ? ahead_pos : INT64_MAX), high = -taser_half_min(there ? -ahead_pos : INT64_MAX);
+                if ((lane & 31) == 0 && lane < RT) {
+                    range[lane >> 5][0] = low;
+                    range[lane >> 5][1] = high;
                 }
             }
         }
@@ -329,103 +415,161 @@ __global__ __launch_bounds__(256) void attention_grad_states_kernel(const TaserA
     constexpr float lift = std::is_same_v<T, _Float16> ? 16384.f : 1.f;
     const TaserRowsAt<T, DP> rows_at(lane);
     const TaserColumnsAt<T, DP> columns_at(lane);
-    taser_f16 sum_k[ND], sum_v[ND];
+    taser_f16 sum[ND];   // of dv, or dk
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum_k[d][r] = sum_v[d][r] = 0.f;
+        for (int r = 0; r < 16; ++r) sum[d][r] = 0.f;
     const float scale2 = a.scale * kLog2e;
+    taser_f16 x[NS];     // scores, then weights; or dp, then dx
 
-    auto compute = [&](const char* q, const char* y, const taser_f4 (*rows_info)[RT / 4], const int64_t* pos, const int64_t* range, const int* in_table) {
-        if (!any) return;
-        taser_f16 s, dp;
+    // As in the forward pass: one bias for the tile goes into the rows' constants, others into the scores. Which it is, and the constants,
+    // are found a tile ahead, under the products of the step before.
+    int low[NS], high[NS];
+    bool sums = false;
+    auto prepare = [&](const taser_f4 (*rows_info)[RT / 4], const int64_t (*range)[2], const int* in_table, int turn) {
+        bool one = true;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+        for (int n = 0; n < NS; ++n) {
+            low[n] = taser_uniform_bucket(bound, taser_apart(range[n][0], key_high), a.buckets);
+            high[n] = taser_uniform_bucket(bound, taser_apart(range[n][1], key_low), a.buckets);
+            one = one && low[n] == high[n] && (foldable >> low[n]) & 1;
+        }
+        sums = !one;
+        float bias = 0.f, top = 0.f, log_sum = 0.f;
+        if (lane < RT) {   // a lane a row
+            bias = table[low[lane >> 5 < NS ? lane >> 5 : 0] * a.group + in_table[lane]];
+            top = ((const float*)rows_info[0])[lane];
+            log_sum = ((const float*)rows_info[1])[lane];
+        }
+        if (lane < RT) ((float*)constants[pair][turn & 1])[lane] = fmaf(sums ? 0.f : bias - top, kLog2e, -log_sum);
+    };
+    // First step: the scores and their weights, or dp.
+    auto begin = [&](const char* q, const char* y, const taser_f4 (*rows_info)[RT / 4], const int64_t* pos, const int64_t (*range)[2], const int* in_table, int turn) {
+        if (second) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            taser_mma(s, rows_at.operand(q, 0, c), k[c]);
-            taser_mma(dp, rows_at.operand(y, 0, c), v[c]);
+            for (int n = 0; n < NS; ++n) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[n][r] = 0.f;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) taser_mma(x[n], rows_at.operand(y, 32 * n, c), own[c]);
+            }
+            if constexpr (sizeof(T) == 2) taser_order<8, 1, NS * NC>();
+            return;
+        }
+        const float by = BIAS && sums ? kLog2e : scale2;
+        const taser_f4* plus = BIAS ? constants[pair][turn & 1] : rows_info[0];
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[n][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) taser_mma(x[n], rows_at.operand(q, 32 * n, c), own[c]);
         }
         if constexpr (BIAS) {
-            const int low = taser_uniform_bucket(bound, taser_apart(range[0], key_high)), high = taser_uniform_bucket(bound, taser_apart(range[1], key_low));
-            int bucket[16];
-            if (low == high) {
+            if (sums) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) bucket[r] = low;
-            } else {   // distances count the other way round here: bound <= query - key
-                int64_t apart[16];
+                for (int n = 0; n < NS; ++n) {
+                    const TaserBuckets of(map, near, bound, low[n], high[n], taser_apart(range[n][0], key_high), taser_apart(range[n][1], key_low));
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    apart[r] = taser_apart(pos[8 * (r >> 2) + 4 * half + (r & 3)], key_pos);
-                    bucket[r] = low;
-                }
-                for (int i = low; i < high; ++i) {
-                    const int64_t x = taser_lane_value(bound, i);
+                    for (int j = 0; j < 4; ++j) {
+                        int bucket[4];
+                        const int row = 32 * n + 8 * j + 4 * half;
+                        of.find<true>(bucket, key_pos, pos + row);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) bucket[r] += x <= apart[r];
+                        for (int i = 0; i < 4; ++i)
+                            x[n][4 * j + i] = fmaf(x[n][4 * j + i], a.scale, table[bucket[i] * a.group + in_table[row + i]]) - ((const float*)rows_info[0])[row + i];
+                    }
                 }
             }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.scale, table[in_table[8 * (r >> 2) + 4 * half + (r & 3)] + bucket[r]]);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const taser_f4 top = rows_info[0][2 * j + half], inverse = rows_info[1][2 * j + half], t = rows_info[2][2 * j + half], whole = rows_info[3][2 * j + half];
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 4 * j + i;
-                float p = BIAS ? __builtin_amdgcn_exp2f((s[r] - top[i]) * kLog2e) * inverse[i] : __builtin_amdgcn_exp2f(fmaf(s[r], scale2, -whole[i]));
-                if (!real) p = 0.f;
-                s[r] = p;
-                dp[r] = p * (dp[r] - t[i]);
+            for (int j = 0; j < 4; ++j) {
+                const taser_f4 more = plus[8 * n + 2 * j + half];
+                taser_f4 w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[i] = __builtin_amdgcn_exp2f(fmaf(x[n][4 * j + i], by, more[i]));
+                    if (!real) w[i] = 0.f;
+                    x[n][4 * j + i] = w[i];
+                }
+                passed[pair][n][j][lane] = w;
             }
+    };
+    // Second step: dv, or dx and dk.
+    auto end = [&](const char* q, const char* y, const taser_f4 (*rows_info)[RT / 4]) {
+        if (second) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const taser_f4 w = passed[pair][n][j][lane], t = rows_info[2][8 * n + 2 * j + half];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[n][4 * j + i] = w[i] * (x[n][4 * j + i] - t[i]);
+                }
         }
+        const char* from = second ? q : y;
+        const float up = second ? 1.f : lift;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const taser_frag<T> p = taser_operand<T>(s, h, lift), x = taser_operand<T>(dp, h);
+        for (int n = 0; n < NS; ++n)
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-                taser_mma(sum_v[d], columns_at.operand(y, 16 * h, d), p);
-                taser_mma(sum_k[d], columns_at.operand(q, 16 * h, d), x);
+            for (int h = 0; h < 2; ++h) {
+                const taser_frag<T> w = taser_operand<T>(x[n], h, up);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) taser_mma(sum[d], columns_at.operand(from, 32 * n + 16 * h, d), w);
             }
-        }
     };
 
     int tile = first;
-    if (tile < last) fetch(q0, y0, info0, pos0, range0, at0, tile);
-    for (; tile < last; tile += 2) {
+    auto open = [&](char* q, char* y, taser_f4 (*rows_info)[RT / 4], int64_t* pos, int64_t (*range)[2], int* in_table, int at) {
+        if (at >= last) return;
+        fetch(q, y, rows_info, pos, range, in_table, at);
+        look(at + 1);
+    };
+    look(tile);
+    open(q0, y0, info0, pos0, range0, at0, tile);
+    for (int turn = 0; tile < last; tile += 2, turn += 2) {
         taser_loads_arrived();
         __syncthreads();
-        if (tile + 1 < last) fetch(q1, y1, info1, pos1, range1, at1, tile + 1);
-        compute(q0, y0, info0, pos0, range0, at0);
+        if constexpr (BIAS)
+            if (turn == 0 && !second) prepare(info0, range0, at0, 0);
+        open(q1, y1, info1, pos1, range1, at1, tile + 1);
+        if (any) begin(q0, y0, info0, pos0, range0, at0, turn);
+        taser_lds_barrier();
+        if constexpr (BIAS)
+            if (!second && tile + 1 < last) prepare(info1, range1, at1, turn + 1);
+        if (any) end(q0, y0, info0);
         if (tile + 1 >= last) break;
         taser_loads_arrived();
         __syncthreads();
-        if (tile + 2 < last) fetch(q0, y0, info0, pos0, range0, at0, tile + 2);
-        compute(q1, y1, info1, pos1, range1, at1);
+        open(q0, y0, info0, pos0, range0, at0, tile + 2);
+        if (any) begin(q1, y1, info1, pos1, range1, at1, turn + 1);
+        taser_lds_barrier();
+        if constexpr (BIAS)
+            if (!second && tile + 2 < last) prepare(info0, range0, at0, turn + 2);
+        if (any) end(q1, y1, info1);
     }
 
     if (state >= a.keys) return;
     const int64_t at = (((int64_t)b * a.keys + state) * a.kv_heads + hk) * a.dim, all = (int64_t)a.batch * a.keys * a.kv_heads * a.dim;
+    const float by = second ? a.scale : 1.f / lift;
+    T* to = (second ? dk : dv) + at;
+    float* part = part_dk ? (second ? part_dk : part_dv) + split * all + at : nullptr;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int e = 32 * d + 8 * j + 4 * half;
-            T x[4], y[4];
+            T y[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float one = sum_k[d][4 * j + i] * a.scale, two = sum_v[d][4 * j + i] * (1.f / lift);
-                x[i] = (T)one;
-                y[i] = (T)two;
-                if (part_dk && e + i < a.dim) {
-                    part_dk[split * all + at + e + i] = one;
-                    part_dv[split * all + at + e + i] = two;
-                }
+                const float one = sum[d][4 * j + i] * by;
+                y[i] = (T)one;
+                if (part && e + i < a.dim) part[e + i] = one;
             }
-            if (part_dk) continue;
-            taser_store(dk + at + e, a.dim - e, x);
-            taser_store(dv + at + e, a.dim - e, y);
+            if (!part) taser_store(to + e, a.dim - e, y);
         }
 }
 
@@ -510,7 +654,7 @@ int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stat
         {
             TaserProfileSpan span(stream, "attention_grad_queries");
             if (a.table)
-                attention_grad_queries_kernel<T, DP, true><<<grid, 256, sizeof(float) * (a.group + 128) * a.buckets, stream>>>(a, info, dout, dq, part, part_table, items);
+                attention_grad_queries_kernel<T, DP, true><<<grid, 256, 0, stream>>>(a, info, dout, dq, part, part_table, items);
             else
                 attention_grad_queries_kernel<T, DP, false><<<grid, 256, 0, stream>>>(a, info, dout, dq, part, part_table, items);
             TASER_HIP_TRY(hipGetLastError());
@@ -539,9 +683,9 @@ int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stat
         {
             TaserProfileSpan span(stream, "attention_grad_states");
             if (a.table)
-                attention_grad_states_kernel<T, DP, true><<<grid, 256, sizeof(float) * a.group * a.buckets, stream>>>(a, info, dout, dk, dv, part, part_v, items);
+                attention_grad_states_kernel<T, DP, true><<<grid, 512, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
             else
-                attention_grad_states_kernel<T, DP, false><<<grid, 256, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
+                attention_grad_states_kernel<T, DP, false><<<grid, 512, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
             TASER_HIP_TRY(hipGetLastError());
         }
         if (part) {
