@@ -38,8 +38,30 @@ struct TaserAttentionArgs {
 
 // Checks a call's arguments and lays them out for the kernels.
 int taser_attention_args(const taser_attention* p, const char* what, TaserAttentionArgs* a);
+// In how many parts the long axis of `blocks` blocks is cut, `tiles` tiles of `tile` us each, where `slots` blocks run at a time: the
+// parts' sums, `bytes` of them a part, are written in 32 bits and read again, in a launch of its own. The cheapest number of parts by that.
+inline int taser_splits(int64_t blocks, int64_t slots, int64_t tiles, double tile, int64_t bytes) {
+    if (blocks < 1 || tiles < 2) return 1;
+    int best = 1;
+    double least = 0.;
+    for (int n = 1; n <= 128 && n <= tiles; n += n < 16 ? 1 : 8) {
+        const double us = (double)((blocks * n + slots - 1) / slots) * (2. * tile + tile * (double)((tiles + n - 1) / n)) + (n > 1 ? 5. + 2. * (double)(n * bytes) / 4e6 : 0.);
+        if (n == 1 || us < 0.95 * least) {
+            best = n;
+            least = us;
+        }
+    }
+    return best;
+}
+
 // Work of taser_cross_attention_grad in bytes.
 uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t type);
+
+// Buckets to whole float4: what a row of such parts takes.
+__host__ __device__ inline int taser_padded(int buckets) { return (buckets + 3) & ~3; }
+// dtable[head][u] = the sum of parts [outer][kv_heads][inner][rows][taser_padded(buckets)] over outer, inner and the rows of that head (row r: head r % group
+// of its key head's).
+int taser_add_tables(const float* parts, int64_t outer, int64_t inner, int32_t kv_heads, int32_t rows, int32_t group, int32_t buckets, int32_t type, void* dtable, hipStream_t stream);
 
 // Windows of few states and rows: kernels of their own.
 bool taser_window_fits(const TaserAttentionArgs& a);
@@ -282,17 +304,18 @@ struct TaserNear {
     int64_t base;   // the table's first entry: just below the first bound
     int last;       // its last; -1: there is no table
     __device__ TaserNear() : base(0), last(-1) {}
-    // By all threads of a block, before a barrier.
-    __device__ TaserNear(const TaserAttentionArgs& a, uint8_t* near) : base(0), last(-1) {
-        if (a.buckets < 2) return;
-        base = a.bounds[0] - 1;
-        const uint64_t span = (uint64_t)a.bounds[a.buckets - 2] - (uint64_t)base;
+    // By all threads of a block, before a barrier; lane l has bound l.
+    __device__ TaserNear(int64_t bound, int buckets, uint8_t* near) : base(0), last(-1) {
+        if (buckets < 2) return;
+        base = taser_lane_value(bound, 0) - 1;
+        const uint64_t span = (uint64_t)taser_lane_value(bound, buckets - 2) - (uint64_t)base;
         if (span >= (uint64_t)kTaserNear) return;
         last = (int)span;
-        for (int e = threadIdx.x; e <= last; e += blockDim.x) {
+        for (int e0 = 0; e0 <= last; e0 += blockDim.x) {
+            const int e = e0 + threadIdx.x;
             int n = 0;
-            for (int u = 0; u < a.buckets - 1; ++u) n += a.bounds[u] - base <= e;
-            near[e] = (uint8_t)n;
+            for (int u = 0; u < buckets - 1; ++u) n += (int)(taser_lane_value(bound, u) - base) <= e;
+            if (e <= last) near[e] = (uint8_t)n;
         }
     }
 };

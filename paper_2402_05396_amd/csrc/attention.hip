@@ -8,6 +8,7 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMostSplits = 128;
 
 // A wave owns 32 query rows (of the queries of one key head: row r is query r / group, head r % group of them), lane l row
 // l % 32 of them. Scores come out transposed, states in registers, so a row's softmax needs one exchange, with the other half of
@@ -27,7 +28,7 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
     __shared__ __attribute__((aligned(1024))) char k0[S::kTiles][S::kTileBytes], v0[S::kTiles][S::kTileBytes], k1[S::kTiles][S::kTileBytes], v1[S::kTiles][S::kTileBytes];
     __shared__ int64_t pos0[S::kTiles][BIAS ? KT : 1], pos1[S::kTiles][BIAS ? KT : 1], ranges[S::kTiles][4][2];
     __shared__ float joined[2][S::kWaves][32];
-    __shared__ uint8_t near[BIAS ? kTaserNear : 1];
+    __shared__ uint8_t near[BIAS && SHARED ? kTaserNear : 1];
     __shared__ float table[BIAS ? TASER_MAX_GROUP_BUCKETS : 1];   // [buckets][group]; of its own, so that no read of it waits for a tile
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t item = taser_stretch_of_work(blockIdx.x, work);
@@ -57,7 +58,7 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
         query_pos = a.query_pos[b * a.query_pos_batch + (row < a.rows ? row : a.rows - 1) / a.group];
         bound = taser_lane_bound(a, lane);
         taser_range(query_pos, true, &query_low, &query_high);
-        map = TaserNear(a, near);
+        if (SHARED) map = TaserNear(bound, a.buckets, near);   // (a few rows meet few tiles of several buckets: not worth making)
         __syncthreads();
         foldable = taser_foldable(table, a.buckets, a.group, lane);
     }
@@ -336,17 +337,19 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
     }
 }
 
-// Joins the splits: a thread has one element of a row.
+// Joins the splits, where they are few: a thread has one element of a row.
 template <typename T>
-__global__ __launch_bounds__(256) void attention_join_kernel(const float* part_out, const float* part_stats, int64_t rows, int32_t dim, int32_t splits, T* out, float* stats,
-                                                             int32_t stat_floats) {
+__global__ __launch_bounds__(256) void attention_join_few_kernel(const float* part_out, const float* part_stats, int64_t rows, int32_t dim, int32_t splits, T* out, float* stats,
+                                                                 int32_t stat_floats) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= rows * dim) return;
     const int64_t row = i / dim;
     const int e = (int)(i - row * dim);
     float top = -INFINITY, sum = 0.f, x = 0.f;
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) top = fmaxf(top, part_stats[2 * (s * rows + row)]);
     if (top != -INFINITY)
+#pragma unroll 4
         for (int s = 0; s < splits; ++s) {
             const float by = __builtin_amdgcn_exp2f((part_stats[2 * (s * rows + row)] - top) * kLog2e);
             sum = fmaf(by, part_stats[2 * (s * rows + row) + 1], sum);
@@ -358,6 +361,53 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const float* part_o
     if (sizeof(T) == 2) taser_rest<T>(stats, row, stat_floats)[e] = (T)(x - (float)(T)x);
     if (e == 0) {
         stats[row * stat_floats] = top;
+        stats[row * stat_floats + 1] = sum;
+    }
+}
+
+// Where they are many: a block has a row, a thread one element of every eighth split. (96 rows of 97 splits 7 us, 66 by the other; 6 000
+// rows of 6 splits 29 us, and 8 by the other.)
+template <typename T>
+__global__ __launch_bounds__(1024) void attention_join_kernel(const float* part_out, const float* part_stats, int64_t rows, int32_t dim, int32_t splits, T* out, float* stats,
+                                                              int32_t stat_floats) {
+    __shared__ float weights[kMostSplits], parts[8][TASER_MAX_HEAD_DIM], whole[2];
+    const int64_t row = blockIdx.x;
+    const int e = threadIdx.x & 127, chain = threadIdx.x >> 7;
+    if (threadIdx.x < 64) {   // the splits' weights, and the row's sum in one order
+        float top = -INFINITY, sum = 0.f;
+        for (int s = threadIdx.x; s < splits; s += 64) top = fmaxf(top, part_stats[2 * (s * rows + row)]);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+        for (int s = threadIdx.x; s < splits; s += 64) {
+            const float by = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((part_stats[2 * (s * rows + row)] - top) * kLog2e);
+            weights[s] = by;
+            sum = fmaf(by, part_stats[2 * (s * rows + row) + 1], sum);
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+        if (threadIdx.x == 0) {
+            whole[0] = top;
+            whole[1] = sum;
+        }
+    }
+    __syncthreads();
+    float x = 0.f;
+    if (e < dim)
+#pragma unroll 4
+        for (int s = chain; s < splits; s += 8) x = fmaf(weights[s], part_out[(s * rows + row) * dim + e], x);
+    parts[chain][e] = x;
+    __syncthreads();
+    if (chain || e >= dim) return;
+    x = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) x += parts[c][e];
+    const float sum = whole[1];
+    x = sum != 0.f ? x / sum : 0.f;
+    out[row * dim + e] = (T)x;
+    if (!stats) return;
+    if (sizeof(T) == 2) taser_rest<T>(stats, row, stat_floats)[e] = (T)(x - (float)(T)x);
+    if (e == 0) {
+        stats[row * stat_floats] = whole[0];
         stats[row * stat_floats + 1] = sum;
     }
 }
@@ -382,7 +432,10 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
     }
     if (a.splits > 1) {
         TaserProfileSpan span(stream, "attention_join");
-        attention_join_kernel<T><<<dim3((unsigned)((rows * a.dim + 255) / 256)), 256, 0, stream>>>(part_out, part_stats, rows, a.dim, a.splits, (T*)out, stats, a.stat_floats);
+        if (a.splits <= 16)
+            attention_join_few_kernel<T><<<dim3((unsigned)((rows * a.dim + 255) / 256)), 256, 0, stream>>>(part_out, part_stats, rows, a.dim, a.splits, (T*)out, stats, a.stat_floats);
+        else
+            attention_join_kernel<T><<<dim3((unsigned)rows), 1024, 0, stream>>>(part_out, part_stats, rows, a.dim, a.splits, (T*)out, stats, a.stat_floats);
         TASER_HIP_TRY(hipGetLastError());
     }
     return TASER_OK;
@@ -396,18 +449,16 @@ template <typename T> int launch_typed(TaserAttentionArgs& a, bool shared, void*
 bool few_rows(const TaserAttentionArgs& a) { return a.rows <= 64; }
 
 // Parts of the states, so that the chip is full where there are few rows.
-int splits_for(const TaserAttentionArgs& a) {
-    const bool few = few_rows(a);
+int splits_for(const TaserAttentionArgs& a, int32_t type) {
     if (taser_window_fits(a)) return 1;
-    const int64_t blocks = (int64_t)a.batch * a.kv_heads * (few ? (a.rows + 31) / 32 : (a.rows + 127) / 128);
-    if (!blocks) return 1;
-    const int64_t most = a.keys / (few ? 256 : 512), wanted = (512 + blocks - 1) / blocks;
-    const int64_t n = wanted < most ? wanted : most;
-    return n < 1 ? 1 : (n > 256 ? 256 : (int)n);
+    const int64_t pairs = (int64_t)a.batch * a.kv_heads, bytes = pairs * a.rows * a.dim * 4;
+    const double width = a.dim <= 64 ? 0.5 : 1.;
+    // us of a tile for a block, of 64 states for 128 rows, or of 128 for 32 (measured)
+    if (few_rows(a)) return taser_splits(pairs * ((a.rows + 31) / 32), 512, (a.keys + 127) / 128, width * (type == TASER_F32 ? 5. : 2.), bytes);
+    return taser_splits(pairs * ((a.rows + 127) / 128), type == TASER_F32 ? 256 : 512, (a.keys + 63) / 64, width * (type == TASER_F32 ? 14. : 2.5), bytes);
 }
 
-uint64_t work_bytes(const TaserAttentionArgs& a) {
-    const int splits = splits_for(a);
+uint64_t work_bytes(const TaserAttentionArgs& a, int splits) {
     return splits > 1 ? sizeof(float) * (uint64_t)splits * a.batch * a.queries * a.heads * (a.dim + 2) : 0;
 }
 
@@ -459,7 +510,7 @@ int taser_attention_args(const taser_attention* p, const char* what, TaserAttent
 extern "C" int taser_cross_attention_bytes(const taser_attention* p, uint64_t* work, uint64_t* grad_work) {
     TaserAttentionArgs a;
     if (const int rc = taser_attention_args(p, "cross_attention_bytes", &a)) return rc;
-    if (work) *work = work_bytes(a);
+    if (work) *work = work_bytes(a, splits_for(a, p->type));
     if (grad_work) *grad_work = taser_attention_grad_bytes(a, p->type);
     return TASER_OK;
 }
@@ -469,8 +520,8 @@ extern "C" int taser_cross_attention(const taser_attention* p, void* out, float*
     if (const int rc = taser_attention_args(p, "cross_attention", &a)) return rc;
     if (!a.batch || !a.queries) return TASER_OK;
     if (!out) return taser_fail(TASER_E_ARG, "cross_attention: null output");
-    a.splits = splits_for(a);
-    const uint64_t need = work_bytes(a);
+    a.splits = splits_for(a, p->type);
+    const uint64_t need = work_bytes(a, a.splits);
     if (need > work_size) return taser_fail(TASER_E_RANGE, "cross_attention: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)need);
     if (need && (!work || (uintptr_t)work % 16)) return taser_fail(TASER_E_ARG, "cross_attention: null or misaligned workspace");
     hipStream_t stream = (hipStream_t)hip_stream;

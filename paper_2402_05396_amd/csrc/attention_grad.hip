@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
         query_pos = a.query_pos[b * a.query_pos_batch + (row < a.rows ? row : a.rows - 1) / a.group];
         bound = taser_lane_bound(a, lane);
         taser_range(query_pos, true, &query_low, &query_high);
-        map = TaserNear(a, near);
+        map = TaserNear(bound, a.buckets, near);
         __syncthreads();
         foldable = taser_foldable(table, a.buckets, a.group, lane);
     }
@@ -271,14 +271,14 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
     if constexpr (BIAS) {
         lds_adds_done();
         __syncthreads();
-        float* to = part_table + item * (a.group * a.buckets);
+        float* to = part_table + item * (a.group * taser_padded(a.buckets));
         const int rows = a.rows - row_tile * 128 < 128 ? a.rows - row_tile * 128 : 128;
         for (int i = threadIdx.x; i < a.group * a.buckets; i += 256) {
             const int of = i / a.buckets, u = i - of * a.buckets;
             int r = (int)((of + a.group - (int64_t)row_tile * 128 % a.group) % a.group);   // the first row of this tile with that head
             float x = 0.f;
             for (; r < rows; r += a.group) x += table_sums[r >> 5][u][r & 31];
-            to[i] = x;
+            to[of * taser_padded(a.buckets) + u] = x;
         }
     }
     if (!real) return;
@@ -348,7 +348,7 @@ __global__ __launch_bounds__(512, (DP == 64 && sizeof(T) == 2 ? 4 : 2)) void att
         key_pos = real ? a.key_pos[b * a.key_pos_batch + state] : 0;
         bound = taser_lane_bound(a, lane);
         taser_range(key_pos, real, &key_low, &key_high);
-        map = TaserNear(a, near);
+        map = TaserNear(bound, a.buckets, near);
         __syncthreads();
         foldable = taser_foldable(table, a.buckets, a.group, lane);
     }
@@ -582,20 +582,35 @@ template <typename T> __global__ __launch_bounds__(256) void attention_grad_add_
     out[i] = (T)x;
 }
 
-// dtable of one head: parts [batch, kv_heads, per_pair][group, buckets], four chains of sums.
+// A block has a head, a thread four buckets of a chain of sums: as many chains as there are threads, then the chains in their order.
 template <typename T>
-__global__ __launch_bounds__(256) void attention_grad_table_kernel(const float* parts, int32_t batch, int32_t kv_heads, int32_t group, int32_t per_pair, int32_t buckets, T* dtable) {
-    __shared__ float sums[4][64];
-    const int head = blockIdx.x, hk = head / group, g = head - hk * group, chain = threadIdx.x >> 6, u = threadIdx.x & 63;
-    float x = 0.f;
-    if (u < buckets)
-        for (int64_t i = chain; i < (int64_t)batch * per_pair; i += 4) {
-            const int64_t item = (i / per_pair * kv_heads + hk) * per_pair + i % per_pair;
-            x += parts[(item * group + g) * buckets + u];
+__global__ __launch_bounds__(1024) void attention_grad_table_kernel(const float* parts, int64_t outer, int64_t inner, int32_t kv_heads, int32_t rows, int32_t group, int32_t buckets, T* dtable) {
+    __shared__ taser_f4 sums[1024];
+    const int head = blockIdx.x, hk = head / group, g = head - hk * group, width = taser_padded(buckets) / 4, chains = 1024 / width, chain = threadIdx.x / width, u = threadIdx.x % width;
+    taser_f4 x = {0.f, 0.f, 0.f, 0.f};
+    if (chain < chains) {
+#pragma unroll 4
+        for (int64_t i = chain; i < outer * inner; i += chains) {
+            const taser_f4* from = (const taser_f4*)parts + ((i / inner * kv_heads + hk) * inner + i % inner) * rows * width + u;
+            for (int r = g; r < rows; r += group) x += from[r * width];
         }
-    sums[chain][u] = x;
+    }
+    sums[threadIdx.x] = x;
     __syncthreads();
-    if ((int)threadIdx.x < buckets) dtable[(int64_t)head * buckets + u] = (T)((sums[0][u] + sums[1][u]) + (sums[2][u] + sums[3][u]));
+    // 16 chains of chains, then those
+    if (chain < 16) {
+        x = taser_f4{0.f, 0.f, 0.f, 0.f};
+        for (int c = chain; c < chains; c += 16) x += sums[c * width + u];
+    }
+    __syncthreads();
+    if (chain < 16) sums[threadIdx.x] = x;
+    __syncthreads();
+    if (chain) return;
+    x = taser_f4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < 16; ++c) x += sums[c * width + u];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (4 * u + i < buckets) dtable[(int64_t)head * buckets + 4 * u + i] = (T)x[i];
 }
 
 struct Plan {
@@ -603,17 +618,15 @@ struct Plan {
     uint64_t info, dq, dk, dv, table, bytes;                // places in the workspace
 };
 
-Plan plan(const TaserAttentionArgs& a) {
+Plan plan(const TaserAttentionArgs& a, int32_t type) {
     Plan p = {};
     const int64_t pairs = (int64_t)a.batch * a.kv_heads;
-    auto parts = [&](int64_t blocks, int64_t most) {
-        const int64_t n = blocks ? (512 + blocks - 1) / blocks : 1;
-        return (int)(n < most ? (n < 1 ? 1 : n) : (most < 1 ? 1 : (most > 64 ? 64 : most)));
-    };
     p.row_tiles = (int)(((int64_t)a.rows + 127) / 128);
     p.state_tiles = (int)(((int64_t)a.keys + 127) / 128);
-    p.row_splits = parts(pairs * p.row_tiles, a.keys / 256);
-    p.state_splits = parts(pairs * p.state_tiles, a.rows / 256);
+    const int64_t rows_bytes = pairs * a.rows * a.dim * 4, states_bytes = 2 * pairs * a.keys * a.dim * 4;
+    const double tile = (a.dim <= 64 ? 0.5 : 1.) * (type == TASER_F32 ? 11. : 1.5);   // us of 32 states, or rows, for a block (measured)
+    p.row_splits = taser_splits(pairs * p.row_tiles, type == TASER_F32 ? 256 : 512, (a.keys + 31) / 32, tile, rows_bytes);
+    p.state_splits = taser_splits(pairs * p.state_tiles, type != TASER_F32 && a.dim <= 64 ? 512 : 256, (a.rows + 31) / 32, tile, states_bytes);
     auto take = [&](uint64_t bytes) {
         const uint64_t at = p.bytes;
         p.bytes += (bytes + 255) / 256 * 256;
@@ -624,7 +637,7 @@ Plan plan(const TaserAttentionArgs& a) {
     p.dq = take(p.row_splits > 1 ? p.row_splits * rows * a.dim * 4 : 0);
     p.dk = take(p.state_splits > 1 ? p.state_splits * states * 4 : 0);
     p.dv = take(p.state_splits > 1 ? p.state_splits * states * 4 : 0);
-    p.table = take(a.table ? (uint64_t)pairs * p.row_tiles * p.row_splits * a.group * a.buckets * 4 : 0);
+    p.table = take(a.table ? (uint64_t)pairs * p.row_tiles * p.row_splits * a.group * taser_padded(a.buckets) * 4 : 0);
     return p;
 }
 
@@ -663,9 +676,8 @@ int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stat
             if (const int rc = add_up<T>(part, p.row_splits, rows * a.dim, dq, stream)) return rc;
     }
     if (a.table) {
-        TaserProfileSpan span(stream, "attention_grad_table");
-        attention_grad_table_kernel<T><<<dim3((unsigned)a.heads), 256, 0, stream>>>(part_table, rows ? a.batch : 0, a.kv_heads, a.group, p.row_tiles * p.row_splits, a.buckets, dtable);
-        TASER_HIP_TRY(hipGetLastError());
+        const int32_t type = std::is_same_v<T, float> ? TASER_F32 : std::is_same_v<T, _Float16> ? TASER_F16 : TASER_BF16;
+        if (const int rc = taser_add_tables(part_table, rows ? a.batch : 0, (int64_t)p.row_tiles * p.row_splits, a.kv_heads, a.group, a.group, a.buckets, type, dtable, stream)) return rc;
     }
     if (states) {
         a.row_tiles = p.state_tiles;
@@ -704,10 +716,20 @@ int launch_typed(TaserAttentionArgs& a, const Plan& p, const void* out, const fl
 
 }  // namespace
 
+int taser_add_tables(const float* parts, int64_t outer, int64_t inner, int32_t kv_heads, int32_t rows, int32_t group, int32_t buckets, int32_t type, void* dtable, hipStream_t stream) {
+    TaserProfileSpan span(stream, "attention_grad_table");
+    const dim3 grid((unsigned)(kv_heads * group));
+    if (type == TASER_F32) attention_grad_table_kernel<float><<<grid, 1024, 0, stream>>>(parts, outer, inner, kv_heads, rows, group, buckets, (float*)dtable);
+    else if (type == TASER_F16) attention_grad_table_kernel<_Float16><<<grid, 1024, 0, stream>>>(parts, outer, inner, kv_heads, rows, group, buckets, (_Float16*)dtable);
+    else attention_grad_table_kernel<__bf16><<<grid, 1024, 0, stream>>>(parts, outer, inner, kv_heads, rows, group, buckets, (__bf16*)dtable);
+    TASER_HIP_TRY(hipGetLastError());
+    return TASER_OK;
+}
+
 // Windows go their own way where there is anything to do.
 static bool window(const TaserAttentionArgs& a) { return taser_window_fits(a) && a.batch && a.queries; }
 
-uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t) { return window(a) ? taser_window_grad_bytes(a) : plan(a).bytes; }
+uint64_t taser_attention_grad_bytes(const TaserAttentionArgs& a, int32_t type) { return window(a) ? taser_window_grad_bytes(a) : plan(a, type).bytes; }
 
 extern "C" int taser_cross_attention_grad(const taser_attention* arg, const void* out, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, void* work,
                                           uint64_t work_size, void* hip_stream) {
@@ -717,7 +739,7 @@ extern "C" int taser_cross_attention_grad(const taser_attention* arg, const void
     if (rows && (!out || !stats || !dout || !dq)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null output, statistics or gradient of the queries' side");
     if (states && (!dk || !dv)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null gradient of the states");
     if (a.table && !dtable) return taser_fail(TASER_E_ARG, "cross_attention_grad: null gradient of the bias table");
-    const Plan p = plan(a);
+    const Plan p = plan(a, arg->type);
     const uint64_t need = taser_attention_grad_bytes(a, arg->type);
     if (need > work_size)
         return taser_fail(TASER_E_RANGE, "cross_attention_grad: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)need);

@@ -1,5 +1,5 @@
-// Attention over windows: at most 64 states and four rows (queries and heads that share a key head) an item, thousands of items. It
-// is bound by memory: an item's keys and values are read once, all of them on their way before the first is used.
+// Attention over windows: at most 64 states and 32 rows (queries and heads that share a key head) an item, thousands of items. An
+// item's keys and values are read once, all of them on their way before the first is used.
 //
 // A wavefront has an item. L lanes hold a row of the states, 16 bytes each, so 64 / L states are read at a time, in N turns; state
 // s L' + g (L' = 64 / L) is group g's in turn s. A score is a sum over a group; then lane (g, c) takes the score of turn c: each
@@ -10,6 +10,7 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWindowRows = 32;
 
 // x of the lane whose number differs in bit M (for M < 16, among lanes that agree in the bits below: they hold the same value).
 template <int M> __device__ inline float other(float x) {
@@ -107,32 +108,22 @@ template <int L, int E> struct Spread {
 template <typename T, int E> struct Chunk { T x[E]; };
 
 // A lane's 16 bytes of a row: where the row ends inside them they are its last 16 (elements of the lane before it come twice, and
-// count once, as zeros of `q`); a row shorter than 16 bytes is read element by element.
-template <typename T, int E> __device__ inline Chunk<T, E> load_chunk(const T* row, int at, int dim, bool there) {
+// count once, as zeros of `q`).
+template <typename T, int E> __device__ inline Chunk<T, E> load_chunk(const T* row, int at, bool there) {
     Chunk<T, E> c;
-    if (dim >= E) {
-        if (there) {
-            __builtin_memcpy(c.x, row + at, 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < E; ++i) c.x[i] = (T)0.f;
-        }
+    if (there) {
+        __builtin_memcpy(c.x, row + at, 16);
     } else {
-        taser_load<T, E>(row, there ? dim : 0, c.x);
+#pragma unroll
+        for (int i = 0; i < E; ++i) c.x[i] = (T)0.f;
     }
     return c;
 }
-template <typename T, int N> __device__ inline void store_values(T* row, int at, int dim, const float (&x)[N]) {
+template <typename T, int N> __device__ inline void store_values(T* to, const float (&x)[N]) {
     T y[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) y[i] = (T)x[i];
-    if (at + N <= dim) {
-        __builtin_memcpy(row + at, y, sizeof(y));
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (at + i < dim) row[at + i] = y[i];
-    }
+    __builtin_memcpy(to, y, sizeof(y));
 }
 
 __device__ inline int bucket_of(const int64_t* bounds, int64_t apart) {   // 64 bounds, those past the last INT64_MAX
@@ -144,21 +135,21 @@ __device__ inline int bucket_of(const int64_t* bounds, int64_t apart) {   // 64 
 }
 
 // What a wave knows of its item.
-template <typename T, int L, int N, int R> struct Item {
+template <typename T, int L, int N> struct Item {
     static constexpr int E = 16 / (int)sizeof(T), kGroups = 64 / L;
     int lane, group, c, at, b, hk, state;   // at: the lane's first element; state: the lane's own
     bool inside;                            // the lane holds elements
     uint64_t seen;                          // by lane: its state takes part
     const T *k, *v;
 
-    __device__ void open(const TaserAttentionArgs& a, int64_t item, int lane_) {
+    __device__ void open(const TaserAttentionArgs& a, int item, int lane_) {
         lane = lane_;
         group = lane / L;
         c = lane % L;
-        hk = (int)(item % a.kv_heads);
-        b = (int)(item / a.kv_heads);
+        b = item / a.kv_heads;
+        hk = item - b * a.kv_heads;
         inside = c * E < a.dim;
-        at = a.dim < E ? 0 : (c * E + E <= a.dim ? c * E : a.dim - E);
+        at = c * E + E <= a.dim ? c * E : a.dim - E;
         state = c * kGroups + group;
         const int32_t length = taser_length(a, b);
         seen = __ballot(c < N && state < length && (!a.mask || a.mask[b * a.mask_batch + state]));
@@ -169,13 +160,16 @@ template <typename T, int L, int N, int R> struct Item {
     __device__ bool turn_seen(int turn) const { return inside && (seen >> (group * L + turn)) & 1; }
     __device__ void load_states(const TaserAttentionArgs& a, Chunk<T, E> (&kc)[N], Chunk<T, E> (&vc)[N]) const {
 #pragma unroll
-        for (int s = 0; s < N; ++s) kc[s] = load_chunk<T, E>(k + turn_state(s) * a.k_token, at, a.dim, turn_seen(s));
+        for (int s = 0; s < N; ++s) kc[s] = load_chunk<T, E>(k + turn_state(s) * a.k_token, at, turn_seen(s));
 #pragma unroll
-        for (int s = 0; s < N; ++s) vc[s] = load_chunk<T, E>(v + turn_state(s) * a.v_token, at, a.dim, turn_seen(s));
+        for (int s = 0; s < N; ++s) vc[s] = load_chunk<T, E>(v + turn_state(s) * a.v_token, at, turn_seen(s));
     }
-    // Row r's elements, those that the lane before has too as zeros.
-    __device__ void load_row(const T* row, int dim, bool there, float (&x)[E]) const {
-        const Chunk<T, E> y = load_chunk<T, E>(row, at, dim, there && inside);
+    __device__ const T* query_row(const TaserAttentionArgs& a, int query, int g) const {
+        return (const T*)a.q + b * a.q_batch + query * a.q_token + (hk * a.group + g) * a.q_head;
+    }
+    __device__ Chunk<T, E> load_row(const T* row, bool there) const { return load_chunk<T, E>(row, at, there && inside); }
+    // A row's elements, those that the lane before has too as zeros.
+    __device__ void widen(const Chunk<T, E>& y, float (&x)[E]) const {
 #pragma unroll
         for (int i = 0; i < E; ++i) x[i] = at + i >= c * E ? (float)y.x[i] : 0.f;
     }
@@ -195,46 +189,43 @@ template <typename T, int L, int N, int R> struct Item {
     __device__ float of_turn(float x, int turn) const { return __shfl(x, (lane & ~(L - 1)) + turn); }
 };
 
-// The bias table of the whole call in LDS where it fits (it does: at most 16 heads, else it is read from memory), bounds beside it.
 __device__ inline void load_bounds(const TaserAttentionArgs& a, int64_t* bounds) {
     if (threadIdx.x < 64) bounds[threadIdx.x] = (int)threadIdx.x < a.buckets - 1 ? a.bounds[threadIdx.x] : INT64_MAX;
     __syncthreads();
 }
 
-template <typename T, int L, int N, int R>
-__global__ __launch_bounds__(256) void window_kernel(const TaserAttentionArgs a, T* out, float* stats, int64_t items) {
-    using I = Item<T, L, N, R>;
+template <typename T, int L, int N>
+__global__ __launch_bounds__(256) void window_kernel(const TaserAttentionArgs a, T* out, float* stats, int items) {
+    using I = Item<T, L, N>;
     constexpr int E = I::E, LEFT = Spread<L, E>::kLeft;
     __shared__ int64_t bounds[64];
     if (a.table) load_bounds(a, bounds);
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
     if (item >= items) return;
     I w;
     w.open(a, item, threadIdx.x & 63);
     Chunk<T, E> k[N], v[N];
     w.load_states(a, k, v);
-    float q[R][E];
-    int query[R], head[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int row = r < a.rows ? r : 0;
-        query[r] = row / a.group;
-        head[r] = w.hk * a.group + row - query[r] * a.group;
-        w.load_row((const T*)a.q + w.b * a.q_batch + query[r] * a.q_token + head[r] * a.q_head, a.dim, r < a.rows, q[r]);
-    }
     const bool mine = (w.seen >> w.lane) & 1;
     const int64_t key_pos = a.table && mine ? a.key_pos[w.b * a.key_pos_batch + w.state] : 0;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (r >= a.rows) break;
+    Chunk<T, E> next = w.load_row(w.query_row(a, 0, 0), true);
+    int64_t apart = 0;
+    for (int r = 0, query = 0, g = 0; r < a.rows; ++r) {
+        float q[E];
+        w.widen(next, q);
+        const int head = w.hk * a.group + g;
+        if (a.table && g == 0) apart = taser_apart(a.query_pos[w.b * a.query_pos_batch + query], key_pos);
+        const int64_t row = ((int64_t)w.b * a.queries + query) * a.heads + head;
+        if (++g == a.group) {
+            g = 0;
+            ++query;
+        }
+        next = w.load_row(w.query_row(a, query, g), r + 1 < a.rows);
         float s[N];
 #pragma unroll
-        for (int t = 0; t < N; ++t) s[t] = w.dot(q[r], k[t]);
+        for (int t = 0; t < N; ++t) s[t] = w.dot(q, k[t]);
         float x = w.own(s) * a.scale;
-        if (a.table) {
-            const int bucket = bucket_of(bounds, taser_apart(a.query_pos[w.b * a.query_pos_batch + query[r]], key_pos));
-            x += (float)((const T*)a.table)[(int64_t)head[r] * a.buckets + bucket];
-        }
+        if (a.table) x += (float)((const T*)a.table)[(int64_t)head * a.buckets + bucket_of(bounds, apart)];
         if (!mine) x = -INFINITY;
         const float top = wave_max(x), p = __builtin_amdgcn_exp2f((x - (top == -INFINITY ? 0.f : top)) * kLog2e), sum = group_sum<64>(p);
         float o[E];
@@ -251,13 +242,12 @@ __global__ __launch_bounds__(256) void window_kernel(const TaserAttentionArgs a,
         float left[LEFT];
 #pragma unroll
         for (int i = 0; i < LEFT; ++i) left[i] = o[i] * inverse;
-        const int64_t row = ((int64_t)w.b * a.queries + query[r]) * a.heads + head[r];
-        if (w.inside) store_values<T, LEFT>(out + row * a.dim, w.at + Spread<L, E>::first(w.lane), a.dim, left);
+        if (w.inside) store_values<T, LEFT>(out + row * a.dim + w.at + Spread<L, E>::first(w.lane), left);
         if (!stats) continue;
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
             for (int i = 0; i < LEFT; ++i) left[i] -= (float)(T)left[i];
-            if (w.inside) store_values<T, LEFT>(taser_rest<T>(stats, row, a.stat_floats), w.at + Spread<L, E>::first(w.lane), a.dim, left);
+            if (w.inside) store_values<T, LEFT>(taser_rest<T>(stats, row, a.stat_floats) + w.at + Spread<L, E>::first(w.lane), left);
         }
         if (w.lane == 0) {
             stats[row * a.stat_floats] = top;
@@ -267,134 +257,145 @@ __global__ __launch_bounds__(256) void window_kernel(const TaserAttentionArgs a,
 }
 
 // A wave takes every waves-th item (their number is a multiple of the key heads': a wave's items have one) and keeps the table's
-// gradient of its R rows, lane u bucket u.
-template <typename T, int L, int N, int R>
-__global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionArgs a, const T* dout, const float* stats, T* dq, T* dk, T* dv, float* part_table, int64_t items, int64_t waves) {
-    using I = Item<T, L, N, R>;
+// gradient, lane u bucket u: in a register where its rows are one (ONE), else in LDS.
+template <typename T, int L, int N, bool ONE>
+__global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionArgs a, const T* dout, const float* stats, T* dq, T* dk, T* dv, float* part_table, int items, int waves) {
+    using I = Item<T, L, N>;
     constexpr int E = I::E, LEFT = Spread<L, E>::kLeft;
     __shared__ int64_t bounds[64];
+    __shared__ float table_sums[ONE ? 1 : 4][ONE ? 1 : kWindowRows][ONE ? 1 : 64];
+    // Sums of dk and dv for all states stay in registers where there is room; else weights and dx wait in LDS until all rows have theirs.
+    constexpr bool LATER = !ONE && N >= 16;
+    __shared__ float2 waiting[LATER ? 4 : 1][LATER ? kWindowRows : 1][LATER ? 64 : 1];
     if (a.table) load_bounds(a, bounds);
-    const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), slot = ONE ? 0 : threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (wave >= waves) return;
-    float table_sums[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) table_sums[r] = 0.f;
-    for (int64_t item = wave; item < items; item += waves) {
+    float table_sum = 0.f;
+    if (!ONE && a.table)
+        for (int r = 0; r < a.rows; ++r) table_sums[slot][r][lane] = 0.f;
+    for (int item = wave; item < items; item += waves) {
         I w;
-        w.open(a, item, threadIdx.x & 63);
+        w.open(a, item, lane);
         Chunk<T, E> k[N], v[N];
         w.load_states(a, k, v);
-        float q[R][E], y[R][E], p[R], dx[R];
-        int64_t row[R];
         const bool mine = (w.seen >> w.lane) & 1;
         const int64_t key_pos = a.table && mine ? a.key_pos[w.b * a.key_pos_batch + w.state] : 0;
-        int query[R], head[R];
+        constexpr int HELD = LATER ? 1 : N;
+        float one[HELD][E], two[HELD][E];   // dk, dv
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int at = r < a.rows ? r : 0;
-            query[r] = at / a.group;
-            head[r] = w.hk * a.group + at - query[r] * a.group;
-            row[r] = ((int64_t)w.b * a.queries + query[r]) * a.heads + head[r];
-            w.load_row((const T*)a.q + w.b * a.q_batch + query[r] * a.q_token + head[r] * a.q_head, a.dim, r < a.rows, q[r]);
-            w.load_row(dout + row[r] * a.dim, a.dim, r < a.rows, y[r]);
-        }
+        for (int t = 0; t < HELD; ++t)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            p[r] = dx[r] = 0.f;
-            if (r >= a.rows) continue;
+            for (int i = 0; i < E; ++i) one[t][i] = two[t][i] = 0.f;
+        const int64_t row0 = (int64_t)w.b * a.queries * a.heads + w.hk * a.group;
+        Chunk<T, E> next_q = w.load_row(w.query_row(a, 0, 0), true), next_y = w.load_row(dout + row0 * a.dim, true);
+        int bucket = 0;
+        for (int r = 0, query = 0, g = 0; r < (ONE ? 1 : a.rows); ++r) {
+            float q[E], y[E];
+            w.widen(next_q, q);
+            w.widen(next_y, y);
+            const int head = w.hk * a.group + g;
+            if (a.table && g == 0) bucket = bucket_of(bounds, taser_apart(a.query_pos[w.b * a.query_pos_batch + query], key_pos));
+            const int64_t row = row0 + (int64_t)query * a.heads + g;
+            const float top = stats[row * a.stat_floats], sum = stats[row * a.stat_floats + 1];
+            if (!ONE) {
+                if (++g == a.group) {
+                    g = 0;
+                    ++query;
+                }
+                next_q = w.load_row(w.query_row(a, query, g), r + 1 < a.rows);
+                next_y = w.load_row(dout + (row0 + (int64_t)query * a.heads + g) * a.dim, r + 1 < a.rows);
+            }
             float s[N], d[N];
 #pragma unroll
             for (int t = 0; t < N; ++t) {
-                s[t] = w.dot(q[r], k[t]);
-                d[t] = w.dot(y[r], v[t]);
+                s[t] = w.dot(q, k[t]);
+                d[t] = w.dot(y, v[t]);
             }
             float x = w.own(s) * a.scale;
             const float dp = w.own(d);
-            int bucket = 0;
-            if (a.table) {
-                bucket = bucket_of(bounds, taser_apart(a.query_pos[w.b * a.query_pos_batch + query[r]], key_pos));
-                x += (float)((const T*)a.table)[(int64_t)head[r] * a.buckets + bucket];
-            }
-            const float top = stats[row[r] * a.stat_floats], sum = stats[row[r] * a.stat_floats + 1];
-            p[r] = mine && sum != 0.f ? __builtin_amdgcn_exp2f((x - top) * kLog2e) / sum : 0.f;
-            const float t = group_sum<64>(mine ? p[r] * dp : 0.f);
-            dx[r] = mine ? p[r] * (dp - t) : 0.f;
-            if (a.table) {
+            if (a.table) x += (float)((const T*)a.table)[(int64_t)head * a.buckets + bucket];
+            const float p = mine && sum != 0.f ? __builtin_amdgcn_exp2f((x - top) * kLog2e) / sum : 0.f;
+            const float t = group_sum<64>(mine ? p * dp : 0.f);
+            const float dx = mine ? p * (dp - t) : 0.f;
+            if (a.table) {   // a lane a bucket: the states' dx pass by in their order
+                float add = 0.f;
                 for (uint64_t left = w.seen; left; left &= left - 1) {
                     const int l = __builtin_ctzll(left);
-                    const float one = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, dx[r]), l));
-                    table_sums[r] += __builtin_amdgcn_readlane(bucket, l) == w.lane ? one : 0.f;
+                    const float value = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, dx), l));
+                    add += __builtin_amdgcn_readlane(bucket, l) == lane ? value : 0.f;
+                }
+                if (ONE) table_sum += add;
+                else table_sums[slot][r][lane] += add;
+            }
+            float sums[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) sums[i] = 0.f;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const float f = w.of_turn(dx, n) * a.scale;
+#pragma unroll
+                for (int i = 0; i < E; ++i) sums[i] = fmaf(f, (float)k[n].x[i], sums[i]);
+                if constexpr (!LATER) {
+                    const float h = w.of_turn(p, n);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        one[n][i] = fmaf(f, q[i], one[n][i]);
+                        two[n][i] = fmaf(h, y[i], two[n][i]);
+                    }
                 }
             }
-        }
-        float sums[R][E];
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int i = 0; i < E; ++i) sums[r][i] = 0.f;
-#pragma unroll
-        for (int t = 0; t < N; ++t) {
-            float one[E], two[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) one[i] = two[i] = 0.f;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float g = w.of_turn(dx[r], t) * a.scale, f = w.of_turn(p[r], t);
-#pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    one[i] = fmaf(g, q[r][i], one[i]);
-                    two[i] = fmaf(f, y[r][i], two[i]);
-                    sums[r][i] = fmaf(g, (float)k[t].x[i], sums[r][i]);
-                }
-            }
-            // A lane whose 16 bytes reach back into the lane's before has zeros there: it writes its own elements.
-            if (w.inside && w.turn_state(t) < a.keys) {
-                const int64_t to = (((int64_t)w.b * a.keys + w.turn_state(t)) * a.kv_heads + w.hk) * a.dim;
-                if (w.at == w.c * E) {
-                    store_values<T, E>(dk + to, w.at, a.dim, one);
-                    store_values<T, E>(dv + to, w.at, a.dim, two);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < E; ++i)
-                        if (w.at + i >= w.c * E) {
-                            dk[to + w.at + i] = (T)one[i];
-                            dv[to + w.at + i] = (T)two[i];
-                        }
-                }
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            Spread<L, E>::sums(sums[r], w.lane);
+            if constexpr (LATER) waiting[slot][r][lane] = float2{dx * a.scale, p};
+            Spread<L, E>::sums(sums, w.lane);
             float left[LEFT];
 #pragma unroll
-            for (int i = 0; i < LEFT; ++i) left[i] = sums[r][i];
-            if (r < a.rows && w.inside) store_values<T, LEFT>(dq + row[r] * a.dim, w.at + Spread<L, E>::first(w.lane), a.dim, left);
+            for (int i = 0; i < LEFT; ++i) left[i] = sums[i];
+            if (w.inside) store_values<T, LEFT>(dq + row * a.dim + w.at + Spread<L, E>::first(w.lane), left);
+        }
+        // A lane whose 16 bytes reach back into the lane's before has zeros there: it writes its own elements.
+        auto write = [&](int n, const float (&x)[E], const float (&y)[E]) {
+            if (!w.inside || w.turn_state(n) >= a.keys) return;
+            const int64_t to = (((int64_t)w.b * a.keys + w.turn_state(n)) * a.kv_heads + w.hk) * a.dim;
+            if (w.at == w.c * E) {
+                store_values<T, E>(dk + to + w.at, x);
+                store_values<T, E>(dv + to + w.at, y);
+            } else {
+#pragma unroll
+                for (int i = 0; i < E; ++i)
+                    if (w.at + i >= w.c * E) {
+                        dk[to + w.at + i] = (T)x[i];
+                        dv[to + w.at + i] = (T)y[i];
+                    }
+            }
+        };
+        if constexpr (LATER) {
+#pragma unroll 1
+            for (int n = 0; n * I::kGroups < a.keys; ++n) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) one[0][i] = two[0][i] = 0.f;
+                for (int r = 0, query = 0, g = 0; r < a.rows; ++r) {
+                    float q[E], y[E];
+                    w.widen(w.load_row(w.query_row(a, query, g), true), q);
+                    w.widen(w.load_row(dout + (row0 + (int64_t)query * a.heads + g) * a.dim, true), y);
+                    const float2 f = waiting[slot][r][(lane & ~(L - 1)) + n];
+#pragma unroll
+                    for (int i = 0; i < E; ++i) {
+                        one[0][i] = fmaf(f.x, q[i], one[0][i]);
+                        two[0][i] = fmaf(f.y, y[i], two[0][i]);
+                    }
+                    if (++g == a.group) {
+                        g = 0;
+                        ++query;
+                    }
+                }
+                write(n, one[0], two[0]);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) write(n, one[n], two[n]);
         }
     }
-    if (a.table) {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r < a.rows && lane < a.buckets) part_table[(wave * a.rows + r) * a.buckets + lane] = table_sums[r];
-    }
-}
-
-// dtable of one head: 16 chains of sums over the waves of its key head and their rows.
-template <typename T>
-__global__ __launch_bounds__(1024) void window_table_kernel(const float* parts, int64_t waves, int32_t kv_heads, int32_t group, int32_t rows, int32_t buckets, T* dtable) {
-    __shared__ float sums[16][64];
-    const int head = blockIdx.x, hk = head / group, g = head - hk * group, chain = threadIdx.x >> 6, u = threadIdx.x & 63;
-    float x = 0.f;
-    if (u < buckets)
-        for (int64_t i = hk + (int64_t)chain * kv_heads; i < waves; i += 16 * kv_heads)
-            for (int r = g; r < rows; r += group) x += parts[(i * rows + r) * buckets + u];
-    sums[chain][u] = x;
-    __syncthreads();
-    if ((int)threadIdx.x >= buckets) return;
-    x = 0.f;
-    for (int i = 0; i < 16; ++i) x += sums[i][u];
-    dtable[(int64_t)head * buckets + u] = (T)x;
+    if (a.table && lane < a.buckets)
+        for (int r = 0; r < a.rows; ++r) part_table[((int64_t)wave * a.rows + r) * taser_padded(a.buckets) + lane] = ONE ? table_sum : table_sums[slot][r][lane];
 }
 
 struct Call {   // one of the two kernels' arguments
@@ -407,29 +408,26 @@ struct Call {   // one of the two kernels' arguments
     hipStream_t stream;
 };
 
-template <typename T, int L, int N, int R> int run(const TaserAttentionArgs& a, const Call& c) {
-    const int64_t items = (int64_t)a.batch * a.kv_heads;
+template <typename T, int L, int N> int run(const TaserAttentionArgs& a, const Call& c) {
+    const int items = a.batch * a.kv_heads;
     if (c.dout) {
         TaserProfileSpan span(c.stream, "attention_window_grad");
-        window_grad_kernel<T, L, N, R><<<dim3((unsigned)((c.waves + 3) / 4)), 256, 0, c.stream>>>(a, (const T*)c.dout, c.stats, (T*)c.dq, (T*)c.dk, (T*)c.dv, c.part_table, items, c.waves);
+        const dim3 grid((unsigned)((c.waves + 3) / 4));
+        if (a.rows == 1) window_grad_kernel<T, L, N, true><<<grid, 256, 0, c.stream>>>(a, (const T*)c.dout, c.stats, (T*)c.dq, (T*)c.dk, (T*)c.dv, c.part_table, items, (int)c.waves);
+        else window_grad_kernel<T, L, N, false><<<grid, 256, 0, c.stream>>>(a, (const T*)c.dout, c.stats, (T*)c.dq, (T*)c.dk, (T*)c.dv, c.part_table, items, (int)c.waves);
     } else {
         TaserProfileSpan span(c.stream, "attention_window");
-        window_kernel<T, L, N, R><<<dim3((unsigned)((items + 3) / 4)), 256, 0, c.stream>>>(a, (T*)c.out, c.stats, items);
+        window_kernel<T, L, N><<<dim3((unsigned)((items + 3) / 4)), 256, 0, c.stream>>>(a, (T*)c.out, c.stats, items);
     }
     TASER_HIP_TRY(hipGetLastError());
     return TASER_OK;
 }
-template <typename T, int L, int N> int run_rows(const TaserAttentionArgs& a, const Call& c) {
-    if (a.rows <= 1) return run<T, L, N, 1>(a, c);
-    if (a.rows <= 2) return run<T, L, N, 2>(a, c);
-    return run<T, L, N, 4>(a, c);
-}
 // Lanes of a row as few as hold it, turns as few as the states need, out of three.
 template <typename T, int L> int run_turns(const TaserAttentionArgs& a, const Call& c) {
     const int turns = (a.keys + 64 / L - 1) / (64 / L);
-    if (turns <= L / 4) return run_rows<T, L, L / 4>(a, c);
-    if (turns <= L / 2) return run_rows<T, L, L / 2>(a, c);
-    return run_rows<T, L, L>(a, c);
+    if (turns <= L / 4) return run<T, L, L / 4>(a, c);
+    if (turns <= L / 2) return run<T, L, L / 2>(a, c);
+    return run<T, L, L>(a, c);
 }
 template <typename T> int run_typed(const TaserAttentionArgs& a, const Call& c) {
     constexpr int E = 16 / (int)sizeof(T);
@@ -454,7 +452,8 @@ int64_t grad_waves(const TaserAttentionArgs& a) {
 
 }  // namespace
 
-bool taser_window_fits(const TaserAttentionArgs& a) { return a.keys >= 1 && a.keys <= 64 && a.rows <= 4; }
+// (a row of at least 16 bytes)
+bool taser_window_fits(const TaserAttentionArgs& a) { return a.keys >= 1 && a.keys <= 64 && a.rows <= kWindowRows && a.dim >= 8 && (int64_t)a.batch * a.kv_heads < INT32_MAX / 2; }
 
 int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out, float* stats, hipStream_t stream) {
     Call c = {};
@@ -465,7 +464,7 @@ int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out,
 }
 
 uint64_t taser_window_grad_bytes(const TaserAttentionArgs& a) {
-    return a.table ? (uint64_t)grad_waves(a) * a.rows * a.buckets * sizeof(float) : 0;
+    return a.table ? (uint64_t)grad_waves(a) * a.rows * taser_padded(a.buckets) * sizeof(float) : 0;
 }
 
 int taser_window_attention_grad(const TaserAttentionArgs& a, int32_t type, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, float* work, hipStream_t stream) {
@@ -479,12 +478,5 @@ int taser_window_attention_grad(const TaserAttentionArgs& a, int32_t type, const
     c.waves = grad_waves(a);
     c.stream = stream;
     if (const int rc = run_any(a, type, c)) return rc;
-    if (!a.table) return TASER_OK;
-    TaserProfileSpan span(stream, "attention_window_table");
-    const dim3 grid((unsigned)a.heads);
-    if (type == TASER_F32) window_table_kernel<float><<<grid, 1024, 0, stream>>>(work, c.waves, a.kv_heads, a.group, a.rows, a.buckets, (float*)dtable);
-    else if (type == TASER_F16) window_table_kernel<_Float16><<<grid, 1024, 0, stream>>>(work, c.waves, a.kv_heads, a.group, a.rows, a.buckets, (_Float16*)dtable);
-    else window_table_kernel<__bf16><<<grid, 1024, 0, stream>>>(work, c.waves, a.kv_heads, a.group, a.rows, a.buckets, (__bf16*)dtable);
-    TASER_HIP_TRY(hipGetLastError());
-    return TASER_OK;
+    return a.table ? taser_add_tables(work, c.waves / a.kv_heads, 1, a.kv_heads, a.rows, a.group, a.buckets, type, dtable, stream) : TASER_OK;
 }

@@ -426,3 +426,39 @@ def test_the_oracle_against_a_direct_softmax():
     want = torch.softmax(q @ k.t() / 3 ** 0.5, 1) @ v
     assert np.abs(_oracle(c)[0]["out"][0, :, 0] - want.numpy()).max() < 1e-14
     assert O.buckets([0, 2, 2], [5, 3], [1, 3, 4]).tolist() == [[3, 3, 1], [3, 1, 0]]
+
+
+WINDOWS = [
+    dict(B=9, Lq=1, Lk=60, H=10, Hk=2, d=128, buckets=16, times=True, lengths="any"),
+    dict(B=4, Lq=8, Lk=64, H=8, Hk=2, d=100, buckets=64, lengths=[64, 0, 63, 1]),
+    dict(B=5, Lq=2, Lk=33, H=3, Hk=3, d=72, mask=0.6),
+    dict(B=6, Lq=1, Lk=17, H=33, Hk=1, d=64, lengths="any"),
+    dict(B=3, Lq=32, Lk=16, H=2, Hk=2, d=9, buckets=3),
+    dict(B=3, Lq=1, Lk=8, H=4, Hk=4, d=7, buckets=2),
+    dict(B=700, Lq=1, Lk=5, H=9, Hk=9, d=16, buckets=4, times=True, lengths="any"),
+]
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", range(len(WINDOWS)))
+def test_windows_of_many_rows_and_heads(kind, size):
+    _check(_case(kind, seed=20 + size, **WINDOWS[size]))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_distances_in_tiles_of_many_buckets(kind):
+    """Tiles whose distances fall into several buckets: near ones, of which a table is made, and ones too far apart for it; and biases so
+    large that they are added to the scores themselves."""
+    for times in (False, True):
+        c = _case(kind, 1, 150, 200, 4, 2, 64, buckets=12, times=times)
+        if times:   # interactions of some hours, several bounds in a tile
+            table, bounds, qp, kp = c["bias"]
+            kp = qp[:, :1] - torch.sort(torch.randint(1, 10 ** 6, (1, 200), generator=torch.Generator().manual_seed(3)), descending=True).values
+            qp = qp[:, :1] + torch.arange(150)[None] * 1000
+            c["bias"] = (table, torch.arange(11) * 90_000, qp, kp)
+        _check(c)
+        c["bias"][0][:, 3] = -2.0 ** 14
+        c["bias"][0][0] = 2.0 ** 14
+        _check(c)
