@@ -205,6 +205,14 @@ __device__ inline void taser_lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// Adds to LDS and goes on: written out, as the compiler would first wait for every load that is on its way to LDS. A lane's adds keep
+// their order; taser_lds_adds_done() comes before another wave reads.
+__device__ inline void taser_lds_add(float* to, float x) {
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)to;
+    asm volatile("ds_add_f32 %0, %1" ::"v"(at), "v"(x) : "memory");
+}
+__device__ inline void taser_lds_adds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Where a lane's part of a tile lies, once for all tiles: 32 rows further on, everything is 32 rows of bytes further on.
 // Operand of the tile's rows (lane l: row l % 32), contraction over elements 16 c ..
 template <typename T, int DP> struct TaserRowsAt {
@@ -305,11 +313,11 @@ struct TaserNear {
     int last;       // its last; -1: there is no table
     __device__ TaserNear() : base(0), last(-1) {}
     // By all threads of a block, before a barrier; lane l has bound l.
-    __device__ TaserNear(int64_t bound, int buckets, uint8_t* near) : base(0), last(-1) {
+    __device__ TaserNear(int64_t bound, int buckets, uint8_t* near, int room = kTaserNear) : base(0), last(-1) {
         if (buckets < 2) return;
         base = taser_lane_value(bound, 0) - 1;
         const uint64_t span = (uint64_t)taser_lane_value(bound, buckets - 2) - (uint64_t)base;
-        if (span >= (uint64_t)kTaserNear) return;
+        if (span >= (uint64_t)room) return;
         last = (int)span;
         for (int e0 = 0; e0 <= last; e0 += blockDim.x) {
             const int e = e0 + threadIdx.x;

@@ -42,14 +42,6 @@ __global__ __launch_bounds__(256) void attention_grad_rows_kernel(const T* out, 
     info[row] = w;
 }
 
-// Adds to LDS and goes on: written out, as the compiler would first wait for every load that is on its way to LDS. A lane's adds keep
-// their order; lds_adds_done() comes before another wave reads.
-__device__ inline void lds_add(float* to, float x) {
-    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)to;
-    asm volatile("ds_add_f32 %0, %1" ::"v"(at), "v"(x) : "memory");
-}
-__device__ inline void lds_adds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
 // ---- dq, dtable -----------------------------------------------------------------------------------------------------------
 // A wave owns 32 rows, as in the forward pass; four waves share tiles of 32 states.
 template <typename T, int DP, bool BIAS>
@@ -212,7 +204,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
                     for (int side = 0; side < 2; ++side)
                         if (half == side)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) lds_add(&my_sums[bucket[i]][lane & 31], s[4 * j + i]);
+                            for (int i = 0; i < 4; ++i) taser_lds_add(&my_sums[bucket[i]][lane & 31], s[4 * j + i]);
                 }
             } else {
                 float x = 0.f;
@@ -269,7 +261,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
     }
 
     if constexpr (BIAS) {
-        lds_adds_done();
+        taser_lds_adds_done();
         __syncthreads();
         float* to = part_table + item * (a.group * taser_padded(a.buckets));
         const int rows = a.rows - row_tile * 128 < 128 ? a.rows - row_tile * 128 : 128;

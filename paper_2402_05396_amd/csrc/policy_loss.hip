@@ -90,29 +90,64 @@ __device__ inline void join(float& top, float& sum, float other_top, float other
     top = best;
 }
 
-// Any row: a block goes over it twice.
-template <typename T>
-__global__ __launch_bounds__(1024) void policy_row_kernel(const Batch p, const T* logits, float* loss, float* logp_out, T* grad) {
+// Any row, a block each. Where a row fits the block's registers (HELD pieces of 16 bytes a thread) it is read once; else what is past them
+// is read again for the gradient.
+template <typename T, int THREADS, int HELD>
+__global__ __launch_bounds__(THREADS, (HELD <= 4 ? 8 : 4)) void policy_row_kernel(const Batch p, const T* logits, float* loss, float* logp_out, T* grad) {
     constexpr int EACH = 16 / sizeof(T);
+    struct Piece { T x[EACH]; };
     __shared__ float tops[16], sums[16], slopes[TASER_MAX_PICKS];
     __shared__ int places[TASER_MAX_PICKS];
     __shared__ float whole;
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = taking_part(p, row), waves = blockDim.x >> 6;
+    const int64_t step = (int64_t)blockDim.x * EACH;
     const T* from = logits + row * p.stride;
-    float top = -INFINITY, sum = 0.f;
-    for (int64_t c = threadIdx.x * EACH; c < n; c += blockDim.x * EACH) {
-        T x[EACH];
-        const int m = n - c < EACH ? (int)(n - c) : EACH;
-        taser_load<T, EACH>(from + c, m, x);
-        float best = -INFINITY, part = 0.f;
+    // what the loss needs of the row's actions is on its way too
+    const int64_t at = row * p.picks + lane;
+    const int action = wave == 0 && lane < p.picks ? p.actions[at] : -1;
+    const bool real = action >= 0 && action < n;
+    const float chosen = real ? (float)from[action] : 0.f;
+    auto load = [&](int64_t c, Piece& x) {   // places past the row's: minus infinity
+        if (c + EACH <= n) {
+            __builtin_memcpy(x.x, from + c, 16);
+        } else {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) best = i < m ? fmaxf(best, (float)x[i]) : best;
+            for (int i = 0; i < EACH; ++i) x.x[i] = c + i < n ? from[c + i] : (T)-INFINITY;
+        }
+    };
+    float top = -INFINITY, sum = 0.f;
+    auto take = [&](const Piece& x) {
+        float best = (float)x.x[0];
+#pragma unroll
+        for (int i = 1; i < EACH; ++i) best = fmaxf(best, (float)x.x[i]);
+        const float now = fmaxf(top, best), base = now == -INFINITY ? 0.f : now;
+        float part = 0.f;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) part += __builtin_amdgcn_exp2f(((float)x.x[i] - base) * kLog2e);
+        sum = (now == top ? sum : sum * __builtin_amdgcn_exp2f((top - base) * kLog2e)) + part;
+        top = now;
+    };
+    Piece held[HELD];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) load(h * step + threadIdx.x * EACH, held[h]);
+    {   // all held pieces against their common maximum
+        float best = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) best = fmaxf(best, (float)held[h].x[i]);
+        top = best;
         const float base = best == -INFINITY ? 0.f : best;
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) part += i < m ? __builtin_amdgcn_exp2f(((float)x[i] - base) * kLog2e) : 0.f;
-        if (best == -INFINITY) sum += part;   // 0, or NaN
-        else join(top, sum, best, part);
+        for (int h = 0; h < HELD; ++h)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) sum += __builtin_amdgcn_exp2f(((float)held[h].x[i] - base) * kLog2e);
+    }
+    for (int64_t c = HELD * step + threadIdx.x * EACH; c < n; c += step) {
+        Piece x;
+        load(c, x);
+        take(x);
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
@@ -129,12 +164,9 @@ __global__ __launch_bounds__(1024) void policy_row_kernel(const Batch p, const T
     for (int w = 1; w < waves; ++w) join(top, sum, tops[w], sums[w]);
     if (top == -INFINITY) top = 0.f;
     if (wave == 0) {
-        const int64_t at = row * p.picks + lane;
-        const int action = lane < p.picks ? p.actions[at] : -1;
-        const bool real = action >= 0 && action < n;
         float l = 0.f, mine = 0.f, slope = 0.f;
         if (real) {
-            l = ((float)from[action] - top) - logf(sum);
+            l = (chosen - top) - logf(sum);
             action_loss(p, at, l, &mine, &slope);
         }
         if (lane < p.picks) {
@@ -152,26 +184,32 @@ __global__ __launch_bounds__(1024) void policy_row_kernel(const Batch p, const T
     __syncthreads();
     const float by = sum > 0.f ? -whole / sum : -whole;
     T* to = grad + row * p.width;
-    for (int64_t c = threadIdx.x * EACH; c < p.width; c += blockDim.x * EACH) {
-        T x[EACH], y[EACH];
-        const int m = n - c < EACH ? (n > c ? (int)(n - c) : 0) : EACH, writes = p.width - c < EACH ? (int)(p.width - c) : EACH;
-        taser_load<T, EACH>(from + c, m, x);
+    auto give = [&](int64_t c, const Piece& x) {
+        Piece y;
+        if (c + EACH <= n) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) y[i] = (T)(i < m ? __builtin_amdgcn_exp2f(((float)x[i] - top) * kLog2e) * by : 0.f);
-        if (writes == EACH) {
-            __builtin_memcpy(to + c, y, sizeof(y));
-        } else {
-#pragma unroll
+            for (int i = 0; i < EACH; ++i) y.x[i] = (T)(__builtin_amdgcn_exp2f(((float)x.x[i] - top) * kLog2e) * by);
+            typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
+            loose u;
+            __builtin_memcpy(&u, y.x, 16);
+            __builtin_nontemporal_store(u, (loose*)(to + c));
+        } else if (c < p.width) {
             for (int i = 0; i < EACH; ++i)
-                if (i < writes) to[c + i] = y[i];
+                if (c + i < p.width) to[c + i] = (T)(c + i < n ? __builtin_amdgcn_exp2f(((float)x.x[i] - top) * kLog2e) * by : 0.f);
         }
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) give(h * step + threadIdx.x * EACH, held[h]);
+    for (int64_t c = HELD * step + threadIdx.x * EACH; c < p.width; c += step) {
+        Piece x;
+        load(c, x);
+        give(c, x);
     }
     __syncthreads();   // the row is written: its actions' places are now put right
-    if ((int)threadIdx.x < p.picks && places[threadIdx.x] >= 0) {
-        const int a = places[threadIdx.x];
-        float g = __builtin_amdgcn_exp2f(((float)from[a] - top) * kLog2e) * by;
-        for (int j = 0; j < p.picks; ++j) g += places[j] == a ? slopes[j] : 0.f;
-        to[a] = (T)g;
+    if (wave == 0 && real) {
+        float g = __builtin_amdgcn_exp2f((chosen - top) * kLog2e) * by;
+        for (int j = 0; j < p.picks; ++j) g += places[j] == action ? slopes[j] : 0.f;
+        to[action] = (T)g;
     }
 }
 
@@ -186,8 +224,13 @@ template <typename T> int launch(const Batch& p, const void* logits, float* loss
         else if (g == 32) policy_window_kernel<T, 32><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
         else policy_window_kernel<T, 64><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
     } else {
-        const int threads = p.width <= 4096 ? 256 : 1024;
-        policy_row_kernel<T><<<dim3((unsigned)p.rows), threads, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
+        // Short rows are held by as few threads as it takes. Of longer ones as much as leaves registers for two blocks a compute unit, one writing
+        // while the other reads: 64 001 bf16 logits 0.28 ms for 4 096 rows, 0.30 with the whole row held by one block.
+        const int64_t pieces = (p.width + 16 / (int64_t)sizeof(T) - 1) / (16 / (int64_t)sizeof(T));
+        const dim3 grid((unsigned)p.rows);
+        if (pieces <= 256) policy_row_kernel<T, 256, 1><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
+        else if (pieces <= 1024) policy_row_kernel<T, 256, 4><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
+        else policy_row_kernel<T, 1024, (sizeof(T) == 2 ? 4 : 8)><<<grid, 1024, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
     }
     TASER_HIP_TRY(hipGetLastError());
     return TASER_OK;

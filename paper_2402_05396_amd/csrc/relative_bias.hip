@@ -3,15 +3,6 @@
 
 namespace {
 
-// How many bounds are at most `apart`: a search over 64 of them (those past the last are INT64_MAX).
-__device__ inline int bucket_of(const int64_t* bounds, int64_t apart) {
-    int at = 0;
-#pragma unroll
-    for (int step = 32; step; step >>= 1)
-        if (bounds[at + step - 1] <= apart) at += step;
-    return at;
-}
-
 struct Distances {
     int32_t heads, buckets, queries, keys;
     int64_t batch;
@@ -19,106 +10,214 @@ struct Distances {
     int64_t query_pos_batch, key_pos_batch;
 };
 
-__device__ inline void load_bounds(const Distances& d, int64_t* bounds) {
-    if (threadIdx.x < 64) bounds[threadIdx.x] = (int)threadIdx.x < d.buckets - 1 ? d.bounds[threadIdx.x] : INT64_MAX;
+// A wave's neighboring states, EACH a lane: their positions and the range of those.
+template <int EACH> struct States {
+    int64_t pos[EACH], least, most;
+    int n;
+    __device__ States(const int64_t* from, int state, int keys) {
+        n = keys - state < EACH ? keys - state : EACH;
+        int64_t low = INT64_MAX, high = INT64_MAX;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            pos[i] = i < n ? from[state + i] : 0;
+            if (i < n) {
+                low = taser_min64(low, pos[i]);
+                high = taser_min64(high, -pos[i]);
+            }
+        }
+        const int64_t x = taser_two_mins(low, high);
+        least = taser_lane_value(x, 0);
+        most = -taser_lane_value(x, 32);
+    }
+};
+constexpr int kNear = 1024;   // distances of the table of buckets
+// What all kernels here have in LDS.
+struct Near {
+    int64_t bound;
+    TaserNear map;
+};
+__device__ inline Near begin(const Distances& d, uint8_t* near, int lane) {
+    Near w;
+    w.bound = lane < d.buckets - 1 ? d.bounds[lane] : INT64_MAX;
+    w.map = TaserNear(w.bound, d.buckets, near, kNear);
+    return w;
+}
+// Buckets of a lane's states.
+template <int EACH> __device__ inline void find(const Distances& d, const Near& w, const uint8_t* near, const States<EACH>& s, int64_t from, int low, int high, int (&bucket)[EACH]) {
+    const TaserBuckets of(w.map, near, w.bound, low, high, taser_apart(from, s.most), taser_apart(from, s.least));
+#pragma unroll
+    for (int j = 0; j < EACH / 4; ++j) {
+        int four[4];
+        of.template find<false>(four, from, s.pos + 4 * j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bucket[4 * j + i] = four[i];
+    }
 }
 
-// A thread has EACH neighboring states of one query: their buckets once, for all heads of its share.
+// A wave has 64 EACH neighboring states of one query, for all heads of its share: their buckets are found once. Bound by the stores, which
+// nothing reads again soon: they go past the caches.
 template <typename T, int EACH>
 __global__ __launch_bounds__(256) void relative_bias_kernel(const Distances d, const T* table, T* bias, int heads_each) {
-    __shared__ int64_t bounds[64];
+    __shared__ uint8_t near[kNear];
     extern __shared__ float values[];   // [heads of this block][buckets]
-    const int head0 = blockIdx.y * heads_each, heads = d.heads - head0 < heads_each ? d.heads - head0 : heads_each;
-    load_bounds(d, bounds);
+    const int lane = threadIdx.x & 63, head0 = blockIdx.y * heads_each, heads = d.heads - head0 < heads_each ? d.heads - head0 : heads_each;
+    const Near w = begin(d, near, lane);
     for (int i = threadIdx.x; i < heads * d.buckets; i += 256) values[i] = (float)table[(int64_t)head0 * d.buckets + i];
     __syncthreads();
-    const int64_t pieces = (d.keys + EACH - 1) / EACH, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t pieces = (d.keys + 64 * EACH - 1) / (64 * EACH), at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= d.batch * d.queries * pieces) return;
     const int64_t row = at / pieces, b = row / d.queries, query = row - b * d.queries;
-    const int state = (int)(at - row * pieces) * EACH, n = d.keys - state < EACH ? d.keys - state : EACH;
+    const int state = (int)(at - row * pieces) * 64 * EACH + lane * EACH;
     const int64_t from = d.query_pos[b * d.query_pos_batch + query];
-    const int64_t* key_pos = d.key_pos + b * d.key_pos_batch + state;
+    const States<EACH> s(d.key_pos + b * d.key_pos_batch, state, d.keys);
+    const int low = taser_uniform_bucket(w.bound, taser_apart(from, s.most), d.buckets), high = taser_uniform_bucket(w.bound, taser_apart(from, s.least), d.buckets);
     int bucket[EACH];
+    if (low == high) {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) bucket[i] = bucket_of(bounds, taser_apart(from, key_pos[i < n ? i : 0]));
+        for (int i = 0; i < EACH; ++i) bucket[i] = low;
+    } else {
+        find<EACH>(d, w, near, s, from, low, high, bucket);
+    }
+    if (s.n <= 0) return;
     T* to = bias + ((b * d.heads + head0) * d.queries + query) * d.keys + state;
     for (int h = 0; h < heads; ++h, to += (int64_t)d.queries * d.keys) {
         T x[EACH];
+        if (low == high) {
+            const T one = (T)values[h * d.buckets + low];
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) x[i] = (T)values[h * d.buckets + bucket[i]];
-        if (n == EACH) {
-            __builtin_memcpy(to, x, sizeof(x));
+            for (int i = 0; i < EACH; ++i) x[i] = one;
+        } else {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) x[i] = (T)values[h * d.buckets + bucket[i]];
+        }
+        if (s.n == EACH) {
+            typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
+            loose u;
+            __builtin_memcpy(&u, x, 16);
+            __builtin_nontemporal_store(u, (loose*)to);
         } else {
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
-                if (i < n) to[i] = x[i];
+                if (i < s.n) to[i] = x[i];
         }
     }
 }
 
-// A block has one head and a share of the (batch entry, query) rows, a wave every fourth of them. A lane adds to a column of sums
-// of its own in LDS, so that nothing is added by two lanes and the order of the sums is fixed.
+// A block has one head and a share of the groups of ROWS queries of a batch entry, a wave every fourth of them; it goes over the states 64 EACH
+// at a time, the gradients of the next ones of all ROWS queries on their way meanwhile. A stretch of states mostly has one bucket, or at
+// least each lane's states do: a lane's sum stays in a register until its bucket changes, then goes to LDS, in a column
+// that it shares with one other lane, one after the other: the order of the sums is fixed.
+template <typename T> constexpr int kRows = sizeof(T) == 4 ? 8 : 4;   // (bf16: 0.134 ms with 4 rows for what takes 0.190 with 8; float32: 0.165 with 8, 0.176 with 4)
 template <typename T, int EACH>
 __global__ __launch_bounds__(256) void relative_bias_grad_kernel(const Distances d, const T* dbias, int64_t batch_stride, int64_t head_stride, int64_t query_stride, float* parts) {
-    __shared__ int64_t bounds[65];   // bounds[0] is below all
-    extern __shared__ float sums[];   // [4 waves][buckets][64 lanes]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, head = blockIdx.y;
-    float* mine = sums + wave * d.buckets * 64 + lane;
-    load_bounds(d, bounds + 1);
-    if (threadIdx.x == 0) bounds[0] = INT64_MIN;
-    for (int u = 0; u < d.buckets; ++u) mine[64 * u] = 0.f;
+    constexpr int ROWS = kRows<T>;
+    struct Piece { T x[EACH]; };
+    __shared__ uint8_t near[kNear];
+    __shared__ int64_t bounds[64];
+    extern __shared__ float sums[];   // [4 waves][buckets][32]: lanes l and l + 32 add to column l one after the other
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
+    float* mine = sums + wave * d.buckets * 32 + (lane & 31);
+    auto add = [&](int bucket, float x) {
+        if (lane < 32) taser_lds_add(mine + 32 * bucket, x);
+        if (lane >= 32) taser_lds_add(mine + 32 * bucket, x);
+    };
+    const Near w = begin(d, near, lane);
+    if (wave == 0) bounds[lane] = w.bound;
+    for (int u = 0; u < d.buckets; ++u) mine[32 * u] = 0.f;
     __syncthreads();
-    const int64_t rows = d.batch * d.queries, step = (int64_t)gridDim.x * 4;
-    for (int64_t row = (int64_t)blockIdx.x * 4 + wave; row < rows; row += step) {
-        const int64_t b = row / d.queries, query = row - b * d.queries, from = d.query_pos[b * d.query_pos_batch + query];
-        const T* x_from = dbias + b * batch_stride + head * head_stride + query * query_stride;
-        const int64_t* key_pos = d.key_pos + b * d.key_pos_batch;
-        for (int state = lane * EACH; state < d.keys; state += 64 * EACH) {
-            const int n = d.keys - state < EACH ? d.keys - state : EACH;
-            T x[EACH];
-            taser_load<T, EACH>(x_from + state, n, x);
-            int64_t apart[EACH];
+    // The bucket of a distance of the lane's own: from the table if it reaches (the same for all lanes), else by a search.
+    auto lane_bucket = [&](int64_t apart, bool read) -> int {
+        if (read) {
+            int at = (int)((uint32_t)(uint64_t)apart - (uint32_t)(uint64_t)w.map.base);
+            at = at < 0 ? 0 : (at > w.map.last ? w.map.last : at);
+            return near[at];
+        }
+        int at = 0;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) apart[i] = taser_apart(from, key_pos[state + (i < n ? i : 0)]);
-            const int first = bucket_of(bounds + 1, apart[0]);
-            const int64_t low = bounds[first], high = bounds[first + 1];
-            bool same = true;
-            float all = 0.f;
+        for (int step = 32; step; step >>= 1)
+            if (bounds[at + step - 1] <= apart) at += step;
+        return at;
+    };
+    const int groups = (d.queries + ROWS - 1) / ROWS;
+    const int64_t units = d.batch * groups, step = (int64_t)gridDim.x * 4;
+    int running = 0;
+    float sum = 0.f;
+    for (int64_t unit = (int64_t)blockIdx.x * 4 + wave; unit < units; unit += step) {
+        const int64_t b = unit / groups;
+        const int query0 = (int)(unit - b * groups) * ROWS, rows = d.queries - query0 < ROWS ? d.queries - query0 : ROWS;
+        const T* from = dbias + b * batch_stride + head * head_stride + query0 * query_stride;
+        const int64_t *key_pos = d.key_pos + b * d.key_pos_batch, *query_pos = d.query_pos + b * d.query_pos_batch + query0;
+        auto load = [&](Piece (&x)[ROWS], int state) {
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                same = same && low <= apart[i] && (apart[i] < high);
-                all += (float)x[i];
+            for (int r = 0; r < ROWS; ++r) {
+                if (r < rows && state + EACH <= d.keys) {
+                    __builtin_memcpy(x[r].x, from + r * query_stride + state, 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) x[r].x[i] = r < rows && state + i < d.keys ? from[r * query_stride + state + i] : (T)0.f;
+                }
             }
-            if (same) {
-                mine[64 * first] += all;
-            } else {
+        };
+        Piece next[ROWS];
+        load(next, lane * EACH);
+        for (int state0 = 0; state0 < d.keys; state0 += 64 * EACH) {
+            const int state = state0 + lane * EACH;
+            Piece x[ROWS];
 #pragma unroll
-                for (int i = 0; i < EACH; ++i)
-                    if (i < n) mine[64 * bucket_of(bounds + 1, apart[i])] += (float)x[i];
+            for (int r = 0; r < ROWS; ++r) x[r] = next[r];
+            const States<EACH> s(key_pos, state, d.keys);
+            if (state0 + 64 * EACH < d.keys) load(next, state + 64 * EACH);
+            int64_t least = s.pos[0], most = s.pos[0];   // of the lane's states
+#pragma unroll
+            for (int i = 1; i < EACH; ++i)
+                if (i < s.n) {
+                    least = taser_min64(least, s.pos[i]);
+                    most = -taser_min64(-most, -s.pos[i]);
+                }
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                if (r >= rows) continue;
+                const int64_t at = query_pos[r];
+                float all = 0.f;
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) all += (float)x[r].x[i];   // (past the last state: 0)
+                int low = taser_uniform_bucket(w.bound, taser_apart(at, s.most), d.buckets), high = taser_uniform_bucket(w.bound, taser_apart(at, s.least), d.buckets);
+                if (low != high) {
+                    const int64_t reach = 1 << 30;
+                    const bool read = w.map.last >= 0 && taser_apart(at, s.most) > w.map.base - reach && taser_apart(at, s.least) < w.map.base + reach;
+                    low = lane_bucket(taser_apart(at, most), read);
+                    high = lane_bucket(taser_apart(at, least), read);
+                    if (__any(low != high)) {
+                        if (low != high) {
+#pragma unroll
+                            for (int i = 0; i < EACH; ++i)
+                                if (i < s.n) add(lane_bucket(taser_apart(at, s.pos[i]), read), (float)x[r].x[i]);
+                            all = 0.f;
+                            low = running;
+                        }
+                    }
+                }
+                if (low != running) {
+                    add(running, sum);
+                    running = low;
+                    sum = 0.f;
+                }
+                sum += all;
             }
         }
     }
+    add(running, sum);
+    taser_lds_adds_done();
     __syncthreads();
     if ((int)threadIdx.x < d.buckets) {   // a lane a bucket, each starting at a column of its own
         float total = 0.f;
-        for (int w = 0; w < 4; ++w) {
-            float x = 0.f;
-            for (int l = 0; l < 64; ++l) x += sums[(w * d.buckets + threadIdx.x) * 64 + ((l + threadIdx.x) & 63)];
-            total += x;
+        for (int v = 0; v < 4; ++v) {
+            float y = 0.f;
+            for (int l = 0; l < 32; ++l) y += sums[(v * d.buckets + threadIdx.x) * 32 + ((l + threadIdx.x) & 31)];
+            total += y;
         }
-        parts[((int64_t)head * gridDim.x + blockIdx.x) * d.buckets + threadIdx.x] = total;
+        parts[((int64_t)blockIdx.x * d.heads + head) * taser_padded(d.buckets) + threadIdx.x] = total;
     }
-}
-
-template <typename T> __global__ __launch_bounds__(256) void relative_bias_grad_add_kernel(const float* parts, int32_t n, int32_t buckets, T* dtable) {
-    __shared__ float sums[4][64];
-    const int chain = threadIdx.x >> 6, u = threadIdx.x & 63;
-    float x = 0.f;
-    if (u < buckets)
-        for (int i = chain; i < n; i += 4) x += parts[((int64_t)blockIdx.x * n + i) * buckets + u];
-    sums[chain][u] = x;
-    __syncthreads();
-    if ((int)threadIdx.x < buckets) dtable[(int64_t)blockIdx.x * buckets + u] = (T)((sums[0][u] + sums[1][u]) + (sums[2][u] + sums[3][u]));
 }
 
 int check(const taser_distances* p, const char* what, Distances* d) {
@@ -136,38 +235,36 @@ int check(const taser_distances* p, const char* what, Distances* d) {
     return TASER_OK;
 }
 
-// Blocks of a head: about 1024 in all, none without a row for each wave.
-int blocks_of_head(const Distances& d) {
-    const int64_t most = (d.batch * d.queries + 3) / 4, wanted = (1024 + d.heads - 1) / d.heads;
+// Blocks of a head: two for each compute unit that its LDS leaves room for, none without a group of queries for each wave.
+int blocks_of_head(const Distances& d, int rows) {
+    const int64_t groups = d.batch * ((d.queries + rows - 1) / rows), most = (groups + 3) / 4, wanted = (1024 + d.heads - 1) / d.heads;
     const int64_t n = most < wanted ? most : wanted;
     return n < 1 ? 1 : (int)n;
 }
+uint64_t work_bytes(const Distances& d, int32_t type) { return (uint64_t)d.heads * blocks_of_head(d, type == TASER_F32 ? kRows<float> : kRows<__bf16>) * taser_padded(d.buckets) * sizeof(float); }
 
 template <typename T> int launch(const Distances& d, const void* table, void* bias, hipStream_t stream) {
     constexpr int EACH = 16 / sizeof(T);
     const int heads_each = d.heads * d.buckets <= 8192 ? d.heads : 8192 / d.buckets;
-    const int64_t threads = d.batch * d.queries * ((d.keys + EACH - 1) / EACH);
+    const int64_t waves = d.batch * d.queries * ((d.keys + 64 * EACH - 1) / (64 * EACH));
     TaserProfileSpan span(stream, "relative_bias");
-    relative_bias_kernel<T, EACH><<<dim3((unsigned)((threads + 255) / 256), (unsigned)((d.heads + heads_each - 1) / heads_each)), 256, sizeof(float) * heads_each * d.buckets, stream>>>(
+    relative_bias_kernel<T, EACH><<<dim3((unsigned)((waves + 3) / 4), (unsigned)((d.heads + heads_each - 1) / heads_each)), 256, sizeof(float) * heads_each * d.buckets, stream>>>(
         d, (const T*)table, (T*)bias, heads_each);
     TASER_HIP_TRY(hipGetLastError());
     return TASER_OK;
 }
 
-template <typename T> int launch_grad(const Distances& d, const void* dbias, const int64_t* strides, void* dtable, float* work, hipStream_t stream) {
+template <typename T> int launch_grad(const Distances& d, int32_t type, const void* dbias, const int64_t* strides, void* dtable, float* work, hipStream_t stream) {
     constexpr int EACH = 16 / sizeof(T);
-    const int blocks = blocks_of_head(d);
+    const int blocks = blocks_of_head(d, kRows<T>);
     const bool some = d.batch && d.queries && d.keys;
     if (some) {
         TaserProfileSpan span(stream, "relative_bias_grad");
-        relative_bias_grad_kernel<T, EACH><<<dim3((unsigned)blocks, (unsigned)d.heads), 256, 4 * 64 * sizeof(float) * d.buckets, stream>>>(d, (const T*)dbias, strides[0], strides[1],
+        relative_bias_grad_kernel<T, EACH><<<dim3((unsigned)blocks, (unsigned)d.heads), 256, 4 * 32 * sizeof(float) * d.buckets, stream>>>(d, (const T*)dbias, strides[0], strides[1],
                                                                                                                                     strides[2], work);
         TASER_HIP_TRY(hipGetLastError());
     }
-    TaserProfileSpan span(stream, "relative_bias_grad_add");
-    relative_bias_grad_add_kernel<T><<<dim3((unsigned)d.heads), 256, 0, stream>>>(work, some ? blocks : 0, d.buckets, (T*)dtable);
-    TASER_HIP_TRY(hipGetLastError());
-    return TASER_OK;
+    return taser_add_tables(work, some ? blocks : 0, 1, d.heads, 1, 1, d.buckets, type, dtable, stream);
 }
 
 }  // namespace
@@ -175,7 +272,7 @@ template <typename T> int launch_grad(const Distances& d, const void* dbias, con
 extern "C" int taser_relative_bias_bytes(const taser_distances* p, uint64_t* work) {
     Distances d;
     if (const int rc = check(p, "relative_bias_bytes", &d)) return rc;
-    if (work) *work = (uint64_t)d.heads * blocks_of_head(d) * d.buckets * sizeof(float);
+    if (work) *work = work_bytes(d, p->type);
     return TASER_OK;
 }
 
@@ -196,12 +293,12 @@ extern "C" int taser_relative_bias_grad(const taser_distances* p, const void* db
     if (const int rc = check(p, "relative_bias_grad", &d)) return rc;
     if (!dtable) return taser_fail(TASER_E_ARG, "relative_bias_grad: null output");
     if (d.batch && d.queries && d.keys && (!dbias || !strides)) return taser_fail(TASER_E_ARG, "relative_bias_grad: null gradient or strides");
-    const uint64_t need = (uint64_t)d.heads * blocks_of_head(d) * d.buckets * sizeof(float);
+    const uint64_t need = work_bytes(d, p->type);
     if (need > work_size) return taser_fail(TASER_E_RANGE, "relative_bias_grad: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)need);
     if (!work || (uintptr_t)work % 16) return taser_fail(TASER_E_ARG, "relative_bias_grad: null or misaligned workspace");
     hipStream_t stream = (hipStream_t)hip_stream;
     taser_clear_stale_hip_error();
-    if (p->type == TASER_F32) return launch_grad<float>(d, dbias, strides, dtable, (float*)work, stream);
-    if (p->type == TASER_F16) return launch_grad<_Float16>(d, dbias, strides, dtable, (float*)work, stream);
-    return launch_grad<__bf16>(d, dbias, strides, dtable, (float*)work, stream);
+    if (p->type == TASER_F32) return launch_grad<float>(d, p->type, dbias, strides, dtable, (float*)work, stream);
+    if (p->type == TASER_F16) return launch_grad<_Float16>(d, p->type, dbias, strides, dtable, (float*)work, stream);
+    return launch_grad<__bf16>(d, p->type, dbias, strides, dtable, (float*)work, stream);
 }
