@@ -8,7 +8,7 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kMostSplits = 128;
+constexpr int kMostSplits = 128, kFineStates = 128;
 
 // A wave owns 32 query rows (of the queries of one key head: row r is query r / group, head r % group of them), lane l row
 // l % 32 of them. Scores come out transposed, states in registers, so a row's softmax needs one exchange, with the other half of
@@ -20,8 +20,10 @@ template <typename T, int DP, bool SHARED> struct Shape {
     static constexpr int kRows = SHARED ? 32 * kWaves : 32;
 };
 
-template <typename T, int DP, bool SHARED, bool BIAS>
-__global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && sizeof(T) == 2 ? 2 : 1)) void attention_kernel(const TaserAttentionArgs a, T* out, float* stats, float* part_out,
+// FINE: the output is exact to 32 bits before it is rounded, for a gradient over few states, whose <dout, out> would have the weights'
+// roundings in it otherwise (over many states they average out).
+template <typename T, int DP, bool SHARED, bool BIAS, bool FINE>
+__global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && sizeof(T) == 2 && !(FINE && DP == 128) ? 2 : 1)) void attention_kernel(const TaserAttentionArgs a, T* out, float* stats, float* part_out,
                                                                                       float* part_stats, int64_t work) {
     using S = Shape<T, DP, SHARED>;
     constexpr int KT = S::kStates, NK = KT / 32, ND = DP / 32, NC = DP / 16;
@@ -201,15 +203,34 @@ __global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && siz
                 part += s[n][r];
             }
         sum += part;
+        // The weights are rounded to the type of the states that they multiply; their sum is of the unrounded ones. Where FINE, what the
+        // rounding took off is multiplied too.
+        if constexpr (FINE) {
 #pragma unroll
-        for (int n = 0; n < NK; ++n)
+            for (int n = 0; n < NK; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                // the weights are rounded to the type of the states that they multiply; their sum is of the unrounded ones
-                const taser_frag<T> p = taser_operand<T>(s[n], h);
+                for (int h = 0; h < 2; ++h) {
+                    const taser_frag<T> p = taser_operand<T>(s[n], h);
+                    taser_frag<T> q;
 #pragma unroll
-                for (int d = 0; d < ND; ++d) taser_mma(o[d], columns_at.operand(v, 32 * n + 16 * h, d), p);
-            }
+                    for (int i = 0; i < 8; ++i) q[i] = (T)(s[n][8 * h + i] - (float)p[i]);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const taser_frag<T> x = columns_at.operand(v, 32 * n + 16 * h, d);
+                        taser_mma(o[d], x, p);
+                        taser_mma(o[d], x, q);
+                    }
+                }
+        } else {
+#pragma unroll
+            for (int n = 0; n < NK; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const taser_frag<T> p = taser_operand<T>(s[n], h);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) taser_mma(o[d], columns_at.operand(v, 32 * n + 16 * h, d), p);
+                }
+        }
     };
 
     const int step = SHARED ? 1 : S::kWaves;
@@ -424,10 +445,18 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
     if (items > INT32_MAX / 2) return taser_fail(TASER_E_RANGE, "cross_attention: too many queries and batch entries for one launch");
     {
         TaserProfileSpan span(stream, "attention");
-        if (a.table)
-            attention_kernel<T, DP, SHARED, true><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
-        else
-            attention_kernel<T, DP, SHARED, false><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
+        auto run = [&](auto bias, auto fine) {
+            attention_kernel<T, DP, SHARED, decltype(bias)::value, decltype(fine)::value><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
+        };
+        const std::true_type yes;
+        const std::false_type no;
+        if (sizeof(T) == 2 && a.keys <= kFineStates) {
+            if (a.table) run(yes, std::bool_constant<sizeof(T) == 2>());
+            else run(no, std::bool_constant<sizeof(T) == 2>());
+        } else {
+            if (a.table) run(yes, no);
+            else run(no, no);
+        }
         TASER_HIP_TRY(hipGetLastError());
     }
     if (a.splits > 1) {
