@@ -107,6 +107,18 @@ template <int L, int E> struct Spread {
 
 template <typename T, int E> struct Chunk { T x[E]; };
 
+// Keeps 16-bit elements as they are across a loop's rounds: widened ahead of it they would take twice the registers, and half the
+// waves would fit.
+template <typename T, int E> __device__ inline void stay_narrow(Chunk<T, E>& c) {
+    if constexpr (sizeof(T) == 2) {
+        typedef uint32_t words __attribute__((ext_vector_type(4)));
+        words x;
+        __builtin_memcpy(&x, c.x, 16);
+        asm volatile("" : "+v"(x));
+        __builtin_memcpy(c.x, &x, 16);
+    }
+}
+
 // A lane's 16 bytes of a row: where the row ends inside them they are its last 16 (elements of the lane before it come twice, and
 // count once, as zeros of `q`).
 template <typename T, int E> __device__ inline Chunk<T, E> load_chunk(const T* row, int at, bool there) {
@@ -223,6 +235,8 @@ __global__ __launch_bounds__(256) void window_kernel(const TaserAttentionArgs a,
         next = w.load_row(w.query_row(a, query, g), r + 1 < a.rows);
         float s[N];
 #pragma unroll
+        for (int t = 0; t < N; ++t) stay_narrow(k[t]);
+#pragma unroll
         for (int t = 0; t < N; ++t) s[t] = w.dot(q, k[t]);
         float x = w.own(s) * a.scale;
         if (a.table) x += (float)((const T*)a.table)[(int64_t)head * a.buckets + bucket_of(bounds, apart)];
@@ -234,6 +248,7 @@ __global__ __launch_bounds__(256) void window_kernel(const TaserAttentionArgs a,
 #pragma unroll
         for (int t = 0; t < N; ++t) {
             const float y = w.of_turn(p, t);
+            stay_narrow(v[t]);
 #pragma unroll
             for (int i = 0; i < E; ++i) o[i] = fmaf(y, (float)v[t].x[i], o[i]);
         }
@@ -308,6 +323,8 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
             float s[N], d[N];
 #pragma unroll
             for (int t = 0; t < N; ++t) {
+                stay_narrow(k[t]);
+                stay_narrow(v[t]);
                 s[t] = w.dot(q, k[t]);
                 d[t] = w.dot(y, v[t]);
             }
@@ -333,6 +350,7 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const float f = w.of_turn(dx, n) * a.scale;
+                stay_narrow(k[n]);
 #pragma unroll
                 for (int i = 0; i < E; ++i) sums[i] = fmaf(f, (float)k[n].x[i], sums[i]);
                 if constexpr (!LATER) {
