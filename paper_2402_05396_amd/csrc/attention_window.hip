@@ -279,7 +279,10 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
     constexpr int E = I::E, LEFT = Spread<L, E>::kLeft;
     __shared__ int64_t bounds[64];
     __shared__ float table_sums[ONE ? 1 : 4][ONE ? 1 : kWindowRows][ONE ? 1 : 64];
-    // Sums of dk and dv for all states stay in registers where there is room; else weights and dx wait in LDS until all rows have theirs.
+    // Sums of dk and dv for all states stay in registers where there is room (half of the turns of a 16-bit row and fewer); else weights
+    // and dx wait in LDS until all rows have theirs, and the rows are read again for each few turns of states. At 64 states of 128 in
+    // 16 bits, two rows, 8000 windows: 385 us (one turn at a time 555, all in registers over 800, spilled); at 50 states of 64 in
+    // bfloat16, eight rows, 20000 windows: registers 843 us, waiting 915.
     constexpr bool LATER = !ONE && N >= 16;
     __shared__ float2 waiting[LATER ? 4 : 1][LATER ? kWindowRows : 1][LATER ? 64 : 1];
     if (a.table) load_bounds(a, bounds);
@@ -295,7 +298,7 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
         w.load_states(a, k, v);
         const bool mine = (w.seen >> w.lane) & 1;
         const int64_t key_pos = a.table && mine ? a.key_pos[w.b * a.key_pos_batch + w.state] : 0;
-        constexpr int HELD = LATER ? 1 : N;
+        constexpr int HELD = LATER ? 32 / E : N;
         float one[HELD][E], two[HELD][E];   // dk, dv
 #pragma unroll
         for (int t = 0; t < HELD; ++t)
@@ -387,25 +390,34 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
         };
         if constexpr (LATER) {
 #pragma unroll 1
-            for (int n = 0; n * I::kGroups < a.keys; ++n) {
+            for (int n = 0; n * I::kGroups < a.keys; n += HELD) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) one[0][i] = two[0][i] = 0.f;
+                for (int t = 0; t < HELD; ++t)
+#pragma unroll
+                    for (int i = 0; i < E; ++i) one[t][i] = two[t][i] = 0.f;
+                Chunk<T, E> next_q = w.load_row(w.query_row(a, 0, 0), true), next_y = w.load_row(dout + row0 * a.dim, true);
                 for (int r = 0, query = 0, g = 0; r < a.rows; ++r) {
                     float q[E], y[E];
-                    w.widen(w.load_row(w.query_row(a, query, g), true), q);
-                    w.widen(w.load_row(dout + (row0 + (int64_t)query * a.heads + g) * a.dim, true), y);
-                    const float2 f = waiting[slot][r][(lane & ~(L - 1)) + n];
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        one[0][i] = fmaf(f.x, q[i], one[0][i]);
-                        two[0][i] = fmaf(f.y, y[i], two[0][i]);
-                    }
+                    w.widen(next_q, q);
+                    w.widen(next_y, y);
                     if (++g == a.group) {
                         g = 0;
                         ++query;
                     }
+                    next_q = w.load_row(w.query_row(a, query, g), r + 1 < a.rows);
+                    next_y = w.load_row(dout + (row0 + (int64_t)query * a.heads + g) * a.dim, r + 1 < a.rows);
+#pragma unroll
+                    for (int t = 0; t < HELD; ++t) {
+                        const float2 f = waiting[slot][r][(lane & ~(L - 1)) + n + t];
+#pragma unroll
+                        for (int i = 0; i < E; ++i) {
+                            one[t][i] = fmaf(f.x, q[i], one[t][i]);
+                            two[t][i] = fmaf(f.y, y[i], two[t][i]);
+                        }
+                    }
                 }
-                write(n, one[0], two[0]);
+#pragma unroll
+                for (int t = 0; t < HELD; ++t) write(n + t, one[t], two[t]);
             }
         } else {
 #pragma unroll
