@@ -2,7 +2,8 @@
  * taser.h — C ABI of the MI355X (gfx950) temporal neighbor finder and feature
  * gather: the mini-batch generation hot path of TASER (arXiv 2402.05396,
  * Sec. 2.1 "Neighbor Finder", Sec. 3.3 "GPU Temporal Neighbor Finding",
- * Sec. 3.4 "GPU Feature Caching", Alg. 1-3).
+ * Sec. 3.4 "GPU Feature Caching", Alg. 1-3), and what its answers go into:
+ * attention with a bias by distance and the sampler's policy loss.
  *
  * Conventions shared by every call
  *   - Plain pointers and sizes only. Each pointer argument says "device" or
@@ -19,9 +20,10 @@
  *     been enqueued and taser_last_error() describes the problem.
  *   - Graph capture: taser_sample_temporal(_rows), taser_gather_features,
  *     taser_candidate_encodings, taser_select_weighted, taser_selector_draw,
- *     taser_selector_update and taser_cache_lookup / _lookup_static /
- *     _prefetch / _gather only launch kernels (no memset or copy nodes, no
- *     synchronization), so a stream
+ *     taser_selector_update, taser_cache_lookup / _lookup_static /
+ *     _prefetch / _gather, taser_cross_attention(_grad),
+ *     taser_relative_bias(_grad) and taser_policy_loss only launch kernels
+ *     (no memset or copy nodes, no synchronization), so a stream
  *     that is being captured into a HIP graph can be passed to them. Three
  *     things happen on first use only and must have happened before a capture:
  *     a cache lookup or prefetch with more requests than any before it on that

@@ -22,11 +22,12 @@ template <typename T, int DP, bool SHARED> struct Shape {
 
 // FINE: the output is exact to 32 bits before it is rounded, for a gradient over few states, whose <dout, out> would have the weights'
 // roundings in it otherwise (over many states they average out).
-template <typename T, int DP, bool SHARED, bool BIAS, bool FINE>
-__global__ __launch_bounds__((64 * Shape<T, DP, SHARED>::kWaves), (SHARED && sizeof(T) == 2 && !(FINE && DP == 128) ? 2 : 1)) void attention_kernel(const TaserAttentionArgs a, T* out, float* stats, float* part_out,
+template <typename T, int ND, bool SHARED, bool BIAS, bool FINE>
+__global__ __launch_bounds__((64 * Shape<T, taser_row_elements(ND), SHARED>::kWaves), (SHARED && sizeof(T) == 2 && !(FINE && ND > 2) ? 2 : 1)) void attention_kernel(const TaserAttentionArgs a, T* out, float* stats, float* part_out,
                                                                                       float* part_stats, int64_t work) {
+    constexpr int DP = taser_row_elements(ND);
     using S = Shape<T, DP, SHARED>;
-    constexpr int KT = S::kStates, NK = KT / 32, ND = DP / 32, NC = DP / 16;
+    constexpr int KT = S::kStates, NK = KT / 32, NC = 2 * ND;
     __shared__ __attribute__((aligned(1024))) char k0[S::kTiles][S::kTileBytes], v0[S::kTiles][S::kTileBytes], k1[S::kTiles][S::kTileBytes], v1[S::kTiles][S::kTileBytes];
     __shared__ int64_t pos0[S::kTiles][BIAS ? KT : 1], pos1[S::kTiles][BIAS ? KT : 1], ranges[S::kTiles][4][2];
     __shared__ float joined[2][S::kWaves][32];
@@ -433,9 +434,9 @@ __global__ __launch_bounds__(1024) void attention_join_kernel(const float* part_
     }
 }
 
-template <typename T, int DP, bool SHARED>
+template <typename T, int ND, bool SHARED>
 int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStream_t stream) {
-    using S = Shape<T, DP, SHARED>;
+    using S = Shape<T, taser_row_elements(ND), SHARED>;
     const int64_t rows = (int64_t)a.batch * a.queries * a.heads;
     float* part_out = a.splits > 1 ? work : nullptr;
     float* part_stats = a.splits > 1 ? work + a.splits * rows * a.dim : nullptr;
@@ -446,7 +447,7 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
     {
         TaserProfileSpan span(stream, "attention");
         auto run = [&](auto bias, auto fine) {
-            attention_kernel<T, DP, SHARED, decltype(bias)::value, decltype(fine)::value><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
+            attention_kernel<T, ND, SHARED, decltype(bias)::value, decltype(fine)::value><<<grid, block, 0, stream>>>(a, (T*)out, stats, part_out, part_stats, items);
         };
         const std::true_type yes;
         const std::false_type no;
@@ -471,8 +472,9 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
 }
 
 template <typename T> int launch_typed(TaserAttentionArgs& a, bool shared, void* out, float* stats, float* work, hipStream_t stream) {
-    if (a.dim <= 64) return shared ? launch<T, 64, true>(a, out, stats, work, stream) : launch<T, 64, false>(a, out, stats, work, stream);
-    return shared ? launch<T, 128, true>(a, out, stats, work, stream) : launch<T, 128, false>(a, out, stats, work, stream);
+    if (a.dim <= 64) return shared ? launch<T, 2, true>(a, out, stats, work, stream) : launch<T, 2, false>(a, out, stats, work, stream);
+    if (a.dim <= 96 && shared) return launch<T, 3, true>(a, out, stats, work, stream);   // (few rows: reading the states bounds it)
+    return shared ? launch<T, 4, true>(a, out, stats, work, stream) : launch<T, 4, false>(a, out, stats, work, stream);
 }
 
 bool few_rows(const TaserAttentionArgs& a) { return a.rows <= 64; }
@@ -481,7 +483,7 @@ bool few_rows(const TaserAttentionArgs& a) { return a.rows <= 64; }
 int splits_for(const TaserAttentionArgs& a, int32_t type) {
     if (taser_window_fits(a)) return 1;
     const int64_t pairs = (int64_t)a.batch * a.kv_heads, bytes = pairs * a.rows * a.dim * 4;
-    const double width = a.dim <= 64 ? 0.5 : 1.;
+    const double width = a.dim <= 64 ? 0.5 : a.dim <= 96 && !few_rows(a) ? 0.75 : 1.;
     // us of a tile for a block, of 64 states for 128 rows, or of 128 for 32 (measured)
     if (few_rows(a)) return taser_splits(pairs * ((a.rows + 31) / 32), 512, (a.keys + 127) / 128, width * (type == TASER_F32 ? 5. : 2.), bytes);
     return taser_splits(pairs * ((a.rows + 127) / 128), type == TASER_F32 ? 256 : 512, (a.keys + 63) / 64, width * (type == TASER_F32 ? 14. : 2.5), bytes);

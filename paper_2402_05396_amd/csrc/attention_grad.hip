@@ -44,10 +44,10 @@ __global__ __launch_bounds__(256) void attention_grad_rows_kernel(const T* out, 
 
 // ---- dq, dtable -----------------------------------------------------------------------------------------------------------
 // A wave owns 32 rows, as in the forward pass; four waves share tiles of 32 states.
-template <typename T, int DP, bool BIAS>
+template <typename T, int ND, bool BIAS>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_queries_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dq,
                                                                                                float* part_dq, float* part_table, int64_t work) {
-    constexpr int KT = 32, ND = DP / 32, NC = DP / 16, BYTES = KT * DP * (int)sizeof(T);
+    constexpr int DP = taser_row_elements(ND), KT = 32, NC = 2 * ND, BYTES = KT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(1024))) char k0[BYTES], v0[BYTES], k1[BYTES], v1[BYTES];
     __shared__ int64_t pos0[BIAS ? KT : 1], pos1[BIAS ? KT : 1], ranges[4][2];
     __shared__ uint8_t near[BIAS ? kTaserNear : 1];
@@ -299,10 +299,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
 // tile's two steps is as many products for the one as for the other, and neither holds more than half of the sums: a wave with both
 // has too many registers for a second one on its SIMD (measured: 610 TFLOP/s so at 2 x 4096 x 4096, 16 heads of 128). Rows of all query
 // heads of the key head pass by, so shared heads' gradients are whole.
-template <typename T, int DP, bool BIAS>
-__global__ __launch_bounds__(512, (DP == 64 && sizeof(T) == 2 ? 4 : 2)) void attention_grad_states_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dk, T* dv, float* part_dk,
+template <typename T, int ND, bool BIAS>
+__global__ __launch_bounds__(512, (ND <= 2 && sizeof(T) == 2 ? 4 : 2)) void attention_grad_states_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dk, T* dv, float* part_dk,
                                                                     float* part_dv, int64_t work) {
-    constexpr int RT = sizeof(T) == 2 ? 64 : 32, NS = RT / 32, ND = DP / 32, NC = DP / 16, BYTES = RT * DP * (int)sizeof(T);
+    constexpr int DP = taser_row_elements(ND), RT = sizeof(T) == 2 ? 64 : 32, NS = RT / 32, NC = 2 * ND, BYTES = RT * DP * (int)sizeof(T);
     __shared__ __attribute__((aligned(1024))) char q0[BYTES], y0[BYTES], q1[BYTES], y1[BYTES];
     __shared__ taser_f4 passed[4][NS][4][64];                 // a pair's weights, by registers and lane
     __shared__ taser_f4 info0[3][RT / 4], info1[3][RT / 4];   // a kind of number of 4 rows
@@ -565,13 +565,29 @@ __global__ __launch_bounds__(512, (DP == 64 && sizeof(T) == 2 ? 4 : 2)) void att
         }
 }
 
-// Adds up parts, in their order.
-template <typename T> __global__ __launch_bounds__(256) void attention_grad_add_kernel(const float* parts, int32_t n_parts, int64_t n, T* out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// Adds up parts of up to three gradients, in their order: one launch for all (of 5 us each in a small call).
+template <typename T> struct Sums {
+    int32_t count = 0, n_parts[3];
+    int64_t n[3];
+    const float* parts[3];
+    T* out[3];
+    void add(const float* parts_, int32_t n_parts_, int64_t n_, T* out_) {
+        if (!n_) return;
+        parts[count] = parts_;
+        n_parts[count] = n_parts_;
+        n[count] = n_;
+        out[count++] = out_;
+    }
+};
+template <typename T> __global__ __launch_bounds__(256) void attention_grad_add_kernel(const Sums<T> sums) {
+    const int of = blockIdx.y;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = sums.n[of];
     if (i >= n) return;
+    const float* parts = sums.parts[of] + i;
     float x = 0.f;
-    for (int p = 0; p < n_parts; ++p) x += parts[p * n + i];
-    out[i] = (T)x;
+#pragma unroll 4
+    for (int p = 0; p < sums.n_parts[of]; ++p) x += parts[p * n];
+    sums.out[of][i] = (T)x;
 }
 
 // A block has a head, a thread four buckets of a chain of sums: as many chains as there are threads, then the chains in their order.
@@ -616,7 +632,7 @@ Plan plan(const TaserAttentionArgs& a, int32_t type) {
     p.row_tiles = (int)(((int64_t)a.rows + 127) / 128);
     p.state_tiles = (int)(((int64_t)a.keys + 127) / 128);
     const int64_t rows_bytes = pairs * a.rows * a.dim * 4, states_bytes = 2 * pairs * a.keys * a.dim * 4;
-    const double tile = (a.dim <= 64 ? 0.5 : 1.) * (type == TASER_F32 ? 11. : 1.5);   // us of 32 states, or rows, for a block (measured)
+    const double tile = (a.dim <= 64 ? 0.5 : a.dim <= 96 ? 0.75 : 1.) * (type == TASER_F32 ? 11. : 1.5);   // us of 32 states, or rows, for a block (measured)
     p.row_splits = taser_splits(pairs * p.row_tiles, type == TASER_F32 ? 256 : 512, (a.keys + 31) / 32, tile, rows_bytes);
     p.state_splits = taser_splits(pairs * p.state_tiles, type != TASER_F32 && a.dim <= 64 ? 512 : 256, (a.rows + 31) / 32, tile, states_bytes);
     auto take = [&](uint64_t bytes) {
@@ -633,17 +649,11 @@ Plan plan(const TaserAttentionArgs& a, int32_t type) {
     return p;
 }
 
-template <typename T> int add_up(const float* parts, int n_parts, int64_t n, T* out, hipStream_t stream) {
-    TaserProfileSpan span(stream, "attention_grad_add");
-    attention_grad_add_kernel<T><<<dim3((unsigned)((n + 255) / 256)), 256, 0, stream>>>(parts, n_parts, n, out);
-    TASER_HIP_TRY(hipGetLastError());
-    return TASER_OK;
-}
-
-template <typename T, int DP>
+template <typename T, int ND>
 int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stats, const T* dout, T* dq, T* dk, T* dv, T* dtable, char* work, hipStream_t stream) {
     const int64_t rows = (int64_t)a.batch * a.queries * a.heads, states = (int64_t)a.batch * a.keys * a.kv_heads * a.dim, pairs = (int64_t)a.batch * a.kv_heads;
     taser_f4* info = (taser_f4*)(work + p.info);
+    Sums<T> sums;
     if (rows) {
         TaserProfileSpan span(stream, "attention_grad_rows");
         attention_grad_rows_kernel<T><<<dim3((unsigned)((rows + 15) / 16)), 256, 0, stream>>>(out, dout, stats, a.stat_floats, rows, a.dim, info);
@@ -659,13 +669,12 @@ int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stat
         {
             TaserProfileSpan span(stream, "attention_grad_queries");
             if (a.table)
-                attention_grad_queries_kernel<T, DP, true><<<grid, 256, 0, stream>>>(a, info, dout, dq, part, part_table, items);
+                attention_grad_queries_kernel<T, ND, true><<<grid, 256, 0, stream>>>(a, info, dout, dq, part, part_table, items);
             else
-                attention_grad_queries_kernel<T, DP, false><<<grid, 256, 0, stream>>>(a, info, dout, dq, part, part_table, items);
+                attention_grad_queries_kernel<T, ND, false><<<grid, 256, 0, stream>>>(a, info, dout, dq, part, part_table, items);
             TASER_HIP_TRY(hipGetLastError());
         }
-        if (part)
-            if (const int rc = add_up<T>(part, p.row_splits, rows * a.dim, dq, stream)) return rc;
+        if (part) sums.add(part, p.row_splits, rows * a.dim, dq);
     }
     if (a.table) {
         const int32_t type = std::is_same_v<T, float> ? TASER_F32 : std::is_same_v<T, _Float16> ? TASER_F16 : TASER_BF16;
@@ -687,23 +696,31 @@ int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stat
         {
             TaserProfileSpan span(stream, "attention_grad_states");
             if (a.table)
-                attention_grad_states_kernel<T, DP, true><<<grid, 512, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
+                attention_grad_states_kernel<T, ND, true><<<grid, 512, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
             else
-                attention_grad_states_kernel<T, DP, false><<<grid, 512, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
+                attention_grad_states_kernel<T, ND, false><<<grid, 512, 0, stream>>>(a, info, dout, dk, dv, part, part_v, items);
             TASER_HIP_TRY(hipGetLastError());
         }
         if (part) {
-            if (const int rc = add_up<T>(part, p.state_splits, states, dk, stream)) return rc;
-            if (const int rc = add_up<T>(part_v, p.state_splits, states, dv, stream)) return rc;
+            sums.add(part, p.state_splits, states, dk);
+            sums.add(part_v, p.state_splits, states, dv);
         }
+    }
+    if (sums.count) {
+        int64_t most = 0;
+        for (int i = 0; i < sums.count; ++i) most = sums.n[i] > most ? sums.n[i] : most;
+        TaserProfileSpan span(stream, "attention_grad_add");
+        attention_grad_add_kernel<T><<<dim3((unsigned)((most + 255) / 256), (unsigned)sums.count), 256, 0, stream>>>(sums);
+        TASER_HIP_TRY(hipGetLastError());
     }
     return TASER_OK;
 }
 
 template <typename T>
 int launch_typed(TaserAttentionArgs& a, const Plan& p, const void* out, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, char* work, hipStream_t stream) {
-    if (a.dim <= 64) return launch<T, 64>(a, p, (const T*)out, stats, (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (T*)dtable, work, stream);
-    return launch<T, 128>(a, p, (const T*)out, stats, (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (T*)dtable, work, stream);
+    if (a.dim <= 64) return launch<T, 2>(a, p, (const T*)out, stats, (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (T*)dtable, work, stream);
+    if (a.dim <= 96) return launch<T, 3>(a, p, (const T*)out, stats, (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (T*)dtable, work, stream);
+    return launch<T, 4>(a, p, (const T*)out, stats, (const T*)dout, (T*)dq, (T*)dk, (T*)dv, (T*)dtable, work, stream);
 }
 
 }  // namespace
