@@ -36,6 +36,7 @@ struct TaserAttentionArgs {
     int32_t direct;           // states are 16-byte aligned and their heads whole 16-byte pieces: tiles are loaded past the registers
 };
 
+inline bool taser_single(const TaserAttentionArgs& a) { return a.stat_floats == 2; }   // single precision
 // Checks a call's arguments and lays them out for the kernels.
 int taser_attention_args(const taser_attention* p, const char* what, TaserAttentionArgs* a);
 // In how many parts the long axis of `blocks` blocks is cut, `tiles` tiles of `tile` us each, where `slots` blocks run at a time: the

@@ -477,7 +477,9 @@ template <typename T> int launch_typed(TaserAttentionArgs& a, bool shared, void*
     return shared ? launch<T, 4, true>(a, out, stats, work, stream) : launch<T, 4, false>(a, out, stats, work, stream);
 }
 
-bool few_rows(const TaserAttentionArgs& a) { return a.rows <= 64; }
+// Rows of its own for each block of waves, or rows shared by them? (8 x 8 pairs, 4096 states, heads of 128, us, own / shared: 16 bits
+// 32 rows 34 / 33, 64 39 / 40, 96 57 / 45; float32 32 rows 105 / 155, 64 186 / 158, 96 349 / 161.)
+bool few_rows(const TaserAttentionArgs& a) { return a.rows <= (taser_single(a) ? 32 : 64); }
 
 // Parts of the states, so that the chip is full where there are few rows.
 int splits_for(const TaserAttentionArgs& a, int32_t type) {

@@ -482,8 +482,14 @@ int64_t grad_waves(const TaserAttentionArgs& a) {
 
 }  // namespace
 
-// (a row of at least 16 bytes)
-bool taser_window_fits(const TaserAttentionArgs& a) { return a.keys >= 1 && a.keys <= 64 && a.rows <= kWindowRows && a.dim >= 8 && (int64_t)a.batch * a.kv_heads < INT32_MAX / 2; }
+// Windows cost by rows times states, tiles by their number, one for up to 32 rows and states. 4000 items, heads of 64, here / by tiles, us,
+// forward and with the gradient: 16 bits, 16 rows of 10 states 23 / 42, 63 / 148; 8 of 64 40 / 42, 122 / 175; 32 of 64 92 / 37, 353 / 178;
+// float32 8 of 64 46 / 105, 167 / 394; 32 of 64 113 / 103, 493 / 400, and 2000 of 128 227 / 87, 659 / 433.
+// (A row has to have 16 bytes.)
+bool taser_window_fits(const TaserAttentionArgs& a) {
+    return a.keys >= 1 && a.keys <= 64 && a.rows <= kWindowRows && a.rows * a.keys <= (taser_single(a) ? 1024 : 768) && a.dim >= 8 &&
+           (int64_t)a.batch * a.kv_heads < INT32_MAX / 2;
+}
 
 int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out, float* stats, hipStream_t stream) {
     Call c = {};
