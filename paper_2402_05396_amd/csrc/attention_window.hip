@@ -5,6 +5,11 @@
 // s L' + g (L' = 64 / L) is group g's in turn s. A score is a sum over a group; then lane (g, c) takes the score of turn c: each
 // state has one lane, whose softmax weight costs one exponential, and where its bucket, its gradient and the sums over all states
 // are found. The weights go back to the groups for the sums over the states.
+//
+// Bound by reading the states: 30000 windows of 25 states, four heads on two of 64, float16, bias: 85 us for 364 MB, 4.4 TB/s; with
+// the gradient in bfloat16 98 + 310 us. 12000 windows of 10 states, two heads of 50, float32: 29 + 48 us for 97 + 200 MB (rows of 200 bytes
+// leave 3 of 16 lanes idle). A score costs as many vector instructions as its row has elements over L, so many rows or states an item are
+// left to the tiles.
 #include "attention.h"
 
 namespace {

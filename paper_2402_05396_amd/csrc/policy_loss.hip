@@ -3,6 +3,9 @@
 // With l = logp of an action: d loss / d l = weight * (-ratio * advantage where that is the smaller term, + kl (1 - exp(ref - l))), and
 // d l / d logit[c] = (c is the action) - softmax[c]. So a row's gradient is minus the sum of its actions' slopes times the softmax,
 // plus each slope at its action.
+//
+// Bound by reading the logits once and writing their gradient once: 4096 rows of 64001 in bfloat16 248 us, 1.05 GB at 4.2 TB/s (rows of an odd
+// length begin inside cache lines: counters say 0.73 GB read, 0.54 written). 12000 rows of 25 with 10 actions: 6 us, a launch.
 #include "attention.h"
 
 namespace {
