@@ -210,13 +210,14 @@ __device__ inline void taser_lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-// Adds to LDS and goes on: written out, as the compiler would first wait for every load that is on its way to LDS. A lane's adds keep
-// their order; taser_lds_adds_done() comes before another wave reads.
-__device__ inline void taser_lds_add(float* to, float x) {
-    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) float*)to;
-    asm volatile("ds_add_f32 %0, %1" ::"v"(at), "v"(x) : "memory");
+// Between the turns of lanes that add to one place of LDS by reading and writing it: the compiler, which looks at a lane by itself, may
+// not make one turn of two. (Additions by the LDS itself take it two clocks a lane, from all waves: 16 of a lane's for each of the few
+// tiles that have several buckets cost 90 of 551 us of a gradient, reads and writes 20.)
+__device__ inline void taser_next_turn() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("" ::: "memory");
 }
-__device__ inline void taser_lds_adds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Where a lane's part of a tile lies, once for all tiles: 32 rows further on, everything is 32 rows of bytes further on.
 // Operand of the tile's rows (lane l: row l % 32), contraction over elements 16 c ..

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void attention_grad_rows_kernel(const T* out, 
 // ---- dq, dtable -----------------------------------------------------------------------------------------------------------
 // A wave owns 32 rows, as in the forward pass; four waves share tiles of 32 states. Bound by registers (queries, their gradients, output: two
 // waves a SIMD) and by what the vector units do to scores between products; tiles with several buckets add each dx to its bucket's sum in
-// LDS. 2 x 4096 x 4096, 16 heads on 4 of 128, bfloat16: 369 us without a bias, 460 with one bucket, 551 with 32 around distance 0.
+// LDS. 2 x 4096 x 4096, 16 heads on 4 of 128, bfloat16: 369 us without a bias, 460 with one bucket, 485 with 32 around distance 0.
 template <typename T, int ND, bool BIAS>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_queries_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dq,
                                                                                                float* part_dq, float* part_table, int64_t work) {
@@ -202,11 +202,25 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
                 for (int j = 0; j < 4; ++j) {
                     int bucket[4];
                     of.find<false>(bucket, query_pos, pos + 8 * j + 4 * half);
+                    // Four at a time: what has a later one's bucket is added to that one, whose write comes after its own.
+                    float x[4];
 #pragma unroll
-                    for (int side = 0; side < 2; ++side)
-                        if (half == side)
+                    for (int i = 0; i < 4; ++i) {
+                        x[i] = s[4 * j + i];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) taser_lds_add(&my_sums[bucket[i]][lane & 31], s[4 * j + i]);
+                        for (int e = 0; e < i; ++e) x[i] += bucket[e] == bucket[i] ? s[4 * j + e] : 0.f;
+                    }
+#pragma unroll
+                    for (int side = 0; side < 2; ++side) {
+                        if (half == side) {
+                            float y[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) y[i] = my_sums[bucket[i]][lane & 31];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) my_sums[bucket[i]][lane & 31] = y[i] + x[i];
+                        }
+                        taser_next_turn();
+                    }
                 }
             } else {
                 float x = 0.f;
@@ -263,7 +277,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
     }
 
     if constexpr (BIAS) {
-        taser_lds_adds_done();
         __syncthreads();
         float* to = part_table + item * (a.group * taser_padded(a.buckets));
         const int rows = a.rows - row_tile * 128 < 128 ? a.rows - row_tile * 128 : 128;

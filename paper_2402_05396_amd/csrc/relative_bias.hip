@@ -121,8 +121,10 @@ __global__ __launch_bounds__(256) void relative_bias_grad_kernel(const Distances
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.y;
     float* mine = sums + wave * d.buckets * 32 + (lane & 31);
     auto add = [&](int bucket, float x) {
-        if (lane < 32) taser_lds_add(mine + 32 * bucket, x);
-        if (lane >= 32) taser_lds_add(mine + 32 * bucket, x);
+        if (lane < 32) mine[32 * bucket] += x;
+        taser_next_turn();
+        if (lane >= 32) mine[32 * bucket] += x;
+        taser_next_turn();
     };
     const Near w = begin(d, near, lane);
     if (wave == 0) bounds[lane] = w.bound;
@@ -210,7 +212,6 @@ __global__ __launch_bounds__(256) void relative_bias_grad_kernel(const Distances
         }
     }
     add(running, sum);
-    taser_lds_adds_done();
     __syncthreads();
     if ((int)threadIdx.x < d.buckets) {   // a lane a bucket, each starting at a column of its own
         float total = 0.f;
