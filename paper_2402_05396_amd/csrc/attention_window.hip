@@ -504,8 +504,9 @@ int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out,
     return run_any(a, type, c);
 }
 
+// Never nothing: a caller that brings no workspace learns it from every gradient, not from those alone that go over tiles.
 uint64_t taser_window_grad_bytes(const TaserAttentionArgs& a) {
-    return a.table ? (uint64_t)grad_waves(a) * a.rows * taser_padded(a.buckets) * sizeof(float) : 0;
+    return a.table ? (uint64_t)grad_waves(a) * a.rows * taser_padded(a.buckets) * sizeof(float) : 256;
 }
 
 int taser_window_attention_grad(const TaserAttentionArgs& a, int32_t type, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, float* work, hipStream_t stream) {
