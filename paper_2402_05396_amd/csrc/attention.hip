@@ -375,13 +375,13 @@ __global__ __launch_bounds__(256) void attention_join_few_kernel(const float* pa
     float top = -INFINITY, sum = 0.f, x = 0.f;
 #pragma unroll 4
     for (int s = 0; s < splits; ++s) top = fmaxf(top, part_stats[2 * (s * rows + row)]);
-    if (top != -INFINITY)
+    // (Splits whose scores are all NaN say minus infinity too, but their sums are not 0.)
 #pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float by = __builtin_amdgcn_exp2f((part_stats[2 * (s * rows + row)] - top) * kLog2e);
-            sum = fmaf(by, part_stats[2 * (s * rows + row) + 1], sum);
-            x = fmaf(by, part_out[(s * rows + row) * dim + e], x);
-        }
+    for (int s = 0; s < splits; ++s) {
+        const float by = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((part_stats[2 * (s * rows + row)] - top) * kLog2e);
+        sum = fmaf(by, part_stats[2 * (s * rows + row) + 1], sum);
+        x = fmaf(by, part_out[(s * rows + row) * dim + e], x);
+    }
     x = sum != 0.f ? x / sum : 0.f;
     out[i] = (T)x;
     if (!stats) return;

@@ -462,3 +462,27 @@ def test_distances_in_tiles_of_many_buckets(kind):
         c["bias"][0][:, 3] = -2.0 ** 14
         c["bias"][0][0] = 2.0 ** 14
         _check(c)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_nan_of_a_query_reaches_its_row_alone(kind):
+    """However the states are cut: not at all, into few parts, into many."""
+    cut = set()
+    for B, Lq, Lk, H, d in ((1, 1, 40, 2, 64), (1, 200, 100, 2, 64), (1, 2, 700, 2, 64), (2, 3, 2500, 4, 50), (1, 200, 3000, 2, 128), (1, 1, 40_000, 2, 64)):
+        c = _case(kind, B, Lq, Lk, H, H // 2, d)
+        c["q"][0, -1, 1, 5] = float("nan")
+        row = torch.zeros((B, Lq, H), dtype=torch.bool)
+        row[0, -1, 1] = True
+        q, k, v, dout, more = _device(c)
+        parts = T.cross_attention_bytes(q, k, v, **more)[0] // (4 * B * Lq * H * (d + 2))
+        cut.add("not" if parts <= 1 else "few" if parts <= 16 else "many")
+        out, stats = T.cross_attention(q, k, v, want_stats=True, **more)
+        grads = T.cross_attention_grad(dout, q, k, v, out, stats, **more)
+        for name, x in (("out", out), ("dq", grads[0])):
+            assert torch.isnan(x[row]).all() and torch.isfinite(x[~row]).all(), (name, Lq, Lk)
+        states = torch.zeros((B, Lk, H // 2), dtype=torch.bool)
+        states[0, :, 0] = True
+        for name, x in (("dk", grads[1]), ("dv", grads[2])):
+            assert torch.isnan(x[states]).all() and torch.isfinite(x[~states]).all(), (name, Lq, Lk)
+    assert cut == {"not", "few", "many"}
