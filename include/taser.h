@@ -558,7 +558,8 @@ int taser_relative_bias_grad(const taser_distances* d, const void* dbias, const 
  *                          clip(ratio, 1 - clip_low, 1 + clip_high) * advantage)
  *                     + kl * (exp(apart) - apart - 1))
  * and 0 for any other action (-1: none), whose logp is 0 too. weight NULL: 1.
- * grad[r][c] = the derivative of the sum of all losses (zeros past count[r]);
+ * grad[r][c] = the derivative of the sum of all losses (zeros past count[r], and
+ * in a row whose actions are all none or of weight 0, whatever its logits are);
  * where ratio * advantage is not the smaller of the two, the first term has none.
  *   logits  device, type, row r at r * logits_stride elements
  *   actions int32[rows][picks]; advantage, old_logp, ref_logp, weight, loss, logp

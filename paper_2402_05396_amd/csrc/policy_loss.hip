@@ -26,8 +26,9 @@ __device__ inline int32_t taking_part(const Batch& p, int64_t row) {
     return n < 0 ? 0 : (n > p.width ? p.width : n);
 }
 
-// Loss of the action at place `at` of the row's, and its slope. An action of weight 0 has neither, whatever else is given for it.
-__device__ inline void action_loss(const Batch& p, int64_t at, float logp, float* loss, float* slope) {
+// Loss of the action at place `at` of the row's, and its slope. An action of weight 0 has neither, whatever else is given for it, and
+// does not count: a row without any that does has no gradient, whatever its logits are.
+__device__ inline bool action_loss(const Batch& p, int64_t at, float logp, float* loss, float* slope) {
     const float w = p.weight ? p.weight[at] : 1.f, a = p.advantage[at];
     const float ratio = p.old_logp ? expf(logp - p.old_logp[at]) : 1.f;
     const float whole = ratio * a, cut = p.old_logp ? fminf(fmaxf(ratio, 1.f - p.low), 1.f + p.high) * a : whole;
@@ -40,6 +41,7 @@ __device__ inline void action_loss(const Batch& p, int64_t at, float logp, float
     }
     *loss = w != 0.f ? w * x : 0.f;
     *slope = w != 0.f ? w * y : 0.f;
+    return w != 0.f;
 }
 
 // Rows of at most 64 candidates and actions: G lanes a row, a candidate and an action a lane.
@@ -64,9 +66,10 @@ __global__ __launch_bounds__(256) void policy_window_kernel(const Batch p, const
     const bool real = action >= 0 && action < n;
     const float chosen = __shfl(x, real ? action : 0, G);
     float l = 0.f, mine = 0.f, slope = 0.f;
+    bool counts = false;
     if (real) {
         l = (chosen - top) - logsum;
-        action_loss(p, at, l, &mine, &slope);
+        counts = action_loss(p, at, l, &mine, &slope);
     }
     if (lane < p.picks) {
         loss[at] = mine;
@@ -76,7 +79,9 @@ __global__ __launch_bounds__(256) void policy_window_kernel(const Batch p, const
     float all = slope;
 #pragma unroll
     for (int m = 1; m < G; m <<= 1) all += __shfl_xor(all, m, G);
-    float g = sum > 0.f ? e / sum * -all : e * -all;
+    constexpr uint64_t lanes = G == 64 ? ~0ull : (1ull << (G & 63)) - 1;
+    const bool some = __ballot(counts) >> (threadIdx.x & 63 & ~(G - 1)) & lanes;
+    float g = !some ? 0.f : sum > 0.f ? e / sum * -all : e * -all;
     for (int j = 0; j < p.picks; ++j) {
         const int a = __shfl(real ? action : -1, j, G);
         const float y = __shfl(slope, j, G);
@@ -102,6 +107,7 @@ __global__ __launch_bounds__(THREADS, (HELD <= 4 ? 8 : 4)) void policy_row_kerne
     __shared__ float tops[16], sums[16], slopes[TASER_MAX_PICKS];
     __shared__ int places[TASER_MAX_PICKS];
     __shared__ float whole;
+    __shared__ uint32_t some;
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = taking_part(p, row), waves = blockDim.x >> 6;
     const int64_t step = (int64_t)blockDim.x * EACH;
@@ -168,9 +174,10 @@ __global__ __launch_bounds__(THREADS, (HELD <= 4 ? 8 : 4)) void policy_row_kerne
     if (top == -INFINITY) top = 0.f;
     if (wave == 0) {
         float l = 0.f, mine = 0.f, slope = 0.f;
+        bool counts = false;
         if (real) {
             l = (chosen - top) - logf(sum);
-            action_loss(p, at, l, &mine, &slope);
+            counts = action_loss(p, at, l, &mine, &slope);
         }
         if (lane < p.picks) {
             loss[at] = mine;
@@ -181,11 +188,16 @@ __global__ __launch_bounds__(THREADS, (HELD <= 4 ? 8 : 4)) void policy_row_kerne
         float all = slope;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) all += __shfl_xor(all, m);
-        if (lane == 0) whole = all;
+        const bool any = __any(counts);
+        if (lane == 0) {
+            whole = all;
+            some = any ? ~0u : 0u;
+        }
     }
     if (!grad) return;
     __syncthreads();
     const float by = sum > 0.f ? -whole / sum : -whole;
+    const uint32_t keep = __builtin_amdgcn_readfirstlane(some);   // all bits of a gradient, or none
     T* to = grad + row * p.width;
     auto give = [&](int64_t c, const Piece& x) {
         Piece y;
@@ -195,10 +207,11 @@ __global__ __launch_bounds__(THREADS, (HELD <= 4 ? 8 : 4)) void policy_row_kerne
             typedef uint32_t loose __attribute__((ext_vector_type(4), aligned(2)));
             loose u;
             __builtin_memcpy(&u, y.x, 16);
+            u &= keep;
             __builtin_nontemporal_store(u, (loose*)(to + c));
         } else if (c < p.width) {
             for (int i = 0; i < EACH; ++i)
-                if (c + i < p.width) to[c + i] = (T)(c + i < n ? __builtin_amdgcn_exp2f(((float)x.x[i] - top) * kLog2e) * by : 0.f);
+                if (c + i < p.width) to[c + i] = (T)(c + i < n && keep ? __builtin_amdgcn_exp2f(((float)x.x[i] - top) * kLog2e) * by : 0.f);
         }
     };
 #pragma unroll
@@ -209,7 +222,7 @@ __global__ __launch_bounds__(THREADS, (HELD <= 4 ? 8 : 4)) void policy_row_kerne
         give(c, x);
     }
     __syncthreads();   // the row is written: its actions' places are now put right
-    if (wave == 0 && real) {
+    if (wave == 0 && real && keep) {
         float g = __builtin_amdgcn_exp2f((chosen - top) * kLog2e) * by;
         for (int j = 0; j < p.picks; ++j) g += places[j] == action ? slopes[j] : 0.f;
         to[action] = (T)g;

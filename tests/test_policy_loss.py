@@ -240,3 +240,20 @@ def test_the_oracle_against_differences():
             up[i] += h
             down[i] -= h
             assert abs((run(up)["loss"].sum() - run(down)["loss"].sum()) / (2 * h) - grad[i]) < 1e-7, i
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_without_an_action_that_counts_have_no_gradient(kind):
+    """Padded rows: no action, or actions of weight 0, over logits that are NaN, infinite or ruled out."""
+    for W in (20, 64, 300, 5000, 70_000):
+        x = torch.zeros((6, W), dtype=KINDS[kind])
+        x[0], x[1], x[2] = float("nan"), -float("inf"), float("inf")
+        x[3, W // 2] = x[5, W // 2] = float("nan")
+        a = torch.full((6, 3), -1, dtype=torch.int32)
+        a[3:, 1] = 2
+        weight = torch.ones((6, 3))
+        weight[3] = 0.0
+        loss, logp, grad = T.policy_loss(x.cuda(), a.cuda(), torch.ones((6, 3)).cuda(), weight=weight.cuda())
+        assert not grad[:4].any() and not loss[:4].any() and not logp[:3].any(), W
+        assert abs(float(grad[4, 2]) + 1 - 1 / W) < 2.0 ** -8 and float(grad[4].float().sum().abs()) < 2.0 ** -8, W
