@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256) void policy_window_kernel(const Batch p, const
     for (int m = 1; m < G; m <<= 1) all += __shfl_xor(all, m, G);
     constexpr uint64_t lanes = G == 64 ? ~0ull : (1ull << (G & 63)) - 1;
     const bool some = __ballot(counts) >> (threadIdx.x & 63 & ~(G - 1)) & lanes;
-    float g = !some ? 0.f : sum > 0.f ? e / sum * -all : e * -all;
+    float g = !some ? 0.f : e / sum * -all;   // (a sum of 0, all are ruled out, or of NaN: NaN, as the softmax is)
     for (int j = 0; j < p.picks; ++j) {
         const int a = __shfl(real ? action : -1, j, G);
         const float y = __shfl(slope, j, G);
@@ -92,9 +92,9 @@ __global__ __launch_bounds__(256) void policy_window_kernel(const Batch p, const
 
 // The larger of two running (maximum, sum of exponentials).
 __device__ inline void join(float& top, float& sum, float other_top, float other_sum) {
-    const float best = fmaxf(top, other_top);
-    if (best == -INFINITY) return;
-    sum = sum * __builtin_amdgcn_exp2f((top - best) * kLog2e) + other_sum * __builtin_amdgcn_exp2f((other_top - best) * kLog2e);
+    // (Where both are minus infinity the sums are 0, or NaN, of which fmaxf says minus infinity too: they are added all the same.)
+    const float best = fmaxf(top, other_top), base = best == -INFINITY ? 0.f : best;
+    sum = sum * __builtin_amdgcn_exp2f((top - base) * kLog2e) + other_sum * __builtin_amdgcn_exp2f((other_top - base) * kLog2e);
     top = best;
 }
 
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(THREADS, (HELD <= 4 ? 8 : 4)) void policy_row_kerne
     }
     if (!grad) return;
     __syncthreads();
-    const float by = sum > 0.f ? -whole / sum : -whole;
+    const float by = -whole / sum;   // (as in a window)
     const uint32_t keep = __builtin_amdgcn_readfirstlane(some);   // all bits of a gradient, or none
     T* to = grad + row * p.width;
     auto give = [&](int64_t c, const Piece& x) {

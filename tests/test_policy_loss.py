@@ -257,3 +257,18 @@ def test_rows_without_an_action_that_counts_have_no_gradient(kind):
         loss, logp, grad = T.policy_loss(x.cuda(), a.cuda(), torch.ones((6, 3)).cuda(), weight=weight.cuda())
         assert not grad[:4].any() and not loss[:4].any() and not logp[:3].any(), W
         assert abs(float(grad[4, 2]) + 1 - 1 / W) < 2.0 ** -8 and float(grad[4].float().sum().abs()) < 2.0 ** -8, W
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_nan_among_logits_of_minus_infinity(kind):
+    """A NaN whose neighbors are all ruled out reaches the row's results, wherever in the row it lies."""
+    for W in (20, 300, 5000, 70_000):
+        for at in (3, 11, W // 2, W - 2):
+            x = torch.full((3, W), -float("inf"), dtype=KINDS[kind])
+            x[:, 1] = 0.5
+            x[1, at] = float("nan")
+            x[2, W - 1] = 0.5
+            a = torch.ones((3, 1), dtype=torch.int32)
+            loss, logp, grad = T.policy_loss(x.cuda(), a.cuda(), torch.ones((3, 1)).cuda())
+            assert torch.isnan(logp[1]).all() and torch.isnan(grad[1, 1]) and torch.isfinite(logp[[0, 2]]).all() and torch.isfinite(grad[[0, 2]]).all(), (W, at)
