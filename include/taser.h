@@ -492,7 +492,8 @@ void taser_selector_free(taser_selector* s);
  * taser_cross_attention_bytes says (either out-pointer may be NULL) for the
  * same block. Both only launch kernels.
  * Sums, softmax statistics and bias are held in 32 bits; softmax weights and
- * their gradients are rounded to `type` where they enter a matrix product.
+ * their gradients are rounded to `type` where they enter a matrix product (for
+ * float16 times powers of two that keep small ones and large ones in its range).
  * ------------------------------------------------------------------------- */
 enum taser_type { TASER_F32 = 0, TASER_F16 = 1, TASER_BF16 = 2 };
 

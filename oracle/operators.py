@@ -23,9 +23,10 @@ def buckets(bounds, query_pos, key_pos):
     return out
 
 
-def attention(q, k, v, kind, lengths=None, mask=None, table=None, bucket=None, scale=None, dout=None):
+def attention(q, k, v, kind, lengths=None, mask=None, table=None, bucket=None, scale=None, dout=None, lifted=False):
     """q [B, Lq, H, d], k, v [B, Lk, Hk, d] float64; bucket: a list of [Lq, Lk] for each batch entry. -> (results, bounds): dicts of
-    out, and with `dout` dq, dk, dv, dtable."""
+    out, and with `dout` dq, dk, dv, dtable. lifted: the bounds of an operator that multiplies dx by a power of two before it rounds it to
+    float16, for each row of dq and each state of dk so that the largest comes to 2^7 at least: not `tiny` each, but 2^-7 `tiny` of the largest."""
     B, Lq, H, d = q.shape
     Lk, Hk = k.shape[1:3]
     g = H // Hk
@@ -71,13 +72,20 @@ def attention(q, k, v, kind, lengths=None, mask=None, table=None, bucket=None, s
             dx = p * (dp - t)
             et = (np.abs(Y) * off["out"][b, :, h]).sum(1, keepdims=True) + d * E32 * (np.abs(Y) * np.abs(o)).sum(1, keepdims=True)
             edx = ep * np.abs(dp - t) + p * ((d + 4) * E32 * (np.abs(Y) @ np.abs(V).T) + et) + 4 * E32 * np.abs(dx) + END32
-            rdx = edx + u16 * np.abs(dx) + (tiny if u16 else 0.0)                  # where it enters a product
+            rdx = edx + u16 * np.abs(dx)                                           # where it enters a product
+            rdq, rdk = rdx + (tiny if u16 else 0.0), rdx + (tiny if u16 else 0.0)
+            if lifted and u16:                                                     # a state has one factor for all heads that share it
+                rdq = rdx + 2.0 ** -7 * tiny * (rdx + np.abs(dx)).max(1, keepdims=True)
+                largest, weights = (0.0, 0.0) if h % g == 0 else (largest, weights)
+                largest, weights, rdk = np.maximum(largest, (rdx + np.abs(dx)).max(0)), weights + np.abs(Q).sum(0), rdx
+                if h % g == g - 1:
+                    off["dk"][b, at, h // g] += scale * 2.0 ** -7 * tiny * largest[:, None] * weights
             n = (Lq * g + len(at) + 8) * E32
-            for name, of, value, err in (("dq", (b, slice(None), h), scale * dx @ K, scale * (rdx @ np.abs(K) + n * np.abs(dx) @ np.abs(K))),):
+            for name, of, value, err in (("dq", (b, slice(None), h), scale * dx @ K, scale * (rdq @ np.abs(K) + n * np.abs(dx) @ np.abs(K))),):
                 res[name][of] += value
                 off[name][of] += err
             res["dk"][b, at, h // g] += scale * dx.T @ Q
-            off["dk"][b, at, h // g] += scale * (rdx.T @ np.abs(Q) + n * np.abs(dx).T @ np.abs(Q))
+            off["dk"][b, at, h // g] += scale * (rdk.T @ np.abs(Q) + n * np.abs(dx).T @ np.abs(Q))
             res["dv"][b, at, h // g] += p.T @ Y
             off["dv"][b, at, h // g] += (ep + (u16 + n) * p).T @ np.abs(Y) + (tiny * 2.0 ** -14 * np.abs(Y).sum(0) if u16 else 0.0)
             if table is not None:

@@ -141,6 +141,19 @@ __device__ inline float taser_halves_max(float x) {
     return fmaxf(__builtin_bit_cast(float, a), __builtin_bit_cast(float, b));
 }
 
+// Half precision ends at 6e-8 and at 65504, and a weight's gradient over thousands of states, of a mean loss or of one scaled up, lies
+// beyond. So it is multiplied by a power of two before it is rounded: one for each column of a product's sums, which are held times the same
+// and multiplied again where a larger value asks for another. The largest value yet lies in 2^7 .. 2^15 (or below, from the start on).
+// (Forward and gradient of 2 x 4096 x 4096, 16 heads on 4 of 128, float16: 1267 us for 1257 without, with a bias 1550 for 1500; of 64
+// elements 798 for 772. At a dout of 1e-3 the error of dq is 0.0003 of it, and was 0.003.)
+template <typename T> constexpr bool taser_lifted = false;
+template <> constexpr inline bool taser_lifted<_Float16> = true;
+constexpr float kTaserFirstLift = 0x1p60f, kTaserMostLifted = 0x1p15f;   // (products of half precision numbers, 2^39 at most, stay finite with it)
+// The factor that brings a magnitude into 2^7 .. 2^8.
+__device__ inline float taser_relift(float most) { return ldexpf(1.f, 134 - (int)(__builtin_bit_cast(uint32_t, most) >> 23)); }
+// 1 / a power of two.
+__device__ inline float taser_unlift(float lift) { return __builtin_bit_cast(float, 0x7f000000u - __builtin_bit_cast(uint32_t, lift)); }
+
 // ---- tiles ----------------------------------------------------------------------------------------------------------
 // A tile holds ROWS rows of DP elements (the head size rounded up, the rest zeros) as 16-byte pieces. Piece c of row r lies
 // at place c ^ taser_swizzle(r). 256 bytes of LDS are read at a time: one piece of 16 neighboring rows (or two neighboring pieces of 8),

@@ -137,6 +137,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
     const float scale2 = a.scale * kLog2e;
+    constexpr bool LIFTED = taser_lifted<T>;
+    float lift = LIFTED ? kTaserFirstLift : 1.f;   // of the row's dx and sums
 
     // As in the forward pass: one bias for the tile goes into the row's constant, others into the scores.
     float tile_bias = 0.f;
@@ -189,11 +191,29 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
             for (int r = 0; r < 16; ++r)
                 if (!((bits >> (8 * (r >> 2) + (r & 3))) & 1)) s[r] = -INFINITY;
         }
+        const float less = LIFTED ? mine[2] * lift : mine[2];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float p = __builtin_amdgcn_exp2f(fmaf(s[r], by, plus));
-            s[r] = p * (dp[r] - mine[2]);
+            s[r] = p * (LIFTED ? fmaf(dp[r], lift, -less) : dp[r] - less);
         }
+        if constexpr (LIFTED) {
+            float most = fabsf(s[0]);
+#pragma unroll
+            for (int r = 1; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
+            most = taser_halves_max(most);
+            if (__any(most >= kTaserMostLifted)) {
+                const float again = most >= kTaserMostLifted ? taser_relift(most) : 1.f;
+                lift *= again;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] *= again;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[d][r] *= again;
+            }
+        }
+        const float down = LIFTED ? taser_unlift(lift) : 1.f;
         if constexpr (BIAS) {
             if (low != high) {   // a row's two lanes add one after the other: the sums have one order
                 const int64_t* range = ranges[turn & 3];
@@ -217,7 +237,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
 #pragma unroll
                             for (int i = 0; i < 4; ++i) y[i] = my_sums[bucket[i]][lane & 31];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) my_sums[bucket[i]][lane & 31] = y[i] + x[i];
+                            for (int i = 0; i < 4; ++i) my_sums[bucket[i]][lane & 31] = y[i] + x[i] * down;
                         }
                         taser_next_turn();
                     }
@@ -227,7 +247,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x += s[r];
                 x = taser_halves_sum(x);
-                if (half == 0) my_sums[low][lane] = sum_before + x;
+                if (half == 0) my_sums[low][lane] = sum_before + x * down;
             }
         }
 #pragma unroll
@@ -291,6 +311,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
     if (!real) return;
     float* part = part_dq ? part_dq + (split * (int64_t)a.batch * a.queries * a.heads + at_row) * a.dim : nullptr;
     T* to = dq + at_row * a.dim;
+    const float back = LIFTED ? a.scale * taser_unlift(lift) : a.scale;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -299,7 +320,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
             T x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float y = acc[d][4 * j + i] * a.scale;
+                const float y = acc[d][4 * j + i] * back;
                 x[i] = (T)y;
                 if (part && e + i < a.dim) part[e + i] = y;
             }
@@ -418,8 +439,9 @@ __global__ __launch_bounds__(512, (ND <= 2 && sizeof(T) == 2 ? 4 : 2)) void atte
         }
     };
 
-    // Weights are at most 1: in half precision they are 2^14 times as large where dv's product takes them.
-    constexpr float lift = std::is_same_v<T, _Float16> ? 16384.f : 1.f;
+    // Weights are at most 1: in half precision they are 2^14 times as large where dv's product takes them. dx has a factor a state.
+    constexpr bool LIFTED = taser_lifted<T>;
+    float lift = !LIFTED ? 1.f : second ? kTaserFirstLift : 0x1p14f;
     const TaserRowsAt<T, DP> rows_at(lane);
     const TaserColumnsAt<T, DP> columns_at(lane);
     taser_f16 sum[ND];   // of dv, or dk
@@ -516,14 +538,30 @@ __global__ __launch_bounds__(512, (ND <= 2 && sizeof(T) == 2 ? 4 : 2)) void atte
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[n][4 * j + i] = w[i] * (x[n][4 * j + i] - t[i]);
                 }
+            if constexpr (LIFTED) {
+                float most = 0.f;
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(x[n][r]));
+                most = taser_halves_max(most);
+                if (__any(most * lift >= kTaserMostLifted)) {
+                    const float before = lift;
+                    if (most * lift >= kTaserMostLifted) lift = taser_relift(most);
+                    const float again = lift * taser_unlift(before);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) sum[d][r] *= again;
+                }
+            }
         }
         const char* from = second ? q : y;
-        const float up = second ? 1.f : lift;
 #pragma unroll
         for (int n = 0; n < NS; ++n)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const taser_frag<T> w = taser_operand<T>(x[n], h, up);
+                const taser_frag<T> w = taser_operand<T>(x[n], h, lift);
 #pragma unroll
                 for (int d = 0; d < ND; ++d) taser_mma(sum[d], columns_at.operand(from, 32 * n + 16 * h, d), w);
             }
@@ -561,7 +599,7 @@ __global__ __launch_bounds__(512, (ND <= 2 && sizeof(T) == 2 ? 4 : 2)) void atte
 
     if (state >= a.keys) return;
     const int64_t at = (((int64_t)b * a.keys + state) * a.kv_heads + hk) * a.dim, all = (int64_t)a.batch * a.keys * a.kv_heads * a.dim;
-    const float by = second ? a.scale : 1.f / lift;
+    const float by = second ? a.scale * taser_unlift(lift) : taser_unlift(lift);
     T* to = (second ? dk : dv) + at;
     float* part = part_dk ? (second ? part_dk : part_dv) + split * all + at : nullptr;
 #pragma unroll

@@ -486,3 +486,82 @@ def test_nan_of_a_query_reaches_its_row_alone(kind):
         for name, x in (("dk", grads[1]), ("dv", grads[2])):
             assert torch.isnan(x[states]).all() and torch.isfinite(x[~states]).all(), (name, Lq, Lk)
     assert cut == {"not", "few", "many"}
+
+
+def _lift_cases():
+    for scale in (2.0 ** -10, 2.0 ** -13, 2.0 ** -16):
+        for Lq, H, Hk, d, buckets in ((160, 2, 1, 64, 0), (1, 4, 2, 128, 0), (130, 2, 2, 80, 6)):
+            yield scale, Lq, H, Hk, d, buckets
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+@pytest.mark.parametrize("scale,Lq,H,Hk,d,buckets", list(_lift_cases()))
+def test_small_gradients_keep_their_digits(kind, scale, Lq, H, Hk, d, buckets):
+    """A mean loss's dout over many states: a weight's gradient is far below the smallest float16 numbers, sums of them are not. Beside the
+    bound of each element: the roundings of the terms (dx, at most u each) and of the result are independent, and so are the terms, so
+    the norm of the errors is some u / 3^0.5 * 2^0.5 of the result's, 4 u with all of 32 bits and the bound's own slack."""
+    c = _case(kind, 1, Lq, 2100, H, Hk, d, buckets=buckets)
+    c["dout"] = (c["dout"].float() * scale).to(KINDS[kind])
+    c["q"] = c["q"] / 16          # as large products as ever, and results that are no subnormal numbers themselves
+    c["kv"][:, :, 0] *= 16
+    got = _run(c)
+    want, off = _lifted(c)
+    _near(got, want, off, (scale, Lq))
+    x = got["dq"].double().cpu().numpy()
+    assert np.linalg.norm(x - want["dq"]) <= 4 * O.U[kind] * np.linalg.norm(want["dq"])
+
+
+def _lifted(c):
+    f = lambda t: t.double().numpy()
+    table = bucket = None
+    if c["bias"]:
+        t, bounds, qp, kp = c["bias"]
+        table, bucket = f(t), [O.buckets(bounds.tolist(), qp[b].tolist(), kp[b].tolist()) for b in range(len(qp))]
+    kv = f(c["kv"])
+    return O.attention(f(c["q"]), kv[:, :, 0], kv[:, :, 1], c["kind"], c["lengths"], c["mask"], table, bucket, c.get("scale"), f(c["dout"]), lifted=True)
+
+
+@gpu
+def test_small_gradients_of_states():
+    """The same of dk: rows of queries 16 times as large."""
+    for scale, Lq, H, Hk, d, buckets in _lift_cases():
+        c = _case("float16", 1, Lq, 2100, H, Hk, d, buckets=buckets)
+        c["dout"] = (c["dout"].float() * scale).half()
+        c["q"] *= 16
+        c["kv"][:, :, 0] /= 16
+        got = _run(c)
+        want, off = _lifted(c)
+        _near(got, want, off, (scale, Lq))
+        x = got["dk"].double().cpu().numpy()
+        rel = np.linalg.norm(x - want["dk"]) / np.linalg.norm(want["dk"])
+        sub = 2.0 ** -25 * x.size ** 0.5 / np.linalg.norm(want["dk"])   # results below 2^-14 are multiples of 2^-24
+        assert rel <= 4 * O.U["float16"] + sub, (scale, Lq, rel, sub)
+
+
+@gpu
+def test_large_gradients_do_not_overflow_between_the_products():
+    """Loss scaling: dx passes float16's largest number, dq, dk and dv do not."""
+    for Lq, H, Hk, d, buckets in ((3, 2, 1, 64, 0), (2, 2, 1, 128, 5), (40, 4, 4, 80, 0)):
+        c = _case("float16", 2, Lq, 200, H, Hk, d, buckets=buckets, lengths=[2, 3])
+        c["dout"] *= 2.0 ** (13 if Lq < 40 else 10)
+        c["kv"][:, :, 1] *= 2.0 if Lq < 40 else 16.0
+        c["q"] /= 256
+        c["kv"][:, :, 0] /= 256
+        got = _run(c)
+        want, off = _lifted(c)
+        _near(got, want, off, Lq)
+
+
+@gpu
+def test_gradients_that_grow_and_shrink_along_the_states_and_rows():
+    """40 powers of two from one end to the other: the factor of float16 follows."""
+    for Lq, Lk, H, Hk, d, buckets in ((200, 700, 2, 1, 64, 0), (1, 2000, 2, 2, 64, 4), (300, 90, 2, 1, 128, 0)):
+        for way in (1, -1):
+            c = _case("float16", 1, Lq, Lk, H, Hk, d, buckets=buckets)
+            along = lambda n: 2.0 ** (way * (torch.arange(n) * (20.0 / n) - 10)).double()
+            c["kv"][:, :, 1] = (c["kv"][:, :, 1].double() * along(Lk)[None, :, None, None]).half()
+            c["dout"] = (c["dout"].double() * along(Lq)[None, :, None, None] * 2.0 ** -4).half()
+            got = _run(c)
+            want, off = _lifted(c)
+            _near(got, want, off, (Lq, way))
