@@ -610,7 +610,7 @@ __global__ __launch_bounds__(512, (ND <= 2 && sizeof(T) == 2 ? 4 : 2)) void atte
             T y[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float one = sum[d][4 * j + i] * by;
+                const float one = real ? sum[d][4 * j + i] * by : 0.f;   // (a NaN among the queries is no masked state's)
                 y[i] = (T)one;
                 if (part && e + i < a.dim) part[e + i] = one;
             }

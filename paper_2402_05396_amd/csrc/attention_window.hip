@@ -381,15 +381,22 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
         auto write = [&](int n, const float (&x)[E], const float (&y)[E]) {
             if (!w.inside || w.turn_state(n) >= a.keys) return;
             const int64_t to = (((int64_t)w.b * a.keys + w.turn_state(n)) * a.kv_heads + w.hk) * a.dim;
+            const bool part = w.turn_seen(n);   // (a NaN among the queries is no masked state's)
+            float kept_x[E], kept_y[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                kept_x[i] = part ? x[i] : 0.f;
+                kept_y[i] = part ? y[i] : 0.f;
+            }
             if (w.at == w.c * E) {
-                store_values<T, E>(dk + to + w.at, x);
-                store_values<T, E>(dv + to + w.at, y);
+                store_values<T, E>(dk + to + w.at, kept_x);
+                store_values<T, E>(dv + to + w.at, kept_y);
             } else {
 #pragma unroll
                 for (int i = 0; i < E; ++i)
                     if (w.at + i >= w.c * E) {
-                        dk[to + w.at + i] = (T)x[i];
-                        dv[to + w.at + i] = (T)y[i];
+                        dk[to + w.at + i] = (T)kept_x[i];
+                        dv[to + w.at + i] = (T)kept_y[i];
                     }
             }
         };

@@ -565,3 +565,25 @@ def test_gradients_that_grow_and_shrink_along_the_states_and_rows():
             got = _run(c)
             want, off = _lifted(c)
             _near(got, want, off, (Lq, way))
+
+
+def _run_any(c):
+    q, k, v, dout, more = _device(c)
+    out, stats = T.cross_attention(q, k, v, want_stats=True, **more)
+    dq, dk, dv, dtable = T.cross_attention_grad(dout, q, k, v, out, stats, **more)
+    return dict(out=out, dq=dq, dk=dk, dv=dv, dtable=dtable)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_states_without_part_have_no_gradient_whatever_the_queries_hold(kind):
+    for Lq, Lk, d in ((1, 60, 64), (9, 40, 50), (4, 64, 128), (1, 300, 64), (200, 300, 64), (130, 90, 30)):
+        c = _case(kind, 3, Lq, Lk, 4, 2, d, buckets=8, lengths=[Lk, 17, 0], mask=0.6)
+        seen = c["mask"] & (torch.arange(Lk)[None] < c["lengths"][:, None])
+        c["q"][:, 0, 0, 3] = float("nan")
+        c["dout"][:, -1, 2, 1] = float("inf")
+        got = _run_any(c)
+        for name in ("dk", "dv"):
+            assert not got[name][~seen].any(), (name, Lq, Lk, d)
+        assert not got["out"][2].any() and not got["dq"][2].any()
+        assert torch.isnan(got["dk"][seen][:, 0]).all()
