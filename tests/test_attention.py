@@ -500,7 +500,8 @@ def _lift_cases():
 def test_small_gradients_keep_their_digits(kind, scale, Lq, H, Hk, d, buckets):
     """A mean loss's dout over many states: a weight's gradient is far below the smallest float16 numbers, sums of them are not. Beside the
     bound of each element: the roundings of the terms (dx, at most u each) and of the result are independent, and so are the terms, so
-    the norm of the errors is some u / 3^0.5 * 2^0.5 of the result's, 4 u with all of 32 bits and the bound's own slack."""
+    the norm of the errors is some u / 3^0.5 * 2^0.5 of the result's, 4 u with all of 32 bits and the bound's own slack, and what results
+    below 2^-14, multiples of 2^-24 in float16, are off by."""
     c = _case(kind, 1, Lq, 2100, H, Hk, d, buckets=buckets)
     c["dout"] = (c["dout"].float() * scale).to(KINDS[kind])
     c["q"] = c["q"] / 16          # as large products as ever, and results that are no subnormal numbers themselves
@@ -509,7 +510,7 @@ def test_small_gradients_keep_their_digits(kind, scale, Lq, H, Hk, d, buckets):
     want, off = _lifted(c)
     _near(got, want, off, (scale, Lq))
     x = got["dq"].double().cpu().numpy()
-    assert np.linalg.norm(x - want["dq"]) <= 4 * O.U[kind] * np.linalg.norm(want["dq"])
+    assert np.linalg.norm(x - want["dq"]) <= 4 * O.U[kind] * np.linalg.norm(want["dq"]) + O.TINY[kind] * x.size ** 0.5
 
 
 def _lifted(c):
