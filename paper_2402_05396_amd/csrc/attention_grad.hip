@@ -81,6 +81,11 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
     }
     taser_f4 mine = {INFINITY, 0.f, 0.f, 0.f};
     if (real) mine = info[at_row];
+    if (mine[0] == INFINITY && mine[1] == 0.f) {   // a row without states: whatever comes back to it
+        mine[2] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) dy[c] = taser_frag<T>{};
+    }
     int64_t query_pos = 0, bound = 0, query_low = 0, query_high = 0;
     uint64_t foldable = 0;
     TaserNear map;

@@ -339,9 +339,10 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
             float x = w.own(s) * a.scale;
             const float dp = w.own(d);
             if (a.table) x += (float)((const T*)a.table)[(int64_t)head * a.buckets + bucket];
-            const float p = mine && sum != 0.f ? __builtin_amdgcn_exp2f((x - top) * kLog2e) / sum : 0.f;
-            const float t = group_sum<64>(mine ? p * dp : 0.f);
-            const float dx = mine ? p * (dp - t) : 0.f;
+            const bool part = mine && sum != 0.f;   // (a row without states gives zeros, whatever comes back to it)
+            const float p = part ? __builtin_amdgcn_exp2f((x - top) * kLog2e) / sum : 0.f;
+            const float t = group_sum<64>(part ? p * dp : 0.f);
+            const float dx = part ? p * (dp - t) : 0.f;
             if (a.table) {   // a lane a bucket: the states' dx pass by in their order
                 float add = 0.f;
                 for (uint64_t left = w.seen; left; left &= left - 1) {

@@ -588,3 +588,15 @@ def test_states_without_part_have_no_gradient_whatever_the_queries_hold(kind):
             assert not got[name][~seen].any(), (name, Lq, Lk, d)
         assert not got["out"][2].any() and not got["dq"][2].any()
         assert torch.isnan(got["dk"][seen][:, 0]).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_query_that_the_bias_leaves_without_states_has_no_gradient(kind):
+    """Minus infinity in all of a head's table: its rows give zeros whatever comes back to them."""
+    for Lq, Lk in ((1, 40), (6, 40), (1, 400), (140, 100)):
+        c = _case(kind, 2, Lq, Lk, 4, 2, 64, buckets=6)
+        c["bias"][0][1] = -float("inf")
+        c["dout"][:, :, 1] = float("nan")
+        got = _run_any(c)
+        assert not got["out"][:, :, 1].any() and not got["dq"][:, :, 1].any() and not got["dtable"][1].any()
