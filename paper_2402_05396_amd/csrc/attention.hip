@@ -539,7 +539,8 @@ int taser_attention_args(const taser_attention* p, const char* what, TaserAttent
     const int size = p->type == TASER_F32 ? 4 : 2, whole = 16 / size;
     bool direct = a->dim % whole == 0 && ((uintptr_t)p->k | (uintptr_t)p->v) % 16 == 0;
     for (int i = 0; i < 3; ++i) direct = direct && p->k_strides[i] % whole == 0 && p->v_strides[i] % whole == 0;
-    // a tile of 64 states within the reach of its descriptor
+    // a tile of 64 states within the reach of its descriptor, and none of those past its last one
+    direct = direct && (p->keys < 2 || (p->k_strides[1] >= a->dim && p->v_strides[1] >= a->dim));
     direct = direct && p->k_strides[1] >= 0 && p->v_strides[1] >= 0 && p->k_strides[1] < kTaserTileBytes / 64 / size && p->v_strides[1] < kTaserTileBytes / 64 / size;
     a->direct = direct;
     return TASER_OK;

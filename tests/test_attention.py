@@ -600,3 +600,22 @@ def test_a_query_that_the_bias_leaves_without_states_has_no_gradient(kind):
         c["dout"][:, :, 1] = float("nan")
         got = _run_any(c)
         assert not got["out"][:, :, 1].any() and not got["dq"][:, :, 1].any() and not got["dtable"][1].any()
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_states_that_overlap_in_memory(kind):
+    """Neighboring states share elements: what lies past the last one takes no part, though its first elements are the last one's."""
+    for Lq, Lk, d, step in ((1, 300, 64, 32), (150, 300, 64, 32), (200, 90, 32, 8), (1, 50, 64, 32), (1, 300, 64, 0)):
+        lengths = [Lk - 70, 17, 1] if Lk > 70 else [Lk - 7, 17, 1]
+        c = _case(kind, 3, Lq, Lk, 2, 2, d, lengths=lengths)
+        g = torch.Generator().manual_seed(2)
+        flat = torch.randn((3, 2, Lk * step + d), generator=g).to(KINDS[kind])
+        view = lambda f: f.as_strided((3, Lk, 2, d), (2 * (Lk * step + d), step, Lk * step + d, 1))
+        dirty = flat.clone()
+        for b, n in enumerate(lengths):
+            dirty[b, :, (n - 1) * step + max(step, 1):] = float("inf") if step else 1.0   # the last state's end, and all past it
+        q, lens, k, v = c["q"].cuda(), c["lengths"].cuda(), view(flat.cuda()), view(dirty.cuda())
+        past = torch.arange(Lk, device="cuda")[None, :, None, None] >= lens[:, None, None, None]
+        out, want = T.cross_attention(q, k, v, lengths=lens), T.cross_attention(q, k.contiguous(), v.masked_fill(past, 0).contiguous(), lengths=lens)
+        assert torch.equal(torch.isnan(out), torch.isnan(want)) and torch.equal(torch.nan_to_num(out), torch.nan_to_num(want)), (Lq, Lk, d, step)
