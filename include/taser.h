@@ -490,7 +490,9 @@ void taser_selector_free(taser_selector* s);
  * Both work in `work`, device memory of the caller's (16-byte aligned, contents
  * arbitrary, free again when the call's kernels have run), as much as
  * taser_cross_attention_bytes says (either out-pointer may be NULL) for the
- * same block. Both only launch kernels.
+ * same block. Both only launch kernels; a call whose kernels would need 2^32
+ * threads (as do more than 2^26 windows, or 2^23 entries and key heads with longer
+ * states) is refused before the first, here and below.
  * Sums, softmax statistics and bias are held in 32 bits; softmax weights and
  * their gradients are rounded to `type` where they enter a matrix product (for
  * float16 times powers of two that keep small ones and large ones in its range).

@@ -448,7 +448,9 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
     a.row_tiles = (a.rows + S::kRows - 1) / S::kRows;
     const int64_t items = (int64_t)a.batch * a.kv_heads * a.splits * a.row_tiles;
     const dim3 grid((unsigned)taser_stretched_grid(items)), block(64 * S::kWaves);
-    if (items > INT32_MAX / 2) return taser_fail(TASER_E_RANGE, "cross_attention: too many queries and batch entries for one launch");
+    const bool few = a.splits <= 16;
+    if (!taser_launch_fits(taser_stretched_grid(items), block.x) || (a.splits > 1 && !taser_launch_fits(few ? (rows * a.dim + 255) / 256 : rows, few ? 256 : 1024)))
+        return taser_fail(TASER_E_RANGE, "cross_attention: too many queries and batch entries for one launch");
     {
         TaserProfileSpan span(stream, "attention");
         auto run = [&](auto bias, auto fine) {
@@ -467,7 +469,7 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
     }
     if (a.splits > 1) {
         TaserProfileSpan span(stream, "attention_join");
-        if (a.splits <= 16)
+        if (few)
             attention_join_few_kernel<T><<<dim3((unsigned)((rows * a.dim + 255) / 256)), 256, 0, stream>>>(part_out, part_stats, rows, a.dim, a.splits, (T*)out, stats, a.stat_floats);
         else
             attention_join_kernel<T><<<dim3((unsigned)rows), 1024, 0, stream>>>(part_out, part_stats, rows, a.dim, a.splits, (T*)out, stats, a.stat_floats);
@@ -510,7 +512,8 @@ int taser_attention_args(const taser_attention* p, const char* what, TaserAttent
     if (p->heads % p->kv_heads) return taser_fail(TASER_E_ARG, "%s: %d query heads cannot share %d key heads evenly", what, p->heads, p->kv_heads);
     if (p->head_dim > TASER_MAX_HEAD_DIM) return taser_fail(TASER_E_RANGE, "%s: heads of %d elements (at most %d)", what, p->head_dim, TASER_MAX_HEAD_DIM);
     const int64_t group = p->heads / p->kv_heads, limit = (int64_t)1 << 31;
-    if (p->batch >= limit || p->queries * group >= limit - 128 || p->keys >= limit - 128 || (p->queries && p->batch * p->heads >= ((int64_t)1 << 39) / p->queries))
+    if (p->batch >= limit || p->queries * group >= limit - 128 || p->keys >= limit - 128 || (p->queries && p->batch * p->heads >= ((int64_t)1 << 39) / p->queries) ||
+        (p->keys && p->batch * p->kv_heads >= ((int64_t)1 << 39) / p->keys))
         return taser_fail(TASER_E_RANGE, "%s: too many queries, states or batch entries", what);
     if (!(p->scale > 0.f) || std::isinf(p->scale)) return taser_fail(TASER_E_ARG, "%s: the scale must be positive and finite", what);
     const bool queries = p->batch && p->queries;

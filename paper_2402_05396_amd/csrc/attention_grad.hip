@@ -707,6 +707,14 @@ Plan plan(const TaserAttentionArgs& a, int32_t type) {
     return p;
 }
 
+// Of the kernels over tiles, those of launch(); the table's has a block of 1024 a head.
+bool launches_fit(const TaserAttentionArgs& a, const Plan& p) {
+    const int64_t pairs = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.batch * a.queries * a.heads, states = pairs * a.keys * a.dim;
+    return taser_launch_fits((rows + 15) / 16, 256) && taser_launch_fits(taser_stretched_grid(pairs * p.row_tiles * p.row_splits), 256) &&
+           taser_launch_fits(taser_stretched_grid(pairs * p.state_tiles * p.state_splits), 512) &&
+           (p.row_splits == 1 || taser_launch_fits((rows * a.dim + 255) / 256, 256)) && (p.state_splits == 1 || taser_launch_fits((states + 255) / 256, 256));
+}
+
 template <typename T, int ND>
 int launch(TaserAttentionArgs& a, const Plan& p, const T* out, const float* stats, const T* dout, T* dq, T* dk, T* dv, T* dtable, char* work, hipStream_t stream) {
     const int64_t rows = (int64_t)a.batch * a.queries * a.heads, states = (int64_t)a.batch * a.keys * a.kv_heads * a.dim, pairs = (int64_t)a.batch * a.kv_heads;
@@ -811,7 +819,7 @@ extern "C" int taser_cross_attention_grad(const taser_attention* arg, const void
     if (need > work_size)
         return taser_fail(TASER_E_RANGE, "cross_attention_grad: %llu bytes of workspace, %llu needed", (unsigned long long)work_size, (unsigned long long)need);
     if (need && (!work || (uintptr_t)work % 16)) return taser_fail(TASER_E_ARG, "cross_attention_grad: null or misaligned workspace");
-    if ((int64_t)a.batch * a.kv_heads * ((int64_t)p.row_tiles * p.row_splits + (int64_t)p.state_tiles * p.state_splits) > INT32_MAX / 2)
+    if (!(window(a) || launches_fit(a, p)) || (a.table && !taser_launch_fits(a.heads, 1024)))
         return taser_fail(TASER_E_RANGE, "cross_attention_grad: too many queries, states and batch entries for one launch");
     hipStream_t stream = (hipStream_t)hip_stream;
     taser_clear_stale_hip_error();

@@ -505,6 +505,7 @@ bool taser_window_fits(const TaserAttentionArgs& a) {
 }
 
 int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out, float* stats, hipStream_t stream) {
+    if (!taser_launch_fits(((int64_t)a.batch * a.kv_heads + 3) / 4, 256)) return taser_fail(TASER_E_RANGE, "cross_attention: too many windows for one launch");
     Call c = {};
     c.out = out;
     c.stats = stats;
@@ -518,6 +519,7 @@ uint64_t taser_window_grad_bytes(const TaserAttentionArgs& a) {
 }
 
 int taser_window_attention_grad(const TaserAttentionArgs& a, int32_t type, const float* stats, const void* dout, void* dq, void* dk, void* dv, void* dtable, float* work, hipStream_t stream) {
+    if (!taser_launch_fits((grad_waves(a) + 3) / 4, 256)) return taser_fail(TASER_E_RANGE, "cross_attention_grad: too many windows for one launch");
     Call c = {};
     c.stats = const_cast<float*>(stats);
     c.dout = dout;

@@ -251,6 +251,7 @@ template <typename T> int launch(const Distances& d, const void* table, void* bi
     constexpr int EACH = 16 / sizeof(T);
     const int heads_each = d.heads * d.buckets <= 8192 ? d.heads : 8192 / d.buckets;
     const int64_t waves = d.batch * d.queries * ((d.keys + 64 * EACH - 1) / (64 * EACH));
+    if (!taser_launch_fits((waves + 3) / 4, 256)) return taser_fail(TASER_E_RANGE, "relative_bias: too many queries and batch entries for one launch");
     TaserProfileSpan span(stream, "relative_bias");
     relative_bias_kernel<T, EACH><<<dim3((unsigned)((waves + 3) / 4), (unsigned)((d.heads + heads_each - 1) / heads_each)), 256, sizeof(float) * heads_each * d.buckets, stream>>>(
         d, (const T*)table, (T*)bias, heads_each);

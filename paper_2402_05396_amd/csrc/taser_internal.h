@@ -16,6 +16,9 @@ int taser_fail_hip(hipError_t e, const char* what);
 // points that check their kernel launches with it call this first.
 inline void taser_clear_stale_hip_error() { (void)hipGetLastError(); }
 
+// A launch has fewer than 2^32 threads along a dimension. Entry points check that of all their kernels before they launch the first.
+inline bool taser_launch_fits(int64_t blocks, int64_t threads) { return blocks <= INT64_MAX / threads && blocks * threads < (int64_t)1 << 32; }
+
 #define TASER_HIP_TRY(expr)                                    \
     do {                                                       \
         hipError_t taser_e_ = (expr);                          \

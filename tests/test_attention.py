@@ -619,3 +619,19 @@ def test_states_that_overlap_in_memory(kind):
         past = torch.arange(Lk, device="cuda")[None, :, None, None] >= lens[:, None, None, None]
         out, want = T.cross_attention(q, k, v, lengths=lens), T.cross_attention(q, k.contiguous(), v.masked_fill(past, 0).contiguous(), lengths=lens)
         assert torch.equal(torch.isnan(out), torch.isnan(want)) and torch.equal(torch.nan_to_num(out), torch.nan_to_num(want)), (Lq, Lk, d, step)
+
+
+def test_calls_that_no_launch_can_take_are_refused_before_the_first():
+    """Fewer than 2^32 threads to a launch: windows four to a block of 256, tiles a block each (of 512 for the states' gradients), a block of
+    1024 for a head of the table's."""
+    L, one, E_RANGE = T.lib(), ctypes.c_void_p(16), -2
+    forward = lambda a: L.taser_cross_attention(ctypes.byref(a), one, one, one, 1 << 60, None)
+    backward = lambda a: L.taser_cross_attention_grad(ctypes.byref(a), *[one] * 8, 1 << 60, None)
+    tiles = dict(heads=8, kv_heads=8, head_dim=4, queries=1, keys=10)
+    for call, a in ((forward, _block(batch=2 ** 21, **tiles)), (backward, _block(batch=2 ** 20, **tiles)), (backward, _block(batch=2 ** 20, **dict(tiles, queries=0))),
+                    (forward, _block(batch=2 ** 24, heads=4, kv_heads=4, queries=1)), (backward, _block(batch=2 ** 24, heads=4, kv_heads=4, queries=1)),
+                    (forward, _block(batch=2 ** 25, queries=1)),
+                    (backward, _block(batch=1, heads=2 ** 22, kv_heads=2 ** 22, queries=1, bias_table=16, buckets=4, bounds=16, query_pos=16, key_pos=16))):
+        assert call(a) == E_RANGE and "launch" in T.last_error(), T.last_error()
+    size = ctypes.c_uint64()
+    assert L.taser_cross_attention_bytes(ctypes.byref(_block(batch=2 ** 30, heads=2 ** 10, kv_heads=2 ** 10, queries=0, keys=1)), None, ctypes.byref(size)) == E_RANGE

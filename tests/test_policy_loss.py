@@ -272,3 +272,11 @@ def test_nan_among_logits_of_minus_infinity(kind):
             a = torch.ones((3, 1), dtype=torch.int32)
             loss, logp, grad = T.policy_loss(x.cuda(), a.cuda(), torch.ones((3, 1)).cuda())
             assert torch.isnan(logp[1]).all() and torch.isnan(grad[1, 1]) and torch.isfinite(logp[[0, 2]]).all() and torch.isfinite(grad[[0, 2]]).all(), (W, at)
+
+
+def test_calls_that_no_launch_can_take_are_refused():
+    """Fewer than 2^32 threads to a launch: 16 to 64 a short row, a block of 256 or 1024 a longer one."""
+    one = ctypes.c_void_p(16)
+    for rows, width, picks in ((2 ** 28, 5, 2), (2 ** 26, 5, 40), (2 ** 24, 100, 2), (2 ** 22, 10_000, 2)):
+        p = T._PolicyBatch(0, picks, rows, width, width, 16, None, 16, 16, None, None, None, 0.2, 0.2, 0.0)
+        assert T.lib().taser_policy_loss(ctypes.byref(p), one, one, one, None) == -2 and "launch" in T.last_error(), T.last_error()

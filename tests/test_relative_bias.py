@@ -156,3 +156,11 @@ def test_argument_errors_without_a_gpu():
     assert L.taser_relative_bias_grad(block(), one, strides, one, None, 1 << 40, None) == E_ARG
     assert L.taser_relative_bias_grad(block(), one, strides, one, ctypes.c_void_p(8), 1 << 40, None) == E_ARG
     assert L.taser_relative_bias_grad(block(), one, strides, one, one, 8, None) == E_RANGE
+
+
+def test_calls_that_no_launch_can_take_are_refused():
+    """Fewer than 2^32 threads to a launch: 64 for each 256 states of a query (512 in 16 bits)."""
+    one = ctypes.c_void_p(16)
+    for batch, queries, keys in ((2 ** 26, 1, 1), (2 ** 15, 2 ** 11, 25), (2 ** 28, 16, 1), (1, 2 ** 25, 300)):
+        d = T._Distances(0, 3, 4, batch, queries, keys, 16, 16, 16, 0, 0)
+        assert T.lib().taser_relative_bias(ctypes.byref(d), one, one, None) == -2 and "launch" in T.last_error(), T.last_error()
