@@ -280,3 +280,31 @@ def test_calls_that_no_launch_can_take_are_refused():
     for rows, width, picks in ((2 ** 28, 5, 2), (2 ** 26, 5, 40), (2 ** 24, 100, 2), (2 ** 22, 10_000, 2)):
         p = T._PolicyBatch(0, picks, rows, width, width, 16, None, 16, 16, None, None, None, 0.2, 0.2, 0.0)
         assert T.lib().taser_policy_loss(ctypes.byref(p), one, one, one, None) == -2 and "launch" in T.last_error(), T.last_error()
+
+
+@gpu
+@pytest.mark.parametrize("W", [25, 300, 5000])
+def test_kl_term_of_a_policy_close_to_its_reference(W):
+    """exp(t) - t - 1 at the t that the kernel has (the returned log-probability's difference, exact where they are close): at most 16
+    roundings off. The gradient's slope, 1 - exp(t), likewise, beside those of W terms in the softmax."""
+    def term(t):   # its series, 20 terms of it, and the function itself past 1/2
+        s = np.zeros_like(t)
+        for n in range(22, 1, -1):
+            s = (s * t + 1) / n
+        return np.where(np.abs(t) < 0.5, t * t * s, np.expm1(t) - t)
+
+    for apart in (3.0, 0.7, 0.4, 0.1, 1e-2, 1e-3, 3e-4, 1e-4, 1e-6):
+        g = torch.Generator().manual_seed(W)
+        x = torch.randn((200, W), generator=g).cuda()
+        a = torch.randint(0, W, (200, 1), generator=g, dtype=torch.int32).cuda()
+        none = torch.zeros((200, 1), device="cuda")
+        _, logp, _ = T.policy_loss(x, a, none)
+        ref = logp + apart * torch.randn((200, 1), generator=g).cuda()
+        loss, again, grad = T.policy_loss(x, a, none, ref_logp=ref, kl=0.5)
+        assert torch.equal(again, logp)
+        t = (ref - logp).double().cpu().numpy()
+        want, got = 0.5 * term(t), loss.double().cpu().numpy()
+        assert (got >= 0).all() and (np.abs(got - want) <= 16 * O.E32 * want + O.END32).all(), (apart, float(np.abs(got / want - 1).max()))
+        slope, chance = -0.5 * np.expm1(t), np.exp(logp.double().cpu().numpy())
+        at = grad.double().cpu().numpy()[np.arange(200), a.cpu().numpy()[:, 0]][:, None]
+        assert (np.abs(at - slope * (1 - chance)) <= (W + 40) * O.E32 * np.abs(slope)).all(), apart
