@@ -700,6 +700,16 @@ def _pool_of(stream):
         yield
 
 
+def _result(shape, dtype, device, stream):
+    """What is written on `stream` and read on torch's current one: the former's memory, so that nothing is left to do with it elsewhere,
+    and not given back before the latter is through with it."""
+    with _pool_of(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _scratch(n, device):
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
@@ -728,8 +738,8 @@ def cross_attention(q, k, v, lengths=None, mask=None, bias=None, scale=None, wan
             return r
     a, work = _attention_block(q, k, v, lengths, mask, bias, scale), ctypes.c_uint64()
     _check(lib().taser_cross_attention_bytes(ctypes.byref(a), ctypes.byref(work), None))
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    stats = torch.empty(_stats_shape(q), dtype=torch.float32, device=q.device) if want_stats else None
+    out = _result(q.shape, q.dtype, q.device, stream)
+    stats = _result(_stats_shape(q), torch.float32, q.device, stream) if want_stats else None
     with _pool_of(stream):
         scratch = _scratch(work.value, q.device)
     _check(lib().taser_cross_attention(ctypes.byref(a), _ptr(out), _ptr(stats), _ptr(scratch), work.value, _stream(stream)))
@@ -752,8 +762,8 @@ def cross_attention_grad(dout, q, k, v, out, stats, lengths=None, mask=None, bia
     if stats.shape != _stats_shape(q):
         raise ValueError("stats must be those that cross_attention gave")
     _check(lib().taser_cross_attention_bytes(ctypes.byref(a), None, ctypes.byref(work)))
-    dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
-    dtable = None if bias is None else torch.empty(bias[0].shape, dtype=q.dtype, device=q.device)
+    dq, dk, dv = (_result(t.shape, q.dtype, q.device, stream) for t in (q, k, v))
+    dtable = None if bias is None else _result(bias[0].shape, q.dtype, q.device, stream)
     with _pool_of(stream):
         scratch = _scratch(work.value, q.device)
     _check(lib().taser_cross_attention_grad(ctypes.byref(a), _ptr(out), _ptr(stats), _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtable), _ptr(scratch), work.value,
@@ -784,7 +794,7 @@ def relative_bias(table, bounds, query_pos, key_pos, stream=None):
     d = _distance_block(table.dtype, table.shape[0], bounds, query_pos, key_pos, batch, table.device)
     if table.dim() != 2 or table.shape[1] != d.buckets:
         raise ValueError("table must be [heads, buckets], bounds one less than buckets")
-    out = torch.empty((batch, table.shape[0], d.queries, d.keys), dtype=table.dtype, device=table.device)
+    out = _result((batch, table.shape[0], d.queries, d.keys), table.dtype, table.device, stream)
     _check(lib().taser_relative_bias(ctypes.byref(d), _ptr(table), _ptr(out), _stream(stream)))
     return out
 
@@ -808,7 +818,7 @@ def relative_bias_grad(dbias, bounds, query_pos, key_pos, stream=None):
     if dbias.shape[2:] != (d.queries, d.keys):
         raise ValueError("dbias must be [B, heads, queries, keys]")
     _check(lib().taser_relative_bias_bytes(ctypes.byref(d), ctypes.byref(work)))
-    out = torch.empty((dbias.shape[1], d.buckets), dtype=dbias.dtype, device=dbias.device)
+    out = _result((dbias.shape[1], d.buckets), dbias.dtype, dbias.device, stream)
     with _pool_of(stream):
         scratch = _scratch(work.value, dbias.device)
     _check(lib().taser_relative_bias_grad(ctypes.byref(d), _ptr(dbias), (ctypes.c_int64 * 3)(*dbias.stride()[:3]), _ptr(out), _ptr(scratch), work.value, _stream(stream)))
@@ -819,9 +829,10 @@ def policy_loss(logits, actions, advantage, old_logp=None, ref_logp=None, count=
     """taser_policy_loss. logits [R, width] of float32, float16 or bfloat16 with contiguous rows; actions int32[R, picks] (-1: none);
     advantage, old_logp, ref_logp, weight float32[R, picks]; count int32[R]. Returns (loss float32[R, picks], logp float32[R, picks],
     grad of the sum of all losses, like the logits and dense, or None)."""
-    r = (_native or _bind()).policy(logits, actions, advantage, old_logp, ref_logp, count, weight, clip_low, clip_high, kl, want_grad, stream)
-    if r is not None:
-        return r
+    if stream is None:
+        r = (_native or _bind()).policy(logits, actions, advantage, old_logp, ref_logp, count, weight, clip_low, clip_high, kl, want_grad, None)
+        if r is not None:
+            return r
     _strided(logits, 2, _TYPES, "logits")
     _want(actions, torch.int32, "actions")
     if actions.dim() != 2 or actions.shape[0] != logits.shape[0]:
@@ -840,8 +851,8 @@ def policy_loss(logits, actions, advantage, old_logp=None, ref_logp=None, count=
         if count.numel() != rows:
             raise ValueError("count must hold a number for each row")
         p.count = count.data_ptr()
-    loss, logp = (torch.empty(actions.shape, dtype=torch.float32, device=logits.device) for _ in range(2))
-    grad = torch.empty((rows, width), dtype=logits.dtype, device=logits.device) if want_grad else None
+    loss, logp = (_result(actions.shape, torch.float32, logits.device, stream) for _ in range(2))
+    grad = _result((rows, width), logits.dtype, logits.device, stream) if want_grad else None
     _check(lib().taser_policy_loss(ctypes.byref(p), _ptr(loss), _ptr(logp), _ptr(grad), _stream(stream)))
     return loss, logp, grad
 

@@ -635,3 +635,35 @@ def test_calls_that_no_launch_can_take_are_refused_before_the_first():
         assert call(a) == E_RANGE and "launch" in T.last_error(), T.last_error()
     size = ctypes.c_uint64()
     assert L.taser_cross_attention_bytes(ctypes.byref(_block(batch=2 ** 30, heads=2 ** 10, kv_heads=2 ** 10, queries=0, keys=1)), None, ctypes.byref(size)) == E_RANGE
+
+
+@gpu
+@pytest.mark.parametrize("name", ["cross_attention", "cross_attention_grad", "relative_bias", "policy_loss"])
+def test_results_of_another_stream_are_that_streams_memory(name):
+    """What the current stream gave back a moment ago, perhaps with work on it still to come, is not written by the other one; and a result
+    given back while the current stream is at work with it is not written again by the other one's next call."""
+    q, k = torch.randn((1, 1 << 16, 1, 64), device="cuda"), torch.randn((1, 4, 1, 64), device="cuda")
+    out, stats = T.cross_attention(q, k, k, want_stats=True)
+    pos, table, bounds = torch.arange(2048, device="cuda")[None], torch.randn((1, 3), device="cuda"), torch.tensor([0, 9], device="cuda")
+    logits, action, one = torch.randn((1, 1 << 22), device="cuda"), torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.ones((1, 1), device="cuda")
+    call = {"cross_attention": lambda **a: T.cross_attention(q, k, k, **a), "cross_attention_grad": lambda **a: T.cross_attention_grad(out, q, k, k, out, stats, **a)[0],
+            "relative_bias": lambda **a: T.relative_bias(table, bounds, pos, pos, **a), "policy_loss": lambda **a: T.policy_loss(logits, action, one, **a)[2]}[name]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    want = call()
+    assert want.numel() * 4 == 1 << 24
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    gone = torch.empty_like(want)
+    place = gone.data_ptr()
+    del gone
+    got = call(stream=side)
+    assert got.data_ptr() != place
+    side.synchronize()
+    assert torch.equal(got, want)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(10_000_000)
+    place = got.data_ptr()
+    del got
+    assert call(stream=side).data_ptr() != place
+    torch.cuda.synchronize()
