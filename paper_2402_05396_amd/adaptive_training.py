@@ -18,7 +18,7 @@ import paper_2402_05396_amd as T
 
 
 class CrossAttention(torch.autograd.Function):
-    """cross_attention with its gradient, a table of biases by distance included."""
+    """cross_attention with its gradient, a table of biases by distance included. (A gradient of the gradient is an error.)"""
 
     @staticmethod
     def forward(ctx, q, k, v, table, bounds, query_pos, key_pos, lengths):
@@ -27,6 +27,7 @@ class CrossAttention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
         q, k, v, table, bounds, query_pos, key_pos, lengths, out, stats = ctx.saved_tensors
         dq, dk, dv, dtable = T.cross_attention_grad(dout.contiguous(), q, k, v, out, stats, lengths=lengths, bias=(table, bounds, query_pos, key_pos))
@@ -34,7 +35,7 @@ class CrossAttention(torch.autograd.Function):
 
 
 class PolicyLoss(torch.autograd.Function):
-    """The sum of policy_loss over rows and picks; its gradient comes with the forward pass."""
+    """The sum of policy_loss over rows and picks; its gradient comes with the forward pass. (Its gradient is an error.)"""
 
     @staticmethod
     def forward(ctx, logits, actions, advantage, old_logp, count):
@@ -43,6 +44,7 @@ class PolicyLoss(torch.autograd.Function):
         return loss.sum()
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dloss):
         return ctx.saved_tensors[0] * dloss, None, None, None, None
 

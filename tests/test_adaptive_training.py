@@ -61,3 +61,21 @@ def test_the_policy_loss_as_a_function():
     (dwant,) = torch.autograd.grad(2 * loss, wide)
     assert abs(got.item() - loss.item()) < r * picks * 8 * 40 * 2.0 ** -24
     assert (dgot.double() - dwant).abs().max().item() < 2 * picks * 8 * 60 * 2.0 ** -24
+
+
+def test_gradients_of_gradients_are_refused():
+    """Where the functions' own gradients are not differentiated, other terms of the sum would be all that is left."""
+    from paper_2402_05396_amd.adaptive_training import CrossAttention, PolicyLoss
+    rng = torch.Generator(device="cuda").manual_seed(5)
+    q, k = (torch.randn((3, n, 2, 16), generator=rng, device="cuda").requires_grad_() for n in (1, 5))
+    table = torch.zeros((2, 3), device="cuda")
+    now, then = torch.zeros((3, 1), dtype=torch.int64, device="cuda"), torch.zeros((3, 5), dtype=torch.int64, device="cuda")
+    out = CrossAttention.apply(q, k, k, table, torch.tensor([1, 2], device="cuda"), now, then, torch.full((3,), 5, dtype=torch.int32, device="cuda"))
+    (dq,) = torch.autograd.grad((out * out).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (dq * q).sum().backward()
+    x = torch.randn((3, 5), generator=rng, device="cuda").requires_grad_()
+    loss = PolicyLoss.apply(x, torch.zeros((3, 1), dtype=torch.int32, device="cuda"), torch.ones((3, 1), device="cuda"), torch.zeros((3, 1), device="cuda"), None)
+    (dx,) = torch.autograd.grad(loss * loss, x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (dx * x).sum().backward()
