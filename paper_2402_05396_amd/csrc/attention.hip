@@ -25,8 +25,8 @@ template <typename T, int DP, bool SHARED> struct Shape {
     static constexpr int kRows = SHARED ? 32 * kWaves : 32;
 };
 
-// FINE: the output is exact to 32 bits before it is rounded, for a gradient over few states, whose <dout, out> would have the weights'
-// roundings in it otherwise (over many states they average out).
+// FINE: the output is exact to 32 bits before it is rounded. Without it 16-bit weights' roundings are in it (1.4 times as far off as the
+// rounded output need be, where they average out over many states) and in the gradient's <dout, out>.
 template <typename T, int ND, bool SHARED, bool BIAS, bool FINE>
 __global__ __launch_bounds__((64 * Shape<T, taser_row_elements(ND), SHARED>::kWaves), (SHARED && sizeof(T) == 2 && !(FINE && ND > 2) ? 2 : 1)) void attention_kernel(const TaserAttentionArgs a, T* out, float* stats, float* part_out,
                                                                                       float* part_stats, int64_t work) {
@@ -458,12 +458,19 @@ int launch(TaserAttentionArgs& a, void* out, float* stats, float* work, hipStrea
         };
         const std::true_type yes;
         const std::false_type no;
-        if (sizeof(T) == 2 && a.keys <= kFineStates) {
-            if (a.table) run(yes, std::bool_constant<sizeof(T) == 2>());
-            else run(no, std::bool_constant<sizeof(T) == 2>());
+        constexpr bool narrow = sizeof(T) == 2;
+        const std::bool_constant<narrow> fine;
+        const std::bool_constant<narrow && !SHARED> rest;   // (what few rows have in any case)
+        // Few rows wait for the states, and what the second product adds is little: 32 x 1 query, 8192 states 164.3 us, 165.0 with it; 2 x 3, 100 001
+        // states 55.2, 57.1; 8 x 2, 3000 states 36.0, 38.8. Many rows wait for the products: 4 x 2048 x 4096 271 us, 442 with it (heads of 64: 158, 212);
+        // up to 128 states, where single weights' roundings do not average out, they have it all the same. With and without `stats` alike: the
+        // output's bits do not depend on whether a gradient will be asked for.
+        if (!SHARED || a.keys <= kFineStates) {
+            if (a.table) run(yes, fine);
+            else run(no, fine);
         } else {
-            if (a.table) run(yes, no);
-            else run(no, no);
+            if (a.table) run(yes, rest);
+            else run(no, rest);
         }
         TASER_HIP_TRY(hipGetLastError());
     }

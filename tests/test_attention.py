@@ -667,3 +667,19 @@ def test_results_of_another_stream_are_that_streams_memory(name):
     del got
     assert call(stream=side).data_ptr() != place
     torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+@pytest.mark.parametrize("size", [(2, 1, 200, 8, 2, 64, 8), (3, 2, 3000, 4, 4, 128, 0), (1, 3, 20_000, 8, 2, 80, 5), (2, 20, 700, 3, 1, 50, 0), (40, 1, 60, 2, 1, 64, 4), (2, 150, 128, 2, 1, 64, 0)])
+def test_weights_of_few_rows_or_states_are_multiplied_as_32_bit_numbers(kind, size):
+    """A weight's rounding to the type is multiplied too, and is itself rounded: u^2 of the weight is what is left beside the roundings of
+    single precision and the output's one."""
+    B, Lq, Lk, H, Hk, d, buckets = size
+    c = _case(kind, B, Lq, Lk, H, Hk, d, buckets=buckets)
+    got = _run(c, train=False)["out"].double().cpu().numpy()
+    want, off = _oracle(dict(c, kind="float32"), train=False)
+    v = c["kv"][:, :, 1].double().abs().numpy().repeat(H // Hk, axis=2)
+    left = off["out"] + O.U[kind] ** 2 * v.max((1, 3))[:, None, :, None] + O.TINY[kind] * 2.0 ** -14 * v.sum(1)[:, None]
+    far = np.abs(got - want["out"]) - (left + O.U[kind] * (np.abs(want["out"]) + left) + O.TINY[kind])
+    assert far.max() <= 0, float(far.max())
