@@ -136,6 +136,18 @@ template <typename T, int E> __device__ inline Chunk<T, E> load_chunk(const T* r
     }
     return c;
 }
+// Values rounded to the type, their 16 bytes by a mask of 4.
+template <typename T, int E> __device__ inline Chunk<T, E> masked_chunk(const float (&x)[E], uint32_t mask) {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    Chunk<T, E> c;
+#pragma unroll
+    for (int i = 0; i < E; ++i) c.x[i] = (T)x[i];
+    words u;
+    __builtin_memcpy(&u, c.x, 16);
+    u &= mask;
+    __builtin_memcpy(c.x, &u, 16);
+    return c;
+}
 template <typename T, int N> __device__ inline void store_values(T* to, const float (&x)[N]) {
     T y[N];
 #pragma unroll
@@ -378,26 +390,25 @@ __global__ __launch_bounds__(256) void window_grad_kernel(const TaserAttentionAr
             for (int i = 0; i < LEFT; ++i) left[i] = sums[i];
             if (w.inside) store_values<T, LEFT>(dq + row * a.dim + w.at + Spread<L, E>::first(w.lane), left);
         }
+        // Which of the group's states take part, by turn (a NaN among the queries is no masked state's). Found here: carried along from the
+        // loads of the states it costs 10 to 20 registers.
+        uint32_t seen = (uint32_t)(w.seen >> (w.group * L));
+        asm volatile("" : "+v"(seen));
         // A lane whose 16 bytes reach back into the lane's before has zeros there: it writes its own elements.
         auto write = [&](int n, const float (&x)[E], const float (&y)[E]) {
             if (!w.inside || w.turn_state(n) >= a.keys) return;
             const int64_t to = (((int64_t)w.b * a.keys + w.turn_state(n)) * a.kv_heads + w.hk) * a.dim;
-            const bool part = w.turn_seen(n);   // (a NaN among the queries is no masked state's)
-            float kept_x[E], kept_y[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                kept_x[i] = part ? x[i] : 0.f;
-                kept_y[i] = part ? y[i] : 0.f;
-            }
+            const uint32_t keep = 0u - ((seen >> n) & 1);
+            const Chunk<T, E> kept_x = masked_chunk<T, E>(x, keep), kept_y = masked_chunk<T, E>(y, keep);
             if (w.at == w.c * E) {
-                store_values<T, E>(dk + to + w.at, kept_x);
-                store_values<T, E>(dv + to + w.at, kept_y);
+                __builtin_memcpy(dk + to + w.at, kept_x.x, 16);
+                __builtin_memcpy(dv + to + w.at, kept_y.x, 16);
             } else {
 #pragma unroll
                 for (int i = 0; i < E; ++i)
                     if (w.at + i >= w.c * E) {
-                        dk[to + w.at + i] = (T)kept_x[i];
-                        dv[to + w.at + i] = (T)kept_y[i];
+                        dk[to + w.at + i] = kept_x.x[i];
+                        dv[to + w.at + i] = kept_y.x[i];
                     }
             }
         };
