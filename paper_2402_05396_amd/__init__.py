@@ -731,7 +731,8 @@ def cross_attention(q, k, v, lengths=None, mask=None, bias=None, scale=None, wan
     with adjacent elements; lengths int32[B]; mask bool[B, keys]; bias = (table [heads, buckets] of q's type, bounds int64[buckets - 1],
     query positions int64[B or 1, queries], key positions int64[B or 1, keys]); scale d ** -0.5 unless given. Returns out (like q,
     dense), with `want_stats` also stats float32[B, queries, heads, n]: a reference near the row's largest score, the sum of the
-    exponentials over it, and what cross_attention_grad needs besides."""
+    exponentials over it, and what cross_attention_grad needs besides. Autograd sees neither this call nor relative_bias and policy_loss:
+    results are detached. adaptive_training has autograd functions of this and of the loss."""
     if stream is None:
         r = (_native or _bind()).attention(q, k, v, lengths, mask, bias, scale, want_stats)
         if r is not None:
@@ -782,7 +783,7 @@ def _distance_block(dtype, heads, bounds, query_pos, key_pos, batch, device):
 
 def relative_bias(table, bounds, query_pos, key_pos, stream=None):
     """taser_relative_bias. table [heads, buckets], bounds int64[buckets - 1], positions int64[B or 1, queries] and [B or 1, keys]
-    -> [B, heads, queries, keys] of the table's type, B the larger of the positions'."""
+    -> [B, heads, queries, keys] of the table's type, B the larger of the positions', detached (its gradient: relative_bias_grad)."""
     if stream is None:
         r = (_native or _bind()).bias(table, bounds, query_pos, key_pos)
         if r is not None:
@@ -828,7 +829,7 @@ def relative_bias_grad(dbias, bounds, query_pos, key_pos, stream=None):
 def policy_loss(logits, actions, advantage, old_logp=None, ref_logp=None, count=None, weight=None, clip_low=0.2, clip_high=0.2, kl=0.0, want_grad=True, stream=None):
     """taser_policy_loss. logits [R, width] of float32, float16 or bfloat16 with contiguous rows; actions int32[R, picks] (-1: none);
     advantage, old_logp, ref_logp, weight float32[R, picks]; count int32[R]. Returns (loss float32[R, picks], logp float32[R, picks],
-    grad of the sum of all losses, like the logits and dense, or None)."""
+    grad of the sum of all losses, like the logits and dense, or None), all detached."""
     if stream is None:
         r = (_native or _bind()).policy(logits, actions, advantage, old_logp, ref_logp, count, weight, clip_low, clip_high, kl, want_grad, None)
         if r is not None:

@@ -1,10 +1,11 @@
 // Attention to states of another length (taser_cross_attention): one pass over the states with the running maximum and sum of
 // a softmax: with m' = max(m, tile's scores), weights exp(x - m'), and sum and output so far times exp(m - m') where m grew.
 //
-// Few rows: bound by reading the states. 32 single tokens, 8192 states, 32 heads on 8 of 128, bfloat16: 160 us for 806 MB, 5.1 TB/s.
+// Few rows: bound by reading the states. 32 single tokens, 8192 states, 32 heads on 8 of 128, bfloat16: 162 us for 806 MB, 5.0 TB/s.
 // Many rows: bound by the matrix products and, beside them, the exponentials and reads of LDS that feed them (counters: matrix cores 0.5
-// busy). 4 x 2048 queries, 4096 states, 16 heads of 128, bfloat16: 239 us, 860 TFLOP/s; 2 x 4096 x 4096 with a bias 330 - 360 us, 285 without;
-// float32, 3 x 333 x 777, 6 heads of 80: 37 us.
+// busy, 1.5 LDS instructions a product). 4 x 2048 queries, 2700 to 4050 of 4096 states, 16 heads of 128, bfloat16: 233 us, 885 TFLOP/s, in
+// single passes, and 270 - 300 without a pause between them, as the clock falls with all of these products; 2 x 4096 x 4096 320 - 380 us
+// with a bias, 265 - 320 without; float32, 3 x 333 x 777, 6 heads of 80: 36 us.
 #include <cmath>
 #include <type_traits>
 
@@ -392,8 +393,8 @@ __global__ __launch_bounds__(256) void attention_join_few_kernel(const float* pa
     }
 }
 
-// Where they are many: a block has a row, a thread one element of every eighth split. (96 rows of 97 splits 7 us, 66 by the other; 6 000
-// rows of 6 splits 29 us, and 8 by the other.)
+// Where they are many: a block has a row, a thread one element of every eighth split. (96 rows of 112 splits 7 us, 45 by the other; 6 000
+// rows of few splits 27 us, and 7 by the other.)
 template <typename T>
 __global__ __launch_bounds__(1024) void attention_join_kernel(const float* part_out, const float* part_stats, int64_t rows, int32_t dim, int32_t splits, T* out, float* stats,
                                                               int32_t stat_floats) {
@@ -491,8 +492,9 @@ template <typename T> int launch_typed(TaserAttentionArgs& a, bool shared, void*
     return shared ? launch<T, 4, true>(a, out, stats, work, stream) : launch<T, 4, false>(a, out, stats, work, stream);
 }
 
-// Rows of its own for each block of waves, or rows shared by them? (8 x 8 pairs, 4096 states, heads of 128, us, own / shared: 16 bits
-// 32 rows 34 / 33, 64 39 / 40, 96 57 / 45; float32 32 rows 105 / 155, 64 186 / 158, 96 349 / 161.)
+// Rows of its own for each block of waves, or rows shared by them? (8 x 8 pairs, 4096 states, heads of 128, us, own / shared: float32 32 rows
+// 111 / 156, 64 188 / 160, 96 352 / 165. bfloat16 32 rows 38 / 36, 64 44 / 40, 96 63 / 50, where the former multiply the weights' rest too:
+// without it they cost 34, 39 and 57.)
 bool few_rows(const TaserAttentionArgs& a) { return a.rows <= (taser_single(a) ? 32 : 64); }
 
 // Parts of the states, so that the chip is full where there are few rows.
@@ -500,7 +502,8 @@ int splits_for(const TaserAttentionArgs& a, int32_t type) {
     if (taser_window_fits(a)) return 1;
     const int64_t pairs = (int64_t)a.batch * a.kv_heads, bytes = pairs * a.rows * a.dim * 4;
     const double width = a.dim <= 64 ? 0.5 : a.dim <= 96 && !few_rows(a) ? 0.75 : 1.;
-    // us of a tile for a block, of 64 states for 128 rows, or of 128 for 32 (measured)
+    // us of a tile for a block, of 64 states for 128 rows, or of 128 for 32 (measured). 512 blocks at a time is right for few rows of up to 64
+    // 16-bit elements; the others' blocks take over 80 KiB of LDS and run 256 at a time, which these parts do not allow for.
     if (few_rows(a)) return taser_splits(pairs * ((a.rows + 31) / 32), 512, (a.keys + 127) / 128, width * (type == TASER_F32 ? 5. : 2.), bytes);
     return taser_splits(pairs * ((a.rows + 127) / 128), type == TASER_F32 ? 256 : 512, (a.keys + 63) / 64, width * (type == TASER_F32 ? 14. : 2.5), bytes);
 }

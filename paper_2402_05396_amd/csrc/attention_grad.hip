@@ -45,7 +45,8 @@ __global__ __launch_bounds__(256) void attention_grad_rows_kernel(const T* out, 
 // ---- dq, dtable -----------------------------------------------------------------------------------------------------------
 // A wave owns 32 rows, as in the forward pass; four waves share tiles of 32 states. Bound by registers (queries, their gradients, output: two
 // waves a SIMD) and by what the vector units do to scores between products; tiles with several buckets add each dx to its bucket's sum in
-// LDS. 2 x 4096 x 4096, 16 heads on 4 of 128, bfloat16: 369 us without a bias, 460 with one bucket, 485 with 32 around distance 0.
+// LDS. 2 x 4096 x 4096, 16 heads on 4 of 128, bfloat16: 379 us without a bias, 498 with 32 buckets around distance 0 (405 and 567 in ten
+// passes without a pause).
 template <typename T, int ND, bool BIAS>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_queries_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dq,
                                                                                                float* part_dq, float* part_table, int64_t work) {
@@ -339,7 +340,10 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void attention_grad_
 // has the keys in registers: scores, weights, dv. The second has the values: dp, dx, dk; the weights come to it through LDS. Each of a
 // tile's two steps is as many products for the one as for the other, and neither holds more than half of the sums: a wave with both
 // has too many registers for a second one on its SIMD (measured: 610 TFLOP/s so at 2 x 4096 x 4096, 16 heads of 128). Rows of all query
-// heads of the key head pass by, so shared heads' gradients are whole. The size above: 567 us without a bias, 600 with (matrix cores 0.37 busy).
+// heads of the key head pass by, so shared heads' gradients are whole. The size above: 589 us without a bias, 629 with (664 and 729 in ten
+// passes without a pause; matrix cores 0.37 busy). Registers are spilled here: 13 in 16 bits, heads of 97 to 128 elements, with a bias; 31 in
+// single precision, with a bias 55; and where heads have up to 64 elements 10, with a bias 103 to 128, since four waves a SIMD leave 128
+// registers: the size above with heads of 64 takes 334 us without a bias, 585 with.
 template <typename T, int ND, bool BIAS>
 __global__ __launch_bounds__(512, (ND <= 2 && sizeof(T) == 2 ? 4 : 2)) void attention_grad_states_kernel(const TaserAttentionArgs a, const taser_f4* info, const T* dout, T* dk, T* dv, float* part_dk,
                                                                     float* part_dv, int64_t work) {

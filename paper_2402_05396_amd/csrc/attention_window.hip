@@ -7,8 +7,8 @@
 // are found. The weights go back to the groups for the sums over the states.
 //
 // Bound by reading the states: 30000 windows of 25 states, four heads on two of 64, float16, bias: 85 us for 364 MB, 4.4 TB/s; with
-// the gradient in bfloat16 98 + 310 us. 12000 windows of 10 states, two heads of 50, float32: 29 + 48 us for 97 + 200 MB (rows of 200 bytes
-// leave 3 of 16 lanes idle). A score costs as many vector instructions as its row has elements over L, so many rows or states an item are
+// the gradient in bfloat16 97 + 326 us, the latter for 850 MB, far from it: scores pass through scratch memory on their way to their lanes. 12000
+// windows of 10 states, two heads of 50, float32: 29 + 48 us for 97 + 200 MB (rows of 200 bytes leave 3 of 16 lanes idle). A score costs as many vector instructions as its row has elements over L, so many rows or states an item are
 // left to the tiles.
 #include "attention.h"
 
@@ -208,7 +208,8 @@ template <typename T, int L, int N> struct Item {
         for (int i = 0; i < E; ++i) d = fmaf(x[i], (float)y.x[i], d);
         return group_sum<L>(d);
     }
-    // The value of turn c, which is the lane's own state's.
+    // The value of turn c, which is the lane's own state's. (The compiler makes an indexed array of it, in LDS or, in the gradient where several
+    // rows share an item, of 4 or 8 turns, in 32 - 80 bytes a lane of scratch memory.)
     __device__ float own(const float (&x)[N]) const {
         float y = x[0];
 #pragma unroll
@@ -509,7 +510,7 @@ int64_t grad_waves(const TaserAttentionArgs& a) {
 // Windows cost by rows times states, tiles by their number, one for up to 32 rows and states. 4000 items, heads of 64, here / by tiles, us,
 // forward and with the gradient: 16 bits, 16 rows of 10 states 23 / 42, 63 / 148; 8 of 64 40 / 42, 122 / 175; 32 of 64 92 / 37, 353 / 178;
 // float32 8 of 64 46 / 105, 167 / 394; 32 of 64 113 / 103, 493 / 400, and 2000 of 128 227 / 87, 659 / 433.
-// (A row has to have 16 bytes.)
+// Calls of a few items go by the same rule: nothing was measured for them. (A row has to have 16 bytes.)
 bool taser_window_fits(const TaserAttentionArgs& a) {
     return a.keys >= 1 && a.keys <= 64 && a.rows <= kWindowRows && a.rows * a.keys <= (taser_single(a) ? 1024 : 768) && a.dim >= 8 &&
            (int64_t)a.batch * a.kv_heads < INT32_MAX / 2;
@@ -524,7 +525,8 @@ int taser_window_attention(const TaserAttentionArgs& a, int32_t type, void* out,
     return run_any(a, type, c);
 }
 
-// Never nothing: a caller that brings no workspace learns it from every gradient, not from those alone that go over tiles.
+// Never nothing (without a bias no kernel touches it): a caller that brings no workspace learns it from every gradient, not from those alone
+// that go over tiles.
 uint64_t taser_window_grad_bytes(const TaserAttentionArgs& a) {
     return a.table ? (uint64_t)grad_waves(a) * a.rows * taser_padded(a.buckets) * sizeof(float) : 256;
 }

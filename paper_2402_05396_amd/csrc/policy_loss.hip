@@ -4,7 +4,7 @@
 // d l / d logit[c] = (c is the action) - softmax[c]. So a row's gradient is minus the sum of its actions' slopes times the softmax,
 // plus each slope at its action.
 //
-// Bound by reading the logits once and writing their gradient once: 4096 rows of 64001 in bfloat16 248 us, 1.05 GB at 4.2 TB/s (rows of an odd
+// Bound by reading the logits once and writing their gradient once: 4096 rows of 64001 in bfloat16 250 us, 1.05 GB at 4.2 TB/s (rows of an odd
 // length begin inside cache lines: counters say 0.73 GB read, 0.54 written). 12000 rows of 25 with 10 actions: 6 us, a launch.
 #include "attention.h"
 
@@ -265,7 +265,7 @@ template <typename T> int launch(const Batch& p, const void* logits, float* loss
         else policy_window_kernel<T, 64><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
     } else {
         // Short rows are held by as few threads as it takes. Of longer ones as much as leaves registers for two blocks a compute unit, one writing
-        // while the other reads: 64 001 bf16 logits 0.28 ms for 4 096 rows, 0.30 with the whole row held by one block.
+        // while the other reads: 64 001 bf16 logits 251 us for 4 096 rows, 274 with the whole row held by one block.
         if (pieces <= 256) policy_row_kernel<T, 256, 1><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
         else if (pieces <= 1024) policy_row_kernel<T, 256, 4><<<grid, 256, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);
         else policy_row_kernel<T, 1024, (sizeof(T) == 2 ? 4 : 8)><<<grid, 1024, 0, stream>>>(p, (const T*)logits, loss, logp, (T*)grad);

@@ -1,7 +1,8 @@
 // The learned bias by distance as a tensor, and the table's gradient from the tensor's (taser_relative_bias, _grad).
 //
 // Both are bound by the tensor's bytes. 12 x 1024 x 1024 in bfloat16 written in 8.2 us (3.1 TB/s, a launch included); 4 x 16 x 1000 x 2047 in
-// float32 read and summed in 165 us (3.2 TB/s: an element also costs a comparison with its neighbor's bucket).
+// float32 read and summed in 165 us, 3.2 TB/s: bound by what each row of 256 states costs beside its elements, 54 vector and 4 LDS instructions
+// in some 800 cycles of a SIMD, among them two searches for the stretch's buckets in 64 bits.
 #include "attention.h"
 
 namespace {
@@ -239,7 +240,8 @@ int check(const taser_distances* p, const char* what, Distances* d) {
     return TASER_OK;
 }
 
-// Blocks of a head: two for each compute unit that its LDS leaves room for, none without a group of queries for each wave.
+// Blocks of a head: some 1024 for all heads, four to a compute unit, as many as its LDS holds with 64 buckets (32 KiB each); none without a
+// group of queries for each wave.
 int blocks_of_head(const Distances& d, int rows) {
     const int64_t groups = d.batch * ((d.queries + rows - 1) / rows), most = (groups + 3) / 4, wanted = (1024 + d.heads - 1) / d.heads;
     const int64_t n = most < wanted ? most : wanted;
