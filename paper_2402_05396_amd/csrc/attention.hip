@@ -4,7 +4,7 @@
 // Few rows: bound by reading the states. 32 single tokens, 8192 states, 32 heads on 8 of 128, bfloat16: 162 us for 806 MB, 5.0 TB/s.
 // Many rows: bound by the matrix products and, beside them, the exponentials and reads of LDS that feed them (counters: matrix cores 0.5
 // busy, 1.5 LDS instructions a product). 4 x 2048 queries, 2700 to 4050 of 4096 states, 16 heads of 128, bfloat16: 233 us, 885 TFLOP/s, in
-// single passes, and 270 - 300 without a pause between them, as the clock falls with all of these products; 2 x 4096 x 4096 320 - 380 us
+// single passes, and 270 - 300 without a pause between them, as all of these products take longer then; 2 x 4096 x 4096 320 - 380 us
 // with a bias, 265 - 320 without; float32, 3 x 333 x 777, 6 heads of 80: 36 us.
 #include <cmath>
 #include <type_traits>

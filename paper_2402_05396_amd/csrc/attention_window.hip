@@ -7,7 +7,7 @@
 // are found. The weights go back to the groups for the sums over the states.
 //
 // Bound by reading the states: 30000 windows of 25 states, four heads on two of 64, float16, bias: 85 us for 364 MB, 4.4 TB/s; with
-// the gradient in bfloat16 97 + 326 us, the latter for 850 MB, far from it: scores pass through scratch memory on their way to their lanes. 12000
+// the gradient in bfloat16 97 + 330 us, the latter for 850 MB, far from it: scores pass through scratch memory on their way to their lanes. 12000
 // windows of 10 states, two heads of 50, float32: 29 + 48 us for 97 + 200 MB (rows of 200 bytes leave 3 of 16 lanes idle). A score costs as many vector instructions as its row has elements over L, so many rows or states an item are
 // left to the tiles.
 #include "attention.h"
