@@ -4,6 +4,9 @@
 // dx q, dq = scale * sum of dx k, dtable = sum of dx by bucket. One kernel owns states and goes over the rows (dk, dv), another
 // owns rows and goes over the states (dq, dtable): scores and dp are computed twice (7 products for 5), but nothing is added to
 // memory by more than one block, so all sums have one order and need no second pass over a gradient.
+// Weights (for dv) and dx (for dk, dq) are rounded to 16-bit types where they enter a product. To multiply what that takes off too, as the
+// forward pass does for few rows, costs a third more products: forward and gradient of 2 x 4096 x 4096 take 20 - 26 % longer then, those of
+// few rows 2 - 7 %. It is not done: errors are 1.4 times those of the results' own rounding.
 #include <cmath>
 #include <type_traits>
 
