@@ -3,7 +3,8 @@
  * gather: the mini-batch generation hot path of TASER (arXiv 2402.05396,
  * Sec. 2.1 "Neighbor Finder", Sec. 3.3 "GPU Temporal Neighbor Finding",
  * Sec. 3.4 "GPU Feature Caching", Alg. 1-3), and what its answers go into:
- * attention with a bias by distance and the sampler's policy loss.
+ * attention with a bias by distance, layer norm, a policy's draws and its
+ * loss, and the models' update.
  *
  * Conventions shared by every call
  *   - Plain pointers and sizes only. Each pointer argument says "device" or
@@ -22,8 +23,9 @@
  *     taser_candidate_encodings, taser_select_weighted, taser_selector_draw,
  *     taser_selector_update, taser_cache_lookup / _lookup_static /
  *     _prefetch / _gather, taser_cross_attention(_grad),
- *     taser_relative_bias(_grad) and taser_policy_loss only launch kernels
- *     (no memset or copy nodes, no synchronization), so a stream
+ *     taser_relative_bias(_grad), taser_policy_loss, taser_policy_draw,
+ *     taser_layer_norm(_grad), taser_adamw_step and taser_adamw_moments only
+ *     launch kernels (no memset or copy nodes, no synchronization), so a stream
  *     that is being captured into a HIP graph can be passed to them. Three
  *     things happen on first use only and must have happened before a capture:
  *     a cache lookup or prefetch with more requests than any before it on that
@@ -586,6 +588,146 @@ typedef struct taser_policy_batch {
 } taser_policy_batch;
 
 int taser_policy_loss(const taser_policy_batch* p, float* loss, float* logp, void* grad, void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Draws from a policy's logits: actions that taser_policy_loss trains on, one
+ * of a few candidates or of a vocabulary, by given random numbers.
+ *
+ * Row r has `width` logits, of which the first count[r] (clamped to [0, width];
+ * all where count is NULL) take part; the rest is not read. With top the
+ * largest, in order of falling logits (equal ones: the lower index first):
+ *   w     = exp((logit - top) / temperature)
+ *   top_k keeps the first top_k (0: all),
+ *   top_p of these the first ones, as few as hold the share top_p of their sum
+ *         of w (1: all),
+ *   min_p of these the ones with w >= min_p (0: all);
+ * the first one is always kept. Draw j of the row is the first kept candidate by
+ * index whose running sum of w exceeds uniform[r][j] times the whole sum: draws
+ * are independent, an action can come twice. A temperature of 0 takes the
+ * largest (the lower index of equal ones).
+ *   logp[r][j] = logit[action] - log(sum over the row of exp(logit)): of the row
+ *                as it is, what taser_policy_loss takes as old_logp
+ * A row without a candidate, or whose logits are all minus infinity, gives the
+ * action -1 with logp 0, as taser_policy_loss has it; a row with a NaN or plus
+ * infinity -1 with a logp of NaN.
+ *   logits    device, type, row r at r * logits_stride elements
+ *   uniform   device float[rows][picks], in [0, 1) (below: as 0; 1 and above, and
+ *             NaN: the last kept candidate of some weight)
+ *   row_*     device arrays of `rows`, or NULL: the one number for every row.
+ *             Row values out of range count as the nearest in it (NaN: a
+ *             temperature of 0, a top_p or min_p of 0).
+ *   temperature >= 0, top_k >= 0, top_p in [0, 1], min_p in [0, 1]
+ *   width in [1, TASER_MAX_DRAW_WIDTH], picks in [1, TASER_MAX_PICKS], rows >= 0
+ * w and its sums are whole multiples of 2^-43 in 64 bits: every sum has one
+ * value, whatever the order, and the same call gives the same actions. A w
+ * below 2^-44 counts as 0: such a candidate may be kept, but is never drawn.
+ * Works in `work` (16-byte aligned, as much as taser_policy_draw_bytes says, 0
+ * for many calls). Only launches kernels.
+ * ------------------------------------------------------------------------- */
+#define TASER_MAX_DRAW_WIDTH (1 << 20)
+
+typedef struct taser_policy_draws {
+    int32_t type, picks;
+    int64_t rows, width, logits_stride;
+    const void* logits;
+    const int32_t* count;
+    const float* uniform;
+    float temperature, top_p, min_p;
+    int32_t top_k;
+    const float *row_temperature, *row_top_p, *row_min_p;
+    const int32_t* row_top_k;
+} taser_policy_draws;
+
+int taser_policy_draw_bytes(const taser_policy_draws* p, uint64_t* work_bytes);
+int taser_policy_draw(const taser_policy_draws* p, int32_t* actions, float* logp, void* work, uint64_t work_bytes,
+                      void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * Layer norm of rows, and its gradient:
+ *   mean = sum(x) / width, rstd = 1 / sqrt(sum((x - mean)^2) / width + eps)
+ *   xhat = (x - mean) * rstd, out = xhat * weight + bias
+ * and for the gradient of sum(out * dout), with g = dout * weight:
+ *   dx      = rstd * (g - mean(g) - xhat * mean(g * xhat))
+ *   dweight = sum over rows of dout * xhat, dbias = sum over rows of dout
+ *   x, dout  device, type, row r at r * x_stride (dout_stride) elements
+ *   weight, bias  device [width], weight_type (type or TASER_F32); NULL: 1 and 0
+ *   out, dx  dense [rows][width], type
+ *   stats    float[rows][2]: mean and rstd (taser_layer_norm: or NULL)
+ *   dweight, dbias  [width], weight_type, or NULL
+ *   width in [1, 2^26), rows >= 0 (none: dweight and dbias are 0), eps >= 0
+ * taser_layer_norm_grad works in `work` (16-byte aligned, as much as
+ * taser_layer_norm_grad_bytes says, none where dweight and dbias are NULL). Sums
+ * are in 32 bits in a fixed order; out and the gradients are rounded once. Both
+ * only launch kernels.
+ * ------------------------------------------------------------------------- */
+typedef struct taser_norm {
+    int32_t type, weight_type;
+    int64_t rows, width, x_stride;
+    const void *x, *weight, *bias;
+    float eps;
+} taser_norm;
+
+int taser_layer_norm(const taser_norm* n, void* out, float* stats, void* hip_stream);
+int taser_layer_norm_grad_bytes(const taser_norm* n, uint64_t* work_bytes);
+int taser_layer_norm_grad(const taser_norm* n, const float* stats, const void* dout, int64_t dout_stride, void* dx,
+                          void* dweight, void* dbias, void* work, uint64_t work_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * One AdamW step over a list of tensors. With g the gradient times grad_scale
+ * (NULL: 1) and c = 1 - beta^step:
+ *   m = beta1 * m + (1 - beta1) * g, v = beta2 * v + (1 - beta2) * g^2
+ *   param = param * (1 - lr * weight_decay)
+ *           - (lr / c1) * m / (sqrt(v) / sqrt(c2) + eps)
+ * in 32 bits, param rounded to its type once.
+ *   param, grad  device, dense, `elements` numbers of type and grad_type; a NULL
+ *                gradient or no elements: the tensor is left as it is
+ *   m, v      bits 32: device float[elements]. bits 8: device uint8[elements],
+ *             with m_unit and v_unit device float[ceil(elements /
+ *             TASER_ADAMW_BLOCK)], a unit for every so many neighbors:
+ *               m = (1 - 2 * (code >> 7)) * (code & 127)^2 * m_unit
+ *               v = (code^2 * v_unit)^2
+ *             All zeros: moments of zero. A step uses its moments before it
+ *             rounds them. A rounded one is one of the two codes beside it, the
+ *             upper one where (r + 1/2) / 2^16 is below the chance that makes its
+ *             expectation exact; r: 16 bits, 16 * (e % 2) of word e % 8 / 2 of Philox
+ *             4x32-10 with key `seed` and counter (e / 8, the tensor's place in the
+ *             list, step, 0x4144414D), e the element's index. A v that is not 0
+ *             has a code of 1 at least; moments whose unit would be below 2^-126
+ *             are 0 (v: have a code whose value is as good as 0). Where a moment is
+ *             not finite the unit, and so its whole block, is NaN.
+ *   step      counts from 1; step_at: device int64, read in its place (NULL: none)
+ *   lr        >= 0; lr_at: device float, read in its place
+ *   grad_scale  device float; where it is NaN the call changes nothing
+ *   betas in [0, 1), eps and weight_decay >= 0
+ * Memory that is written (param, m, v and units) must overlap neither other
+ * tensors' nor a gradient: such calls are refused. Any number of tensors, at most
+ * 2^35 elements each; only launches kernels, one for every 56 tensors.
+ *
+ * taser_adamw_moments: 8-bit moments of one tensor as numbers of `type`, dense.
+ * ------------------------------------------------------------------------- */
+#define TASER_ADAMW_BLOCK 256
+
+typedef struct taser_adamw_tensor {
+    int32_t type, grad_type;
+    int64_t elements;
+    void* param;
+    const void* grad;
+    void *m, *v;
+    float *m_unit, *v_unit;
+} taser_adamw_tensor;
+
+typedef struct taser_adamw {
+    int32_t bits;
+    int64_t step;
+    const int64_t* step_at;
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *lr_at, *grad_scale;
+    uint64_t seed;
+} taser_adamw;
+
+int taser_adamw_step(const taser_adamw* a, const taser_adamw_tensor* tensors, int64_t n, void* hip_stream);
+int taser_adamw_moments(const uint8_t* m, const uint8_t* v, const float* m_unit, const float* v_unit, int64_t elements,
+                        int32_t type, void* m_out, void* v_out, void* hip_stream);
 
 /* Message for the most recent error on the calling thread (static storage). */
 const char* taser_last_error(void);

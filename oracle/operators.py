@@ -1,5 +1,5 @@
-"""Attention to states of another length, the bias by distance and the clipped policy loss from their definitions, in 64 bits on
-the CPU, with how far a result in fewer bits may be off.
+"""Attention to states of another length, the bias by distance, the clipped policy loss, layer norm, a policy's draws and the AdamW
+step from their definitions, in 64 bits on the CPU, with how far a result in fewer bits may be off.
 
 The bounds follow from the roundings that the operators say they make. u is half the spacing of the element type above 1 (2^-24,
 2^-11, 2^-8), `tiny` half its spacing at 0. Softmax weights, their gradients dx and
@@ -148,3 +148,162 @@ def policy_loss(logits, actions, advantage, kind, old=None, ref=None, count=None
         egrad[r, :c] = eextra + eslopes * p + abs(slopes) * (ep + 4 * E32 * p) + 2 * E32 * (np.abs(extra) + abs(slopes) * p)
     egrad = egrad + u * (np.abs(grad) + egrad) + tiny
     return {"loss": loss, "logp": logp, "grad": grad}, {"loss": eloss, "logp": elogp, "grad": egrad}
+
+
+def layer_norm(x, kind, weight=None, bias=None, eps=1e-5, dout=None, kept=None):
+    """x, dout float64 [R, W]; kept: the weights' kind, kind unless given -> (results, bounds) of out and, with `dout`, dx, dweight, dbias.
+    The operator's sums are in 32 bits; out and the gradients are rounded to their types once."""
+    R, W = x.shape
+    u, tiny = U[kind], TINY[kind]
+    u2, tiny2 = U[kept or kind], TINY[kept or kind]
+    w = np.ones(W) if weight is None else weight
+    b = np.zeros(W) if bias is None else bias
+    mean = x.mean(1, keepdims=True)
+    away = x - mean
+    em = (W + 4) * E32 * np.abs(x).mean(1, keepdims=True) + E32 * np.abs(mean)
+    ea = em + E32 * np.abs(away)
+    var = (away ** 2).mean(1, keepdims=True) + eps
+    evar = (2 * np.abs(away) * ea + ea ** 2).mean(1, keepdims=True) + (W + 8) * E32 * var
+    rstd = var ** -0.5
+    part = np.minimum(evar / var, 0.99)
+    er = rstd * ((1 - part) ** -0.5 - 1 + 4 * E32)
+    xhat = away * rstd
+    ex = ea * (rstd + er) + np.abs(away) * er + 2 * E32 * np.abs(xhat)
+    out = xhat * w + b
+    eo = ex * np.abs(w) + 4 * E32 * (np.abs(xhat * w) + np.abs(b))
+    res, off = {"out": out}, {"out": eo + u * (np.abs(out) + eo) + tiny}
+    if dout is None:
+        return res, off
+    g = dout * w
+    s, t = g.mean(1, keepdims=True), (g * xhat).mean(1, keepdims=True)
+    es = (W + 6) * E32 * np.abs(g).mean(1, keepdims=True)
+    et = (np.abs(g) * ex).mean(1, keepdims=True) + (W + 8) * E32 * np.abs(g * xhat).mean(1, keepdims=True)
+    inner = g - s - xhat * t
+    ei = 4 * E32 * (np.abs(g) + np.abs(s) + np.abs(xhat * t)) + es + ex * (np.abs(t) + et) + np.abs(xhat) * et
+    dx = rstd * inner
+    ed = (rstd + er) * ei + er * np.abs(inner) + 2 * E32 * np.abs(dx)
+    dweight, dbias = (dout * xhat).sum(0), dout.sum(0)
+    ew = (np.abs(dout) * ex).sum(0) + (R + 8) * E32 * np.abs(dout * xhat).sum(0)
+    eb = (R + 8) * E32 * np.abs(dout).sum(0)
+    res.update(dx=dx, dweight=dweight, dbias=dbias)
+    off.update(dx=ed + u * (np.abs(dx) + ed) + tiny, dweight=ew + u2 * (np.abs(dweight) + ew) + tiny2, dbias=eb + u2 * (np.abs(dbias) + eb) + tiny2)
+    return res, off
+
+
+def policy_draw(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, count=None):
+    """logits, uniform float64 [R, W], [R, n]; settings numbers or arrays [R], as the operator has them (in 32 bits) -> (actions, logp, how far logp
+    may be off, sure). sure: the draw is further from every border (of top-p's share, min_p's weight, the running sum) than weights that are whole
+    multiples of 2^-43, off by another 2^-41 of their own, could move it."""
+    R, W = logits.shape
+    n = uniform.shape[1]
+    of = lambda x: np.broadcast_to(np.asarray(x, np.float64), (R,))
+    temperature, top_k, top_p, min_p = of(temperature), of(top_k), of(top_p), of(min_p)
+    actions, logp, off, sure = np.full((R, n), -1), np.zeros((R, n)), np.zeros((R, n)), np.ones((R, n), bool)
+    for r in range(R):
+        c = W if count is None else min(max(int(count[r]), 0), W)
+        x = logits[r, :c]
+        if not c or (np.isneginf(x).all()):
+            continue
+        if np.isnan(x).any() or np.isposinf(x).any():
+            logp[r] = np.nan
+            continue
+        top = x.max()
+        order = np.argsort(-x, kind="stable")
+        w = np.zeros(c)
+        if temperature[r] > 0:
+            w = np.exp((x - top) / temperature[r])
+            w[np.isneginf(x)] = 0
+        else:
+            w[order[0]] = 1
+        rounded = (w != 0) & (w != 1)   # the others, and their sums, are exact on either side
+        slack = lambda s: min(s, w[rounded].sum()) * 2.0 ** -41 + rounded.sum() * 2.0 ** -43
+        clear = lambda margin, s: margin > slack(s) or slack(s) == 0
+        keep, certain = np.zeros(c, bool), True
+        k = int(top_k[r]) if top_k[r] > 0 else c
+        before, whole = 0.0, w[order[:k]].sum()
+        for i, at in enumerate(order[:k]):
+            if i and top_p[r] < 1 and before >= top_p[r] * whole:
+                certain = certain and clear(before - top_p[r] * whole, whole)
+                break
+            certain = certain and (i == 0 or top_p[r] >= 1 or clear(top_p[r] * whole - before, whole))
+            certain = certain and (i == 0 or min_p[r] <= 0 or w[at] == 1 or clear(abs(w[at] - min_p[r]), 1.0))
+            keep[at] = i == 0 or w[at] >= min_p[r]
+            before += w[at]
+        running = np.cumsum(np.where(keep, w, 0.0))
+        last = np.nonzero(np.where(keep, w, 0.0) > 2.0 ** -45)[0][-1]
+        s = np.exp(x - top).sum()
+        for j in range(n):
+            place = min(max(uniform[r, j], 0.0), 1.0) * running[-1]
+            a = min(int((running <= place).sum()), last)
+            actions[r, j] = a
+            away = [abs(y - place) for y in (running[a], running[a - 1] if a else np.inf)]
+            sure[r, j] = certain and (keep.sum() == 1 or uniform[r, j] == 0 or clear(min(away), running[-1]))
+            logp[r, j] = x[a] - top - np.log(s)
+            off[r, j] = (c + 16) * E32 + 4 * E32 * (abs(x[a] - top) + abs(np.log(s)) + abs(x[a]))
+    return actions, logp, off, sure
+
+
+def philox(counter, key):
+    """Philox4x32-10: counter, four uint32 arrays; key, two numbers -> four uint32 arrays."""
+    c, k = [np.asarray(x, np.uint64) for x in counter], [int(x) for x in key]
+    low, shift = np.uint64(0xFFFFFFFF), np.uint64(32)
+    for _ in range(10):
+        a, b = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(b >> shift) ^ c[1] ^ np.uint64(k[0]), b & low, (a >> shift) ^ c[3] ^ np.uint64(k[1]), a & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return [x.astype(np.uint32) for x in c]
+
+
+def adamw_chance(n, number, step, seed):
+    """float64 [n]: what an 8-bit moment's place between its two codes is compared with."""
+    piece = np.arange((n + 7) // 8, dtype=np.uint64)
+    same = lambda x: np.full(piece.shape, x & 0xFFFFFFFF, np.uint64)
+    words = philox((piece & np.uint64(0xFFFFFFFF), same(number), same(step), same(0x4144414D)), (seed & 0xFFFFFFFF, seed >> 32 & 0xFFFFFFFF))
+    halves = np.stack([h for x in words for h in (x & np.uint32(0xFFFF), x >> np.uint32(16))], 1).reshape(-1)[:n]
+    return (halves.astype(np.float64) + 0.5) / 65536
+
+
+def adamw_decode(m, v, m_unit, v_unit):
+    """Codes and units -> moments, in 64 bits."""
+    at = np.arange(len(m)) // 256
+    m, v = m.astype(np.int64), v.astype(np.float64)
+    return np.where(m >= 128, -1.0, 1.0) * (m % 128) ** 2 * m_unit.astype(np.float64)[at], (v ** 2 * v_unit.astype(np.float64)[at]) ** 2
+
+
+def adamw(p, g, m, v, kind, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.01, scale=1.0):
+    """float64 arrays -> (results, bounds) of p, m, v. Multipliers are rounded to 32 bits, as every product and sum is."""
+    g = g * scale
+    eg = E32 * np.abs(g) if scale != 1.0 else 0.0
+    m2, v2 = beta1 * m + (1 - beta1) * g, beta2 * v + (1 - beta2) * g * g
+    em = 4 * E32 * (np.abs(beta1 * m) + np.abs((1 - beta1) * g)) + (1 - beta1) * eg + END32
+    ev = 6 * E32 * v2 + 2 * (1 - beta2) * np.abs(g) * eg + END32
+    c1, c2 = 1 - beta1 ** step, 1 - beta2 ** step
+    root = np.sqrt(v2)
+    eroot = np.sqrt(v2 + ev) - root + 2 * E32 * root
+    den = root / np.sqrt(c2) + eps
+    eden = eroot / np.sqrt(c2) + 4 * E32 * den
+    with np.errstate(divide="ignore", invalid="ignore"):
+        move = lr / c1 * m2 / den
+        emove = lr / c1 * em / den + np.abs(move) * (eden / np.maximum(den - eden, 1e-300) + 10 * E32)
+    out = p * (1 - lr * decay) - move
+    ep = 3 * E32 * np.abs(p) + emove + 2 * E32 * np.abs(move) + END32
+    return {"p": out, "m": m2, "v": v2}, {"p": ep + U[kind] * (np.abs(out) + ep) + TINY[kind], "m": em, "v": ev}
+
+
+def adamw_codes(x, chance, quad):
+    """Magnitudes of one block (64 bits), their chances -> (codes, sure, unit): quad: x = (unit c^2)^2, else unit c^2. sure: the code is the same where x is off by
+    20 * 2^-24 of itself and of the block's largest."""
+    power, most = (4, 255) if quad else (2, 127)
+    largest = x.max() if len(x) else 0.0
+    if largest == 0:
+        return np.zeros(len(x), np.int64), np.ones(len(x), bool), 0.0
+    y = x / largest * float(most) ** power
+    c = np.minimum(np.floor(y ** (1 / power)), most - 1)
+    low, high = c ** power, (c + 1) ** power
+    place = (y - low) / (high - low)
+    codes = (c + (place > chance)).astype(np.int64)
+    if quad:
+        codes[(x > 0) & (codes == 0)] = 1
+    slack = 40 * E32 * y / (high - low)
+    sure = np.abs(place - chance) > slack
+    return codes, sure, largest

@@ -23,7 +23,8 @@ LIB_PATH = os.path.join(_HERE, "libtaser.so")
 RECENT, UNIFORM, WEIGHTED, INVERSE_TIMESPAN = 0, 1, 2, 3
 INPUT_ON_DEVICE = 1
 MAX_K, MAX_M, MAX_HOPS = 64, 64, 3
-MAX_HEAD_DIM, MAX_BUCKETS, MAX_PICKS = 128, 64, 64
+MAX_HEAD_DIM, MAX_BUCKETS, MAX_PICKS, MAX_DRAW_WIDTH = 128, 64, 64, 1 << 20
+ADAMW_BLOCK = 256
 
 EXPORTS = ("taser_tcsr_build", "taser_tcsr_build_bytes", "taser_tcsr_build_in", "taser_tcsr_size", "taser_tcsr_view", "taser_tcsr_free", "taser_sample_temporal", "taser_sample_temporal_rows",
            "taser_candidate_encodings", "taser_select_weighted", "taser_gather_features", "taser_cache_init", "taser_cache_lookup", "taser_cache_lookup_static", "taser_cache_prefetch", "taser_cache_gather", "taser_cache_tune", "taser_cache_count_accesses", "taser_cache_access_counts",
@@ -31,7 +32,8 @@ EXPORTS = ("taser_tcsr_build", "taser_tcsr_build_bytes", "taser_tcsr_build_in", 
            "taser_cache_free", "taser_selector_init", "taser_selector_draw", "taser_selector_update",
            "taser_selector_scores", "taser_selector_size", "taser_selector_free",
            "taser_cross_attention", "taser_cross_attention_bytes", "taser_cross_attention_grad", "taser_relative_bias", "taser_relative_bias_bytes",
-           "taser_relative_bias_grad", "taser_policy_loss", "taser_profile_begin", "taser_profile_begin_only", "taser_profile_end", "taser_last_error")
+           "taser_relative_bias_grad", "taser_policy_loss", "taser_policy_draw", "taser_policy_draw_bytes", "taser_layer_norm", "taser_layer_norm_grad",
+           "taser_layer_norm_grad_bytes", "taser_adamw_step", "taser_adamw_moments", "taser_profile_begin", "taser_profile_begin_only", "taser_profile_end", "taser_last_error")
 
 
 class TaserError(RuntimeError):
@@ -66,6 +68,27 @@ class _PolicyBatch(ctypes.Structure):
     _fields_ = ([("type", ctypes.c_int32), ("picks", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("rows", "width", "logits_stride")] +
                 [(n, ctypes.c_void_p) for n in ("logits", "count", "actions", "advantage", "old_logp", "ref_logp", "weight")] +
                 [(n, ctypes.c_float) for n in ("clip_low", "clip_high", "kl")])
+
+
+class _PolicyDraws(ctypes.Structure):
+    _fields_ = ([("type", ctypes.c_int32), ("picks", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("rows", "width", "logits_stride")] +
+                [(n, ctypes.c_void_p) for n in ("logits", "count", "uniform")] + [(n, ctypes.c_float) for n in ("temperature", "top_p", "min_p")] + [("top_k", ctypes.c_int32)] +
+                [(n, ctypes.c_void_p) for n in ("row_temperature", "row_top_p", "row_min_p", "row_top_k")])
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = ([("type", ctypes.c_int32), ("weight_type", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("rows", "width", "x_stride")] +
+                [(n, ctypes.c_void_p) for n in ("x", "weight", "bias")] + [("eps", ctypes.c_float)])
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = ([("type", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("elements", ctypes.c_int64)] +
+                [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_unit", "v_unit")])
+
+
+class _Adamw(ctypes.Structure):
+    _fields_ = ([("bits", ctypes.c_int32), ("step", ctypes.c_int64), ("step_at", ctypes.c_void_p)] + [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] +
+                [("lr_at", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p), ("seed", ctypes.c_uint64)])
 
 
 _lib = None
@@ -122,6 +145,14 @@ def lib():
         L.taser_relative_bias.argtypes = [D, vp, vp, vp]
         L.taser_relative_bias_grad.argtypes = [D, vp, ctypes.POINTER(i64), vp, vp, u64, vp]
         L.taser_policy_loss.argtypes = [P, vp, vp, vp, vp]
+        S, N, W = ctypes.POINTER(_PolicyDraws), ctypes.POINTER(_Norm), ctypes.POINTER(_Adamw)
+        L.taser_policy_draw_bytes.argtypes = [S, ctypes.POINTER(u64)]
+        L.taser_policy_draw.argtypes = [S, vp, vp, vp, u64, vp]
+        L.taser_layer_norm.argtypes = [N, vp, vp, vp]
+        L.taser_layer_norm_grad_bytes.argtypes = [N, ctypes.POINTER(u64)]
+        L.taser_layer_norm_grad.argtypes = [N, vp, vp, i64, vp, vp, vp, vp, u64, vp]
+        L.taser_adamw_step.argtypes = [W, ctypes.POINTER(_AdamwTensor), i64, vp]
+        L.taser_adamw_moments.argtypes = [vp, vp, vp, vp, i64, i32, vp, vp, vp]
         L.taser_profile_begin.argtypes = []
         L.taser_profile_begin_only.argtypes = [ctypes.c_char_p]
         L.taser_profile_end.argtypes = [ctypes.POINTER(_KernelTime), i32, ctypes.POINTER(i32)]
@@ -856,6 +887,227 @@ def policy_loss(logits, actions, advantage, old_logp=None, ref_logp=None, count=
     grad = _result((rows, width), logits.dtype, logits.device, stream) if want_grad else None
     _check(lib().taser_policy_loss(ctypes.byref(p), _ptr(loss), _ptr(logp), _ptr(grad), _stream(stream)))
     return loss, logp, grad
+
+
+def _same_device(t, device, name):
+    if t.device != device:
+        raise TypeError(f"{name}: expected a tensor on {device}")
+    return t
+
+
+def _guard(device, stream):
+    """Launches go to the tensors' device, also where another is the current one; a stream has to be that device's."""
+    if stream is not None and getattr(stream, "device", device) != device:
+        raise ValueError(f"the stream must be one of {device}")
+    return torch.cuda.device(device)
+
+
+def _rows_of(per_row, dtype, rows, name, device):
+    """A setting for each row -> its address; it must be a contiguous device tensor of `dtype` with a number for each."""
+    _same_device(_want(per_row, dtype, name), device, name)
+    if per_row.numel() != rows:
+        raise ValueError(f"{name} must hold a number for each row")
+    return per_row.data_ptr()
+
+
+def _draw_block(logits, uniform, temperature, top_k, top_p, min_p, count):
+    _strided(logits, 2, _TYPES, "logits")
+    rows, width = logits.shape
+    _same_device(_want(uniform, torch.float32, "uniform"), logits.device, "uniform")
+    if uniform.dim() != 2 or uniform.shape[0] != rows:
+        raise ValueError("logits must be [R, width] and uniform [R, picks]")
+    p = _PolicyDraws(_TYPES[logits.dtype], uniform.shape[1], rows, width, logits.stride(0) if rows > 1 else width, logits.data_ptr())
+    p.uniform = uniform.data_ptr()
+    for name, x, dtype in (("temperature", temperature, torch.float32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("top_k", top_k, torch.int32)):
+        if isinstance(x, torch.Tensor):
+            setattr(p, "row_" + name, _rows_of(x, dtype, rows, name, logits.device))
+        else:
+            setattr(p, name, x if name != "top_k" else min(x, 2 ** 31 - 1))
+    if count is not None:
+        p.count = _rows_of(count, torch.int32, rows, "count", logits.device)
+    return p
+
+
+def policy_draw_bytes(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, count=None):
+    """taser_policy_draw_bytes -> workspace bytes of policy_draw."""
+    p, work = _draw_block(logits, uniform, temperature, top_k, top_p, min_p, count), ctypes.c_uint64()
+    _check(lib().taser_policy_draw_bytes(ctypes.byref(p), ctypes.byref(work)))
+    return work.value
+
+
+def policy_draw(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, count=None, stream=None):
+    """taser_policy_draw. logits [R, width] of float32, float16 or bfloat16 with contiguous rows; uniform float32[R, picks] in [0, 1);
+    temperature, top_p, min_p a number or float32[R], top_k a number or int32[R]; count int32[R]. Returns (actions int32[R, picks],
+    logp float32[R, picks]): what policy_loss takes as actions and old_logp. A row without candidates gives -1 and 0, one with a NaN or plus
+    infinity -1 and NaN."""
+    if stream is None:
+        r = (_native or _bind()).policy_draw(logits, uniform, temperature, top_k, top_p, min_p, count)
+        if r is not None:
+            return r
+    p, work = _draw_block(logits, uniform, temperature, top_k, top_p, min_p, count), ctypes.c_uint64()
+    with _guard(logits.device, stream):
+        _check(lib().taser_policy_draw_bytes(ctypes.byref(p), ctypes.byref(work)))
+        actions, logp = (_result(uniform.shape, dtype, logits.device, stream) for dtype in (torch.int32, torch.float32))
+        with _pool_of(stream):
+            scratch = _scratch(work.value, logits.device)
+        _check(lib().taser_policy_draw(ctypes.byref(p), _ptr(actions), _ptr(logp), _ptr(scratch), work.value, _stream(stream)))
+    return actions, logp
+
+
+def _norm_block(x, weight, bias, eps):
+    _strided(x, 2, _TYPES, "x")
+    rows, width = x.shape
+    n = _Norm(_TYPES[x.dtype], _TYPES[x.dtype], rows, width, x.stride(0) if rows > 1 else width, x.data_ptr(), None, None, eps)
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is None:
+            continue
+        if t.dtype not in (x.dtype, torch.float32):
+            raise TypeError(f"{name}: expected {x.dtype} or float32")
+        _same_device(_want(t, t.dtype, name), x.device, name)
+        if t.shape != (width,):
+            raise ValueError(f"{name} must be [width]")
+        if bias is not None and weight is not None and weight.dtype != bias.dtype:
+            raise TypeError("weight and bias: expected one type")
+        n.weight_type = _TYPES[t.dtype]
+        setattr(n, name, t.data_ptr())
+    return n
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, want_stats=False, stream=None):
+    """taser_layer_norm. x [R, width] of float32, float16 or bfloat16 with contiguous rows; weight and bias [width] of x's type or float32.
+    Returns out (like x, dense), with `want_stats` also stats float32[R, 2]: the rows' means and reciprocal deviations, which layer_norm_grad
+    takes. Results are detached; adaptive_training has an autograd function."""
+    if stream is None:
+        r = (_native or _bind()).layer_norm(x, weight, bias, eps, want_stats)
+        if r is not None:
+            return r
+    n = _norm_block(x, weight, bias, eps)
+    with _guard(x.device, stream):
+        out = _result(x.shape, x.dtype, x.device, stream)
+        stats = _result((x.shape[0], 2), torch.float32, x.device, stream) if want_stats else None
+        _check(lib().taser_layer_norm(ctypes.byref(n), _ptr(out), _ptr(stats), _stream(stream)))
+    return (out, stats) if want_stats else out
+
+
+def layer_norm_grad(dout, x, stats, weight=None, bias=None, stream=None):
+    """taser_layer_norm_grad: the gradients of layer_norm's sum(out * dout) -> (dx, dweight or None, dbias or None), dense, dweight and dbias of
+    their type where weight and bias are given. dout [R, width] of x's type with contiguous rows; stats as layer_norm(want_stats=True) gave
+    them for the same x and eps."""
+    if stream is None:
+        r = (_native or _bind()).layer_norm_grad(dout, x, stats, weight, bias)
+        if r is not None:
+            return r
+    n, work = _norm_block(x, weight, bias, 0.0), ctypes.c_uint64()
+    _strided(dout, 2, x.dtype, "dout", x.device)
+    if dout.shape != x.shape:
+        raise ValueError("dout must have x's shape")
+    _same_device(_want(stats, torch.float32, "stats"), x.device, "stats")
+    if stats.shape != (x.shape[0], 2):
+        raise ValueError("stats must be those that layer_norm gave")
+    with _guard(x.device, stream):
+        if weight is not None or bias is not None:
+            _check(lib().taser_layer_norm_grad_bytes(ctypes.byref(n), ctypes.byref(work)))
+        dx = _result(x.shape, x.dtype, x.device, stream)
+        dweight, dbias = (None if t is None else _result(t.shape, t.dtype, x.device, stream) for t in (weight, bias))
+        with _pool_of(stream):
+            scratch = _scratch(work.value, x.device)
+        _check(lib().taser_layer_norm_grad(ctypes.byref(n), _ptr(stats), _ptr(dout), dout.stride(0) if x.shape[0] > 1 else x.shape[1], _ptr(dx), _ptr(dweight), _ptr(dbias),
+                                           _ptr(scratch), work.value, _stream(stream)))
+    return dx, dweight, dbias
+
+
+def layer_norm_grad_bytes(x, weight=None, bias=None):
+    """taser_layer_norm_grad_bytes -> workspace bytes of layer_norm_grad where it gives dweight or dbias."""
+    n, work = _norm_block(x, weight, bias, 0.0), ctypes.c_uint64()
+    _check(lib().taser_layer_norm_grad_bytes(ctypes.byref(n), ctypes.byref(work)))
+    return work.value
+
+
+def adamw_state(params, bits=32):
+    """Moments of zero for adamw_step -> (m, v, units): lists of a tensor for each of params, float32 like it and units None, or with bits=8 codes
+    uint8 like it and units a pair of lists of float32, one for every 256 neighbors."""
+    if bits not in (8, 32):
+        raise ValueError("bits must be 8 or 32")
+    m, v = ([torch.zeros(p.shape, dtype=torch.uint8 if bits == 8 else torch.float32, device=p.device) for p in params] for _ in range(2))
+    if bits == 32:
+        return m, v, None
+    return m, v, tuple([torch.zeros(-(-p.numel() // ADAMW_BLOCK), device=p.device) for p in params] for _ in range(2))
+
+
+def _scalar_at(x, dtype, name, device):
+    _same_device(_want(x, dtype, name), device, name)
+    if x.numel() != 1:
+        raise ValueError(f"{name} must be one number")
+    return x.data_ptr()
+
+
+def adamw_step(params, grads, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, units=None, grad_scale=None, seed=0, stream=None):
+    """taser_adamw_step: updates params, m and v (and units) in place. params: tensors of float32, float16 or bfloat16, on one device; grads: as many, of
+    any of the three types, or None for a tensor that is to be left as it is; m, v, units as adamw_state made them (8 bits where units are
+    given). Tensors are contiguous. step: this one's number, from 1, or an int64 tensor that holds it; lr: a number or a float32 tensor;
+    grad_scale: a float32 tensor that gradients are multiplied by (where it is NaN nothing changes); seed: of the roundings to 8 bits.
+    For groups of parameters with rates of their own, one call each."""
+    params, grads, m, v = (x if isinstance(x, list) else list(x) for x in (params, grads, m, v))
+    if stream is None:
+        r = (_native or _bind()).adamw_step(params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, units, grad_scale, seed)
+        if r is not None:
+            return
+    n, kept = len(params), torch.float32 if units is None else torch.uint8
+    m_units, v_units = ([None] * n, [None] * n) if units is None else units
+    if not len(grads) == len(m) == len(v) == len(m_units) == len(v_units) == n:
+        raise ValueError("there must be a gradient (or None), moments and units for each parameter")
+    a, tensors = _Adamw(32 if units is None else 8, 0, None, 0.0, beta1, beta2, eps, weight_decay, None, None, seed & (2 ** 64 - 1)), (_AdamwTensor * max(n, 1))()
+    device = params[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    for i, (p, g) in enumerate(zip(params, grads)):
+        if p.dtype not in _TYPES:
+            raise TypeError(f"parameter {i}: expected float32, float16 or bfloat16")
+        _same_device(_want(p, p.dtype, f"parameter {i}"), device, f"parameter {i}")
+        t = tensors[i]
+        t.type, t.elements, t.param = _TYPES[p.dtype], p.numel(), p.data_ptr()
+        for name, x, dtype, size in (("m", m[i], kept, p.numel()), ("v", v[i], kept, p.numel()), ("m_unit", m_units[i], torch.float32, -(-p.numel() // ADAMW_BLOCK)),
+                                     ("v_unit", v_units[i], torch.float32, -(-p.numel() // ADAMW_BLOCK))):
+            if x is None and units is None and name.endswith("unit"):
+                continue
+            _same_device(_want(x, dtype, f"{name} {i}"), device, f"{name} {i}")
+            if x.numel() != size:
+                raise ValueError(f"{name} {i} must hold {size} numbers")
+            setattr(t, name, x.data_ptr())
+        if g is not None:
+            if g.dtype not in _TYPES:
+                raise TypeError(f"gradient {i}: expected float32, float16 or bfloat16")
+            _same_device(_want(g, g.dtype, f"gradient {i}"), device, f"gradient {i}")
+            if g.shape != p.shape:
+                raise ValueError(f"gradient {i} must have its parameter's shape")
+            t.grad_type, t.grad = _TYPES[g.dtype], g.data_ptr()
+    if isinstance(step, torch.Tensor):
+        a.step_at = _scalar_at(step, torch.int64, "step", device)
+    else:
+        a.step = step
+    if isinstance(lr, torch.Tensor):
+        a.lr_at = _scalar_at(lr, torch.float32, "lr", device)
+    else:
+        a.lr = lr
+    if grad_scale is not None:
+        a.grad_scale = _scalar_at(grad_scale, torch.float32, "grad_scale", device)
+    with _guard(device, stream):
+        _check(lib().taser_adamw_step(ctypes.byref(a), tensors, n, _stream(stream)))
+
+
+def adamw_moments(m, v, units, dtype=torch.float32, stream=None):
+    """taser_adamw_moments: one tensor's 8-bit moments (codes uint8, units a pair of float32[ceil(n / 256)]) as numbers -> (m, v) of `dtype`, shaped like
+    the codes."""
+    _want(m, torch.uint8, "m")
+    m_unit, v_unit = units
+    for name, t, like in (("v", v, torch.uint8), ("m's unit", m_unit, torch.float32), ("v's unit", v_unit, torch.float32)):
+        _same_device(_want(t, like, name), m.device, name)
+    if dtype not in _TYPES:
+        raise TypeError("dtype: expected float32, float16 or bfloat16")
+    if v.shape != m.shape or m_unit.numel() != -(-m.numel() // ADAMW_BLOCK) or v_unit.numel() != m_unit.numel():
+        raise ValueError("m and v must have one shape, and a unit for every 256 of their elements")
+    with _guard(m.device, stream):
+        out = [_result(m.shape, dtype, m.device, stream) for _ in range(2)]
+        _check(lib().taser_adamw_moments(_ptr(m), _ptr(v), _ptr(m_unit), _ptr(v_unit), m.numel(), _TYPES[dtype], _ptr(out[0]), _ptr(out[1]), _stream(stream)))
+    return tuple(out)
 
 
 def profile_begin():

@@ -12,6 +12,7 @@
 #include <Python.h>
 
 #include <cmath>
+#include <vector>
 
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
@@ -39,6 +40,12 @@ struct Api {
     decltype(&taser_relative_bias) relative_bias;
     decltype(&taser_relative_bias_grad) relative_bias_grad;
     decltype(&taser_policy_loss) policy_loss;
+    decltype(&taser_policy_draw_bytes) policy_draw_bytes;
+    decltype(&taser_policy_draw) policy_draw;
+    decltype(&taser_layer_norm) layer_norm;
+    decltype(&taser_layer_norm_grad_bytes) layer_norm_grad_bytes;
+    decltype(&taser_layer_norm_grad) layer_norm_grad;
+    decltype(&taser_adamw_step) adamw_step;
     decltype(&taser_last_error) last_error;
 } api;
 PyObject* error_class = nullptr;                                  // TaserError
@@ -608,6 +615,227 @@ PyObject* policy(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- a policy's draws, layer norm, AdamW -------------------------------------------------------
+// Calls on another device than the current one are the general half's.
+bool is_current(const at::Tensor* t) { return t->device().index() == c10::hip::current_device(); }
+const at::Tensor* beside(const at::Tensor* t, const at::Tensor& other) { return t && t->device() == other.device() ? t : nullptr; }
+bool get_number(PyObject* o, double* v) {
+    if (PyFloat_CheckExact(o)) {
+        *v = PyFloat_AS_DOUBLE(o);
+        return true;
+    }
+    int64_t i;
+    if (!get_int(o, -((int64_t)1 << 53), (int64_t)1 << 53, &i)) return false;
+    *v = (double)i;
+    return true;
+}
+
+// (logits, uniform, temperature, top_k, top_p, min_p, count), on torch's current stream
+PyObject* policy_draw(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_policy_draws p = {};
+    void* stream;
+    const at::Tensor* logits = n_args == 7 ? plain(o[0]) : nullptr;
+    if (!logits || !element_type(logits->scalar_type(), &p.type) || !(logits = strided(o[0], 2, logits->scalar_type())) || !is_current(logits)) return not_plain();
+    const at::Tensor* uniform = beside(device_array(o[1], at::kFloat), *logits);
+    if (!uniform || uniform->dim() != 2 || uniform->size(0) != logits->size(0) || uniform->size(1) > TASER_MAX_PICKS) return not_plain();
+    p.rows = logits->size(0);
+    p.width = logits->size(1);
+    p.logits_stride = p.rows > 1 ? logits->stride(0) : p.width;
+    p.picks = (int32_t)uniform->size(1);
+    p.logits = logits->data_ptr();
+    p.uniform = static_cast<const float*>(uniform->data_ptr());
+    struct { PyObject* given; float* one; const float** rows; } of[3] = {{o[2], &p.temperature, &p.row_temperature}, {o[4], &p.top_p, &p.row_top_p}, {o[5], &p.min_p, &p.row_min_p}};
+    for (auto& x : of) {
+        double v;
+        if (get_number(x.given, &v)) {
+            *x.one = (float)v;
+            continue;
+        }
+        const at::Tensor* t = beside(device_array(x.given, at::kFloat), *logits);
+        if (!t || t->numel() != p.rows) return not_plain();
+        *x.rows = static_cast<const float*>(t->data_ptr());
+    }
+    int64_t k;
+    if (get_int(o[3], INT32_MIN, INT32_MAX, &k)) {
+        p.top_k = (int32_t)k;
+    } else {
+        const at::Tensor* t = beside(device_array(o[3], at::kInt), *logits);
+        if (!t || t->numel() != p.rows) return not_plain();
+        p.row_top_k = static_cast<const int32_t*>(t->data_ptr());
+    }
+    if (o[6] != Py_None) {
+        const at::Tensor* t = beside(device_array(o[6], at::kInt), *logits);
+        if (!t || t->numel() != p.rows) return not_plain();
+        p.count = static_cast<const int32_t*>(t->data_ptr());
+    }
+    uint64_t bytes = 0;
+    if (!get_stream(Py_None, &stream)) return not_plain();
+    if (const int rc = api.policy_draw_bytes(&p, &bytes)) return raise(rc);
+    const at::Tensor actions = make(uniform->sizes(), at::kInt, logits->device()), logp = make(uniform->sizes(), at::kFloat, logits->device()), work = scratch(bytes, *logits);
+    void *p_actions = actions.data_ptr(), *p_logp = logp.data_ptr(), *p_work = bytes ? work.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.policy_draw(&p, static_cast<int32_t*>(p_actions), static_cast<float*>(p_logp), p_work, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    Ref x(THPVariable_Wrap(actions)), y(THPVariable_Wrap(logp));
+    return x.p && y.p ? PyTuple_Pack(2, x.p, y.p) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, weight, bias) -> the argument block
+bool norm_block(PyObject* const* o, taser_norm* n, const at::Tensor** x, const at::Tensor* (&kept)[2]) {
+    *n = taser_norm{};
+    const at::Tensor* t = plain(o[0]);
+    if (!t || !element_type(t->scalar_type(), &n->type) || !(t = strided(o[0], 2, t->scalar_type())) || !is_current(t)) return false;
+    n->weight_type = n->type;
+    n->rows = t->size(0);
+    n->width = t->size(1);
+    n->x_stride = n->rows > 1 ? t->stride(0) : n->width;
+    n->x = t->data_ptr();
+    for (int i = 0; i < 2; ++i) {
+        kept[i] = nullptr;
+        if (o[1 + i] == Py_None) continue;
+        const at::Tensor* w = plain(o[1 + i]);
+        if (!w || (w->scalar_type() != t->scalar_type() && w->scalar_type() != at::kFloat) || !beside(device_array(o[1 + i], w->scalar_type()), *t) || w->dim() != 1 || w->size(0) != n->width)
+            return false;
+        if (i && kept[0] && kept[0]->scalar_type() != w->scalar_type()) return false;
+        if (!element_type(w->scalar_type(), &n->weight_type)) return false;
+        kept[i] = w;
+    }
+    n->weight = kept[0] ? kept[0]->data_ptr() : nullptr;
+    n->bias = kept[1] ? kept[1]->data_ptr() : nullptr;
+    *x = t;
+    return true;
+}
+
+// (x, weight, bias, eps, want_stats), on torch's current stream
+PyObject* layer_norm(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_norm n;
+    const at::Tensor *x, *kept[2];
+    void* stream;
+    double eps;
+    if (n_args != 5 || !PyBool_Check(o[4]) || !norm_block(o, &n, &x, kept) || !get_number(o[3], &eps) || !get_stream(Py_None, &stream)) return not_plain();
+    n.eps = (float)eps;
+    const at::Tensor out = make(x->sizes(), x->scalar_type(), x->device());
+    at::Tensor stats;
+    if (o[4] == Py_True) stats = make({n.rows, 2}, at::kFloat, x->device());
+    void *p_out = out.data_ptr(), *p_stats = stats.defined() ? stats.data_ptr() : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.layer_norm(&n, p_out, static_cast<float*>(p_stats), stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    if (o[4] != Py_True) return THPVariable_Wrap(out);
+    Ref a(THPVariable_Wrap(out)), b(THPVariable_Wrap(stats));
+    return a.p && b.p ? PyTuple_Pack(2, a.p, b.p) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// (dout, x, stats, weight, bias), on torch's current stream
+PyObject* layer_norm_grad(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_norm n;
+    const at::Tensor *x, *kept[2];
+    void* stream;
+    if (n_args != 5) return not_plain();
+    PyObject* const block[3] = {o[1], o[3], o[4]};
+    if (!norm_block(block, &n, &x, kept) || !get_stream(Py_None, &stream)) return not_plain();
+    const at::Tensor *dout = beside(strided(o[0], 2, x->scalar_type()), *x), *stats = beside(device_array(o[2], at::kFloat), *x);
+    if (!dout || dout->sizes() != x->sizes() || !stats || stats->dim() != 2 || stats->size(0) != n.rows || stats->size(1) != 2) return not_plain();
+    uint64_t bytes = 0;
+    if (kept[0] || kept[1])
+        if (const int rc = api.layer_norm_grad_bytes(&n, &bytes)) return raise(rc);
+    const at::Tensor dx = make(x->sizes(), x->scalar_type(), x->device()), work = scratch(bytes, *x);
+    at::Tensor grads[2];
+    for (int i = 0; i < 2; ++i)
+        if (kept[i]) grads[i] = make({n.width}, kept[i]->scalar_type(), x->device());
+    const void *p_stats = stats->data_ptr(), *p_dout = dout->data_ptr();
+    void *p_dx = dx.data_ptr(), *p_work = bytes ? work.data_ptr() : nullptr, *p_grads[2] = {kept[0] ? grads[0].data_ptr() : nullptr, kept[1] ? grads[1].data_ptr() : nullptr};
+    const int64_t stride = n.rows > 1 ? dout->stride(0) : n.width;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.layer_norm_grad(&n, static_cast<const float*>(p_stats), p_dout, stride, p_dx, p_grads[0], p_grads[1], p_work, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    Ref a(THPVariable_Wrap(dx)), b(kept[0] ? THPVariable_Wrap(grads[0]) : nullptr), c(kept[1] ? THPVariable_Wrap(grads[1]) : nullptr);
+    if (!a.p || (kept[0] && !b.p) || (kept[1] && !c.p)) return nullptr;
+    return PyTuple_Pack(3, a.p, b.p ? b.p : Py_None, c.p ? c.p : Py_None);
+    END_HANDLE_TH_ERRORS
+}
+
+// (params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, units, grad_scale, seed), on torch's current stream. None: not the plain case; True: done
+PyObject* adamw_step(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    taser_adamw a = {};
+    void* stream;
+    if (n_args != 13) return not_plain();
+    PyObject* lists[6] = {o[0], o[1], o[2], o[3], nullptr, nullptr};
+    const bool bytes = o[10] != Py_None;
+    if (bytes) {
+        if (!PyTuple_CheckExact(o[10]) || PyTuple_GET_SIZE(o[10]) != 2) return not_plain();
+        lists[4] = PyTuple_GET_ITEM(o[10], 0);
+        lists[5] = PyTuple_GET_ITEM(o[10], 1);
+    }
+    for (PyObject* list : lists)
+        if (list && (!PyList_CheckExact(list) || PyList_GET_SIZE(list) != PyList_GET_SIZE(lists[0]))) return not_plain();
+    const Py_ssize_t n = PyList_GET_SIZE(lists[0]);
+    if (!n) return not_plain();
+    std::vector<taser_adamw_tensor> tensors((size_t)n);
+    const at::Tensor* first = plain(PyList_GET_ITEM(lists[0], 0));
+    if (!first || !first->is_cuda() || !is_current(first)) return not_plain();
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        taser_adamw_tensor& t = tensors[(size_t)i];
+        PyObject *param = PyList_GET_ITEM(lists[0], i), *grad = PyList_GET_ITEM(lists[1], i);
+        const at::Tensor* p = plain(param);
+        if (!p || !element_type(p->scalar_type(), &t.type) || !beside(device_array(param, p->scalar_type()), *first)) return not_plain();
+        t.elements = p->numel();
+        t.param = p->data_ptr();
+        if (grad != Py_None) {
+            const at::Tensor* g = plain(grad);
+            if (!g || !element_type(g->scalar_type(), &t.grad_type) || !beside(device_array(grad, g->scalar_type()), *first) || g->sizes() != p->sizes()) return not_plain();
+            t.grad = g->data_ptr();
+        }
+        void* moments[4] = {};
+        for (int j = 0; j < (bytes ? 4 : 2); ++j) {
+            const at::Tensor* x = beside(device_array(PyList_GET_ITEM(lists[2 + j], i), j < 2 && bytes ? at::kByte : at::kFloat), *first);
+            if (!x || x->numel() != (j < 2 ? t.elements : (t.elements + TASER_ADAMW_BLOCK - 1) / TASER_ADAMW_BLOCK)) return not_plain();
+            moments[j] = x->data_ptr();
+        }
+        t.m = moments[0];
+        t.v = moments[1];
+        t.m_unit = static_cast<float*>(moments[2]);
+        t.v_unit = static_cast<float*>(moments[3]);
+    }
+    a.bits = bytes ? 8 : 32;
+    if (!get_int(o[4], INT64_MIN, INT64_MAX, &a.step)) {
+        const at::Tensor* t = beside(device_array(o[4], at::kLong), *first);
+        if (!t || t->numel() != 1) return not_plain();
+        a.step_at = static_cast<const int64_t*>(t->data_ptr());
+    }
+    if (!get_number(o[5], &a.lr)) {
+        const at::Tensor* t = beside(device_array(o[5], at::kFloat), *first);
+        if (!t || t->numel() != 1) return not_plain();
+        a.lr_at = static_cast<const float*>(t->data_ptr());
+    }
+    if (!get_number(o[6], &a.beta1) || !get_number(o[7], &a.beta2) || !get_number(o[8], &a.eps) || !get_number(o[9], &a.weight_decay) || !get_u64(o[12], &a.seed) || !get_stream(Py_None, &stream))
+        return not_plain();
+    if (o[11] != Py_None) {
+        const at::Tensor* t = beside(device_array(o[11], at::kFloat), *first);
+        if (!t || t->numel() != 1) return not_plain();
+        a.grad_scale = static_cast<const float*>(t->data_ptr());
+    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.adamw_step(&a, tensors.data(), (int64_t)n, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(TaserError, {entry point: address})
 template <typename F> bool entry(PyObject* addresses, const char* name, F* to) {
     PyObject* o = PyDict_GetItemString(addresses, name);
@@ -628,7 +856,10 @@ PyObject* bind(PyObject*, PyObject* args) {
         !entry(addresses, "taser_cross_attention_bytes", &to.cross_attention_bytes) || !entry(addresses, "taser_cross_attention", &to.cross_attention) ||
         !entry(addresses, "taser_cross_attention_grad", &to.cross_attention_grad) || !entry(addresses, "taser_relative_bias_bytes", &to.relative_bias_bytes) ||
         !entry(addresses, "taser_relative_bias", &to.relative_bias) || !entry(addresses, "taser_relative_bias_grad", &to.relative_bias_grad) ||
-        !entry(addresses, "taser_policy_loss", &to.policy_loss) || !entry(addresses, "taser_last_error", &to.last_error))
+        !entry(addresses, "taser_policy_loss", &to.policy_loss) || !entry(addresses, "taser_policy_draw_bytes", &to.policy_draw_bytes) ||
+        !entry(addresses, "taser_policy_draw", &to.policy_draw) || !entry(addresses, "taser_layer_norm", &to.layer_norm) ||
+        !entry(addresses, "taser_layer_norm_grad_bytes", &to.layer_norm_grad_bytes) || !entry(addresses, "taser_layer_norm_grad", &to.layer_norm_grad) ||
+        !entry(addresses, "taser_adamw_step", &to.adamw_step) || !entry(addresses, "taser_last_error", &to.last_error))
         return nullptr;
     api = to;
     Py_INCREF(cls);
@@ -640,6 +871,7 @@ PyObject* bind(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, FAST("sample", sample), FAST("gather", gather), FAST("encodings", encodings),
                          FAST("select", select), FAST("lookup", lookup), FAST("draw", draw), FAST("update", update), FAST("scores", scores),
                          FAST("attention", attention), FAST("attention_grad", attention_grad), FAST("bias", bias), FAST("bias_grad", bias_grad), FAST("policy", policy),
+                         FAST("policy_draw", policy_draw), FAST("layer_norm", layer_norm), FAST("layer_norm_grad", layer_norm_grad), FAST("adamw_step", adamw_step),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Native half of the Python binding, built for " TASER_BINDING_TAG ".", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

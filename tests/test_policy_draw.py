@@ -1,0 +1,281 @@
+"""Draws from a policy's logits against their definition in 64 bits (GPU), the oracle against counting by hand (CPU)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_05396_amd as T
+from oracle import operators as O
+
+KINDS = {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}
+gpu = pytest.mark.gpu
+PLAIN = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+
+
+class Absent:
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+def _case(kind, R, W, n=1, seed=0, count=False, spread=2.0, **settings):
+    g = torch.Generator().manual_seed(seed)
+    c = dict(kind=kind, logits=(torch.randn((R, W), generator=g) * spread).to(KINDS[kind]), uniform=torch.rand((R, n), generator=g), count=None, **{**PLAIN, **settings})
+    if count:
+        c["count"] = torch.randint(0, W + 2, (R,), generator=g, dtype=torch.int32)
+    return c
+
+
+def _rows(R, seed):
+    """Settings of each row's own, among them those that switch something off."""
+    g = torch.Generator().manual_seed(seed)
+    one = lambda values, dtype=torch.float32: torch.tensor(values, dtype=dtype)[torch.randint(0, len(values), (R,), generator=g)]
+    return dict(temperature=one([0.0, 0.3, 0.7, 1.0, 1.7, 30.0]), top_k=one([0, 1, 2, 5, 40, 10 ** 6, -3], torch.int32), top_p=one([1.0, 0.0, 0.1, 0.5, 0.9, 0.999, 1.5]),
+                min_p=one([0.0, 0.001, 0.1, 0.7, 1.0, -1.0]))
+
+
+def _run(c, **more):
+    d = lambda t: t.cuda() if isinstance(t, torch.Tensor) else t
+    return T.policy_draw(d(c["logits"]), d(c["uniform"]), **{n: d(c[n]) for n in PLAIN}, count=d(c["count"]), **more)
+
+
+def _as_given(x):
+    """A setting as the kernels have it: in 32 bits, in its range."""
+    return x.numpy() if isinstance(x, torch.Tensor) else np.float32(x)
+
+
+def _check(c, share=0.98):
+    actions, logp = (t.cpu().numpy() for t in _run(c))
+    want, l, off, sure = O.policy_draw(c["logits"].double().numpy(), c["uniform"].double().numpy(), **{n: _as_given(c[n]) for n in PLAIN}, count=c["count"])
+    assert sure.mean() >= share and actions.dtype == np.int32 and logp.dtype == np.float32
+    wrong = (actions != want) & sure
+    assert not wrong.any(), [(int(r), int(j), int(actions[r, j]), int(want[r, j])) for r, j in zip(*np.nonzero(wrong))][:5]
+    same = actions == want
+    assert np.array_equal(np.isnan(logp), np.isnan(l)) and (np.abs(logp - l) <= off)[same & ~np.isnan(l)].all()
+    return actions, logp
+
+
+SHAPES = [(1, 1, 1), (700, 25, 10), (333, 16, 4), (65, 17, 3), (64, 33, 1), (40, 64, 64), (50, 3, 60), (33, 65, 1), (30, 130, 40), (9, 1000, 5), (7, 4096, 3), (5, 8192, 2), (5, 8193, 64), (3, 33_001, 2),
+          (2, 70_001, 3)]
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_against_64_bits(kind, shape):
+    for i, settings in enumerate((PLAIN, dict(temperature=0.7, top_k=12), dict(temperature=1.3, top_p=0.8), dict(min_p=0.05), dict(temperature=0.9, top_k=30, top_p=0.6, min_p=0.02), dict(temperature=0.0))):
+        _check(_case(kind, *shape, seed=shape[1] + i, count=i in (1, 4), **settings))
+    _check(_case(kind, *shape, seed=shape[1], count=True, **_rows(shape[0], shape[1])))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_flat_and_steep_rows(kind):
+    """Equal logits throughout; a few values many times over; one far above the rest; spreads that leave most weights at 0."""
+    for W in (20, 300, 9000, 70_000):
+        for settings in (PLAIN, dict(top_k=7), dict(top_p=0.3), dict(top_k=W // 2, top_p=0.5), dict(temperature=0.01, top_p=0.9), dict(temperature=50.0, top_p=0.7, top_k=W - 1)):
+            c = _case(kind, 4, W, 5, seed=W, **settings)
+            c["logits"][0] = 1.5
+            c["logits"][1] = (c["logits"][1].float() * 0.5).round().to(KINDS[kind])
+            c["logits"][2, W // 3] = 60.0
+            c["logits"][3] = (c["logits"][3].float() * 100).to(KINDS[kind])
+            _check(c, share=0.9)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_the_smallest_and_largest_numbers(kind):
+    for W in (30, 500, 9000):
+        c = _case(kind, 3, W, 8, seed=2, top_p=0.95)
+        c["uniform"] = torch.tensor([0.0, 2.0 ** -24, 1 - 2.0 ** -24, 1.0, 7.0, -1.0, float("nan"), 0.5]).repeat(3, 1)
+        actions, _ = (t.cpu() for t in _run(c))
+        given = dict(c, uniform=torch.nan_to_num(c["uniform"], nan=1.0).clamp(0, 1))
+        want, _, _, sure = O.policy_draw(c["logits"].double().numpy(), given["uniform"].double().numpy(), top_p=np.float32(0.95))
+        assert (actions.numpy() == want)[:, [0, 3, 4, 5, 6]].all() and ((actions.numpy() == want) | ~sure).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_what_takes_no_part_is_not_read(kind):
+    for R, W in ((50, 25), (6, 300), (4, 20_000)):
+        c = _case(kind, R, W, 3, seed=4, count=True, temperature=0.8, top_k=W // 2, top_p=0.9)
+        c["count"][0], c["count"][1] = 0, 1
+        past = torch.arange(W)[None] >= c["count"][:, None]
+        dirty = dict(c, logits=torch.where(past, torch.tensor(float("nan"), dtype=KINDS[kind]), c["logits"]))
+        a, b = _run(dirty), _check(c)
+        assert np.array_equal(a[0].cpu().numpy(), b[0]) and np.array_equal(a[1].cpu().numpy(), b[1])
+        assert (b[0][0] == -1).all() and not b[1][0].any() and (b[0][1] == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_logits_that_are_not_finite(kind):
+    for W in (20, 300, 9000):
+        for settings in (PLAIN, dict(temperature=0.0), dict(top_k=W // 3 + 1, top_p=0.9), dict(top_k=W - 1), dict(temperature=float("inf"))):
+            c = _case(kind, 7, W, 4, seed=9, **settings)
+            x = c["logits"]
+            x[0] = -float("inf")                    # all ruled out
+            x[1, ::2] = -float("inf")               # some
+            x[2, :] = -float("inf")
+            x[2, W - 1] = -3.0                      # but one
+            x[3, W // 2] = float("nan")
+            x[4, 1] = float("inf")
+            x[5, 2], x[5, 3] = -float("inf"), float("nan")
+            actions, logp = (t.cpu() for t in _run(c))
+            assert (actions[[0, 3, 4, 5]] == -1).all() and not logp[0].any() and torch.isnan(logp[3:6]).all()
+            assert (actions[1] % 2 == 1).all() and (actions[2] == W - 1).all() and not logp[2].any()
+            if settings.get("temperature") != float("inf"):
+                _check(c)
+
+
+@gpu
+def test_zeros_of_both_signs_are_one_value():
+    for W in (40, 3000):
+        x = torch.full((2, W), -5.0)
+        x[0, 3::2], x[0, 4::2] = 0.0, -0.0
+        x[1, 3::2], x[1, 4::2] = -0.0, 0.0
+        for settings in (dict(temperature=0.0), dict(top_k=1), dict(top_p=0.0), dict(top_k=3)):
+            c = dict(kind="float32", logits=x, uniform=torch.tensor([[0.1, 0.5, 0.9]] * 2), count=None, **{**PLAIN, **settings})
+            actions, _ = _check(c, share=0.6)
+            assert (actions <= (5 if settings == dict(top_k=3) else 3)).all()
+
+
+@gpu
+def test_frequencies():
+    """200 000 draws of 12 candidates: a candidate of chance p comes within 5 standard deviations, sqrt(p (1 - p) / n), of its share."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    n = 200_000
+    for W in (12, 100):
+        x = torch.randn((1, W), generator=g, device="cuda") * 1.5
+        actions, _ = T.policy_draw(x.expand(n // 50, W).contiguous(), torch.rand((n // 50, 50), generator=g, device="cuda"), temperature=0.8, top_k=10, top_p=0.95)
+        w = torch.softmax(x[0].double().cpu() / 0.8, 0)
+        order = torch.argsort(-w, stable=True)[:10]
+        share = w[order] / w[order].sum()
+        kept = order[(share.cumsum(0) - share) < 0.95]
+        p = torch.zeros(W, dtype=torch.float64)
+        p[kept] = w[kept] / w[kept].sum()
+        got = torch.bincount(actions.flatten().cpu(), minlength=W).double() / n
+        assert (got[p == 0] == 0).all() and ((got - p).abs() <= 5 * (p * (1 - p) / n).sqrt() + 1e-12).all()
+
+
+@gpu
+def test_strides_alignment_streams_and_bits(monkeypatch):
+    for kind, R, W, n in (("bfloat16", 9, 25, 3), ("float16", 5, 4097, 3), ("float32", 4, 777, 1), ("bfloat16", 3, 66_000, 2)):
+        c = _case(kind, R, W, n, seed=1, count=True, **_rows(R, W))
+        want = _run(c)
+        wide = torch.full((R, W + 7), float("nan"), dtype=KINDS[kind])
+        wide[:, 3:W + 3] = c["logits"]
+        view = wide.cuda()[:, 3:W + 3]
+        side = torch.cuda.Stream()
+        more = {m: c[m].cuda() for m in PLAIN}
+        u, count = c["uniform"].cuda(), c["count"].cuda()
+        side.wait_stream(torch.cuda.current_stream())
+        for stream in (None, side):
+            got = T.policy_draw(view, u, **more, count=count, stream=stream)
+            side.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        with monkeypatch.context() as m:
+            m.setattr(T, "_native", Absent())
+            assert all(torch.equal(a, b) for a, b in zip(_run(c), want))
+            numbers = dict(c, temperature=1, top_k=5, top_p=0.5, min_p=0)
+            ones = _run(numbers)
+        assert all(torch.equal(a, b) for a, b in zip(_run(numbers), ones))
+        rows = dict(c, temperature=torch.full((R,), 1.0), top_k=torch.full((R,), 5, dtype=torch.int32), top_p=torch.full((R,), 0.5), min_p=torch.zeros(R))
+        assert all(torch.equal(a, b) for a, b in zip(_run(rows), ones))
+
+
+@gpu
+def test_graph():
+    for W in (25, 5000, 70_000):
+        c = {n: t.cuda() if isinstance(t, torch.Tensor) else t for n, t in _case("float32", 30, W, 3, seed=5, temperature=0.7, top_k=40, top_p=0.9).items()}
+        call = lambda: _run(c)
+        call()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = call()
+        for _ in range(3):
+            c["logits"].normal_()
+            c["uniform"].uniform_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, call()))
+    empty = T.policy_draw(torch.zeros((0, 5), device="cuda"), torch.zeros((0, 2), device="cuda"))
+    assert [x.shape for x in empty] == [(0, 2), (0, 2)]
+
+
+@gpu
+@pytest.mark.parametrize("W", [25, 300, 20_000])
+def test_draws_are_what_the_loss_trains_on(W):
+    """The log-probabilities are the loss's own: its ratio is 1 where the policy has not changed."""
+    c = _case("float32", 50, W, 4, seed=3, count=True, temperature=0.6, top_p=0.9)
+    c["count"][0] = 0
+    actions, logp = _run(c)
+    loss, again, grad = T.policy_loss(c["logits"].cuda(), actions, torch.ones((50, 4), device="cuda"), old_logp=logp, count=c["count"].cuda())
+    # either log-probability: W + 16 roundings of the sum, 4 of terms of at most 30 in size
+    assert (again - logp).abs().max() <= 2 * ((W + 16) + 4 * 30) * O.E32
+    assert not loss[0].any() and not grad[0].any() and (loss[1:][actions[1:] >= 0] + 1).abs().max() <= 4 * ((W + 16) + 4 * 30) * O.E32
+
+
+@gpu
+def test_refusals_of_the_binding():
+    x, u = torch.zeros((4, 9), device="cuda"), torch.zeros((4, 2), device="cuda")
+    T.policy_draw(x, u)
+    assert T.policy_draw_bytes(x, u) >= 0
+    for bad in ((x.double(), u), (x[0], u), (x.t(), u), (x.cpu(), u), (x, u.double()), (x, u.cpu()), (x, u.t().contiguous().t())):
+        with pytest.raises(TypeError):
+            T.policy_draw(*bad)
+    one = torch.zeros(4, device="cuda")
+    for bad in (dict(temperature=one.double()), dict(top_k=one), dict(top_p=one.int()), dict(min_p=one.cpu()), dict(count=one)):
+        with pytest.raises(TypeError):
+            T.policy_draw(x, u, **bad)
+    for bad in (dict(temperature=one[:3]), dict(top_k=one.int()[:2]), dict(count=one.int()[:3])):
+        with pytest.raises(ValueError):
+            T.policy_draw(x, u, **bad)
+    for bad in ((x[:3], u), (x, u[0])):
+        with pytest.raises(ValueError):
+            T.policy_draw(*bad)
+    for bad in (dict(temperature=-0.1), dict(temperature=float("nan")), dict(top_k=-1), dict(top_p=-0.1), dict(top_p=1.1), dict(min_p=-0.1), dict(min_p=1.1), dict(top_p=float("nan"))):
+        with pytest.raises(T.TaserError):
+            T.policy_draw(x, u, **bad)
+    with pytest.raises(T.TaserError):
+        T.policy_draw(x, torch.zeros((4, 65), device="cuda"))
+
+
+# ---- without a GPU ----------------------------------------------------------------------------
+def test_argument_errors_without_a_gpu():
+    L, one, E_ARG, E_RANGE = T.lib(), ctypes.c_void_p(16), -1, -2
+
+    def block(**change):
+        p = T._PolicyDraws(0, 2, 3, 5, 5, 16, None, 16, 1.0, 1.0, 0.0, 0, None, None, None, None)
+        for n, x in change.items():
+            setattr(p, n, x)
+        return ctypes.byref(p)
+
+    size = ctypes.c_uint64()
+    assert L.taser_policy_draw(None, one, one, one, 2 ** 40, None) == E_ARG and L.taser_policy_draw_bytes(None, ctypes.byref(size)) == E_ARG and L.taser_policy_draw_bytes(block(), None) == E_ARG
+    for change, code in ((dict(type=3), E_ARG), (dict(rows=-1), E_ARG), (dict(width=0), E_ARG), (dict(picks=0), E_ARG), (dict(picks=65), E_RANGE), (dict(width=2 ** 20 + 1), E_RANGE),
+                         (dict(rows=2 ** 31), E_RANGE), (dict(temperature=-1.0), E_ARG), (dict(temperature=float("nan")), E_ARG), (dict(top_k=-1), E_ARG), (dict(top_p=1.5), E_ARG),
+                         (dict(top_p=float("nan")), E_ARG), (dict(min_p=-0.5), E_ARG), (dict(logits=None), E_ARG), (dict(uniform=None), E_ARG), (dict(logits_stride=4), E_ARG)):
+        assert L.taser_policy_draw(block(**change), one, one, one, 2 ** 40, None) == code, change
+    assert L.taser_policy_draw(block(), None, one, one, 2 ** 40, None) == E_ARG and L.taser_policy_draw(block(), one, None, one, 2 ** 40, None) == E_ARG
+    assert L.taser_policy_draw(block(rows=0), None, None, None, 0, None) == 0
+    for rows, width, picks in ((2 ** 28, 5, 2), (2 ** 26, 5, 40), (2 ** 24, 100, 2), (2 ** 22, 10_000, 2)):   # fewer than 2^32 threads to a launch
+        assert L.taser_policy_draw(block(rows=rows, width=width, logits_stride=width, picks=picks), one, one, one, 2 ** 40, None) == E_RANGE and "launch" in T.last_error()
+
+
+def test_the_oracle_by_hand():
+    x = np.log(np.array([[1.0, 4.0, 2.0, 4.0, 8.0, 1.0]]))
+    def kept(n=4000, **settings):
+        u = (np.arange(n)[None] + 0.5) / n
+        actions = O.policy_draw(x, u, **settings)[0][0]
+        return {int(a): float((actions == a).mean()) for a in np.unique(actions)}
+    near = lambda got, want: got.keys() == want.keys() and all(abs(got[a] - want[a]) < 1e-3 for a in want)
+    assert near(kept(), {0: 0.05, 1: 0.2, 2: 0.1, 3: 0.2, 4: 0.4, 5: 0.05})
+    assert near(kept(top_k=2), {1: 1 / 3, 4: 2 / 3})                       # of equal ones the first
+    assert near(kept(top_k=3, top_p=0.51), {1: 1 / 3, 4: 2 / 3})           # 8 of 16 are less than 0.51
+    assert near(kept(top_k=3, top_p=0.49), {4: 1.0})
+    assert near(kept(min_p=0.25), {1: 4 / 18, 2: 2 / 18, 3: 4 / 18, 4: 8 / 18})
+    assert near(kept(temperature=0.5, top_k=3), {1: 16 / 96, 3: 16 / 96, 4: 64 / 96})
+    assert near(kept(temperature=0.0), {4: 1.0}) and near(kept(top_p=0.0), {4: 1.0})
+    assert abs(O.policy_draw(x, np.array([[0.0]]), temperature=0.0)[1][0, 0] - np.log(0.4)) < 1e-12
+    assert O.policy_draw(x, np.array([[0.3]]), count=[0])[0][0, 0] == -1
