@@ -259,7 +259,7 @@ def test_argument_errors_without_a_gpu():
         assert L.taser_policy_draw(block(**change), one, one, one, 2 ** 40, None) == code, change
     assert L.taser_policy_draw(block(), None, one, one, 2 ** 40, None) == E_ARG and L.taser_policy_draw(block(), one, None, one, 2 ** 40, None) == E_ARG
     assert L.taser_policy_draw(block(rows=0), None, None, None, 0, None) == 0
-    for rows, width, picks in ((2 ** 28, 5, 2), (2 ** 26, 5, 40), (2 ** 24, 100, 2), (2 ** 22, 10_000, 2)):   # fewer than 2^32 threads to a launch
+    for rows, width, picks in ((2 ** 28, 5, 2), (2 ** 26, 5, 40), (2 ** 24, 100, 2), (2 ** 23, 10_000, 2)):   # fewer than 2^32 threads to a launch
         assert L.taser_policy_draw(block(rows=rows, width=width, logits_stride=width, picks=picks), one, one, one, 2 ** 40, None) == E_RANGE and "launch" in T.last_error()
 
 
