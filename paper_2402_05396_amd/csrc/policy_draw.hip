@@ -91,9 +91,20 @@ template <int G> __device__ inline uint64_t sum_of(uint64_t x) { return shuffle(
 
 // Rows of at most 64 candidates and draws: G lanes a row.
 template <typename T, int G> __global__ __launch_bounds__(256) void draw_window_kernel(const Draws p, const T* logits, int32_t* actions, float* logp) {
+    struct __attribute__((aligned(16))) Candidate {
+        float x;
+        uint64_t w;
+    };
+    __shared__ Candidate seen[256];   // each lane's, for the others of its row: one LDS read a look, where lanes asked for by number are three
+    __shared__ uint64_t sums[256];
     const int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
-    const int lane = threadIdx.x % G, first = threadIdx.x & 63 & ~(G - 1);
+    const int lane = threadIdx.x % G, first = threadIdx.x & 63 & ~(G - 1), row_at = threadIdx.x - lane;
     if (row >= p.rows) return;   // the lanes of a row leave together
+    // What this wave wrote to LDS is there for it to read.
+    auto written = [] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
     constexpr uint64_t lanes = G == 64 ? ~0ull : (1ull << (G & 63)) - 1;
     auto ballot = [&](bool yes) { return __ballot(yes) >> first & lanes; };
     const int n = taking_part(p, row);
@@ -116,12 +127,14 @@ template <typename T, int G> __global__ __launch_bounds__(256) void draw_window_
         if (rule.top_k || rule.top_p) {
             int rank = 0;
             uint64_t before = 0;
+            seen[threadIdx.x] = Candidate{x, w};
+            written();
+#pragma unroll 4
             for (int j = 0; j < n; ++j) {
-                const float other = __shfl(x, j, G);
-                const uint64_t weight = shuffle(w, j, G);
-                const bool ahead = other > x || (other == x && j < lane);
+                const Candidate other = seen[row_at + j];
+                const bool ahead = other.x > x || (other.x == x && j < lane);
                 rank += ahead;
-                before += ahead ? weight : 0;
+                before += ahead ? other.w : 0;
             }
             const bool in = !rule.top_k || rank < rule.top_k;
             const uint64_t share = share_of(rule.top_p, sum_of<G>(in ? w : 0));
@@ -132,12 +145,12 @@ template <typename T, int G> __global__ __launch_bounds__(256) void draw_window_
     const uint64_t upto = running<G>(w), whole = shuffle(upto, G - 1, G);
     const int64_t at = row * p.picks + lane;
     const uint64_t place = lane < p.picks ? place_of(p.uniform[at], whole) : 0;
-    int action = -1;
-    for (int j = 0; j < p.picks; ++j) {
-        const uint64_t hit = ballot(upto > shuffle(place, j, G));
-        if (lane == j) action = __ffsll((long long)hit) - 1;
-    }
-    const float chosen = __shfl(x, action < 0 ? 0 : action, G);
+    sums[threadIdx.x] = upto;
+    written();
+    int action = 0;   // the first sum past the place: they ascend
+#pragma unroll
+    for (int step = G / 2; step; step >>= 1) action += sums[row_at + action + step - 1] <= place ? step : 0;
+    const float chosen = __shfl(x, action, G);
     if (lane >= p.picks) return;
     actions[at] = none ? -1 : action;
     logp[at] = bad ? __builtin_nanf("") : none ? 0.f : (chosen - top) - logf(total);
