@@ -3,17 +3,16 @@
 //   out = xhat weight + bias,  xhat = (x - mean) rstd;  with g = dout weight:
 //   dx = rstd (g - mean(g) - xhat mean(g xhat)),  dweight = sum over rows of dout xhat,  dbias = sum over rows of dout
 //
-// Both are bound by reading and writing rows once. A row belongs to a group of G threads, each with up to 16 of its columns in registers:
+// Both are bound by reading and writing rows once. A row belongs to a group of threads, each with up to 16 of its columns (in the gradient 8) in registers:
 // mean first, then the squares of what is away from it (no difference of large sums). A group goes from row to row, its columns' weights and,
 // in the gradient, its columns' sums of dweight and dbias staying in registers, the next row on its way; a block adds its groups' sums
-// through LDS, a second launch the blocks', in an order that the sizes fix. Rows past 1024 threads' registers are read again for each
-// of their passes, and dweight and dbias come from a kernel of their own, by columns.
+// through LDS, a second launch the blocks', in an order that the sizes fix. Rows of more than 8192 are a block's each, held in registers up to 32768
+// and read again for each pass past that, and their dweight and dbias come from a kernel of their own, by columns.
 #include "pieces.h"
 
 namespace {
 
-constexpr int kColumns = 16;                  // of a thread
-constexpr int64_t kHeld = 1024 * kColumns;    // the longest row that is held
+constexpr int64_t kHeld = 8192;       // rows up to it stay in registers, with what belongs to their columns
 
 struct Norm {
     int64_t rows, width, x_stride, dout_stride;
@@ -22,35 +21,36 @@ struct Norm {
     float eps;
 };
 
-// Sums of two numbers over a group of G threads. Groups of more than a wave go through LDS, `turn` alternates between its two halves.
-template <int G> __device__ inline void group_sums(float& a, float& b, float2 (*shared)[16], int turn) {
+// Sums of two numbers over a group of threads: G lanes of a wave, or (G = 0) `waves` waves, by way of LDS, `turn` alternating between its two halves.
+template <int G> __device__ inline void group_sums(float& a, float& b, float2 (*shared)[16], int turn, int waves) {
+    constexpr int LANES = G ? G : 64;
 #pragma unroll
-    for (int m = 1; m < (G < 64 ? G : 64); m <<= 1) {
+    for (int m = 1; m < LANES; m <<= 1) {
         a += __shfl_xor(a, m);
         b += __shfl_xor(b, m);
     }
-    if (G <= 64) return;
-    const int wave = threadIdx.x >> 6, first = threadIdx.x / G * (G / 64);
+    if (G || waves == 1) return;
+    const int wave = threadIdx.x >> 6, first = wave / waves * waves;
     if ((threadIdx.x & 63) == 0) shared[turn & 1][wave] = make_float2(a, b);
     __syncthreads();
     a = b = 0.f;
-#pragma unroll
-    for (int w = 0; w < G / 64; ++w) {
-        a += shared[turn & 1][first + w].x;
-        b += shared[turn & 1][first + w].y;
+    for (int w = 0; w < waves; ++w) {
+        const float2 x = shared[turn & 1][first + w];
+        a += x.x;
+        b += x.y;
     }
 }
 
-// Columns of this thread: piece h at (h G + lane) EACH.
-template <typename T, int G, int HELD> __device__ inline void load_row(const T* row, int lane, int64_t width, TaserPiece<T> (&p)[HELD]) {
+// A thread's columns: piece h at (h threads + lane) EACH.
+template <typename T, int HELD> __device__ inline void load_row(const T* row, int threads, int lane, int64_t width, TaserPiece<T> (&p)[HELD]) {
 #pragma unroll
-    for (int h = 0; h < HELD; ++h) taser_load_piece<T>(row, (int64_t)(h * G + lane) * kTaserEach<T>, width, (T)0.f, p[h]);
+    for (int h = 0; h < HELD; ++h) taser_load_piece<T>(row, (int64_t)(h * threads + lane) * kTaserEach<T>, width, (T)0.f, p[h]);
 }
-template <typename T, int G, int HELD> __device__ inline void load_weights(const void* from, int32_t type, int lane, int64_t width, float none, float (&w)[HELD][kTaserEach<T>]) {
+template <typename T, int HELD> __device__ inline void load_weights(const void* from, int32_t type, int threads, int lane, int64_t width, float none, float (&w)[HELD][kTaserEach<T>]) {
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
         if (from) {
-            taser_load_floats<kTaserEach<T>>(from, type, (int64_t)(h * G + lane) * kTaserEach<T>, width, w[h]);
+            taser_load_floats<kTaserEach<T>>(from, type, (int64_t)(h * threads + lane) * kTaserEach<T>, width, w[h]);
         } else {
 #pragma unroll
             for (int i = 0; i < kTaserEach<T>; ++i) w[h][i] = none;
@@ -58,18 +58,19 @@ template <typename T, int G, int HELD> __device__ inline void load_weights(const
     }
 }
 
-template <typename T, int G, int HELD, int THREADS> __global__ __launch_bounds__(THREADS) void norm_kernel(const Norm p, const T* x, T* out, float* stats) {
-    constexpr int EACH = kTaserEach<T>, GROUPS = THREADS / G;
+// G: lanes of a group, or 0: groups of `waves` waves.
+template <typename T, int G, int HELD, int THREADS> __global__ __launch_bounds__(THREADS) void norm_kernel(const Norm p, int waves, const T* x, T* out, float* stats) {
+    constexpr int EACH = kTaserEach<T>;
     __shared__ float2 shared[2][16];
-    const int lane = threadIdx.x % G;
-    const int64_t group = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G, groups = (int64_t)gridDim.x * GROUPS, turns = (p.rows + groups - 1) / groups;
+    const int threads = G ? G : waves * 64, lane = threadIdx.x % threads, here = blockDim.x / threads;
+    const int64_t groups = (int64_t)gridDim.x * here, turns = (p.rows + groups - 1) / groups;
     float weight[HELD][EACH], bias[HELD][EACH];
-    load_weights<T, G, HELD>(p.weight, p.weight_type, lane, p.width, 1.f, weight);
-    load_weights<T, G, HELD>(p.bias, p.weight_type, lane, p.width, 0.f, bias);
+    load_weights<T, HELD>(p.weight, p.weight_type, threads, lane, p.width, 1.f, weight);
+    load_weights<T, HELD>(p.bias, p.weight_type, threads, lane, p.width, 0.f, bias);
     TaserPiece<T> next[HELD];
     // A group without a row of its own left takes the last one once more: it writes nothing.
-    int64_t row = group;
-    load_row<T, G, HELD>(x + (row < p.rows ? row : p.rows - 1) * p.x_stride, lane, p.width, next);
+    int64_t row = (int64_t)blockIdx.x * here + threadIdx.x / threads;
+    load_row<T, HELD>(x + (row < p.rows ? row : p.rows - 1) * p.x_stride, threads, lane, p.width, next);
     const float by = 1.f / (float)p.width;
     for (int64_t turn = 0; turn < turns; ++turn, row += groups) {
         float v[HELD][EACH];
@@ -78,18 +79,18 @@ template <typename T, int G, int HELD, int THREADS> __global__ __launch_bounds__
         for (int h = 0; h < HELD; ++h)
 #pragma unroll
             for (int i = 0; i < EACH; ++i) sum += v[h][i] = (float)next[h].x[i];
-        if (turn + 1 < turns) load_row<T, G, HELD>(x + (row + groups < p.rows ? row + groups : p.rows - 1) * p.x_stride, lane, p.width, next);
-        group_sums<G>(sum, none, shared, 0);
+        if (turn + 1 < turns) load_row<T, HELD>(x + (row + groups < p.rows ? row + groups : p.rows - 1) * p.x_stride, threads, lane, p.width, next);
+        group_sums<G>(sum, none, shared, 0, waves);
         const float mean = sum * by;
         float squares = 0.f;
 #pragma unroll
         for (int h = 0; h < HELD; ++h)
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                v[h][i] = (int64_t)(h * G + lane) * EACH + i < p.width ? v[h][i] - mean : 0.f;
+                v[h][i] = (int64_t)(h * threads + lane) * EACH + i < p.width ? v[h][i] - mean : 0.f;
                 squares = fmaf(v[h][i], v[h][i], squares);
             }
-        group_sums<G>(squares, none, shared, 1);
+        group_sums<G>(squares, none, shared, 1, waves);
         const float rstd = 1.f / sqrtf(squares * by + p.eps);
         if (row >= p.rows) continue;   // its last turn
         if (stats && lane == 0) {
@@ -101,130 +102,158 @@ template <typename T, int G, int HELD, int THREADS> __global__ __launch_bounds__
             TaserPiece<T> y;
 #pragma unroll
             for (int i = 0; i < EACH; ++i) y.x[i] = (T)fmaf(v[h][i] * rstd, weight[h][i], bias[h][i]);
-            taser_store_piece<T>(out + row * p.width, (int64_t)(h * G + lane) * EACH, p.width, y);
+            taser_store_piece<T>(out + row * p.width, (int64_t)(h * threads + lane) * EACH, p.width, y);
         }
     }
 }
 
-// Rows past 1024 threads' registers: a block each, read three times.
-template <typename T> __global__ __launch_bounds__(1024) void norm_wide_kernel(const Norm p, const T* x, T* out, float* stats) {
+template <typename T> __device__ inline void put_out(const Norm& p, int64_t c, float mean, float rstd, const TaserPiece<T>& v, T* to) {
+    constexpr int EACH = kTaserEach<T>;
+    float weight[EACH], bias[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) weight[i] = 1.f, bias[i] = 0.f;
+    if (p.weight) taser_load_floats<EACH>(p.weight, p.weight_type, c, p.width, weight);
+    if (p.bias) taser_load_floats<EACH>(p.bias, p.weight_type, c, p.width, bias);
+    TaserPiece<T> y;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) y.x[i] = (T)fmaf(((float)v.x[i] - mean) * rstd, weight[i], bias[i]);
+    taser_store_piece<T>(to, c, p.width, y);
+}
+
+// Longer rows: a block each. HELD pieces stay in registers; what is past them is read three times.
+template <typename T, int HELD> __global__ __launch_bounds__(1024) void norm_long_kernel(const Norm p, const T* x, T* out, float* stats) {
     constexpr int EACH = kTaserEach<T>;
     __shared__ float2 shared[2][16];
     const T* from = x + (int64_t)blockIdx.x * p.x_stride;
     T* to = out + (int64_t)blockIdx.x * p.width;
-    const int64_t step = 1024 * EACH;
+    const int waves = blockDim.x >> 6;
+    const int64_t step = blockDim.x * EACH, past = HELD * step + threadIdx.x * EACH;
+    TaserPiece<T> held[HELD], v;
+    load_row<T, HELD>(from, blockDim.x, threadIdx.x, p.width, held);
     float sum = 0.f, none = 0.f, squares = 0.f;
-    for (int64_t c = threadIdx.x * EACH; c < p.width; c += step) {
-        TaserPiece<T> v;
-        taser_load_piece<T>(from, c, p.width, (T)0.f, v);
+    auto add = [&](const TaserPiece<T>& piece) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) sum += (float)v.x[i];
-    }
-    group_sums<1024>(sum, none, shared, 0);
-    const float mean = sum / (float)p.width;
-    for (int64_t c = threadIdx.x * EACH; c < p.width; c += step) {
-        TaserPiece<T> v;
+        for (int i = 0; i < EACH; ++i) sum += (float)piece.x[i];
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) add(held[h]);
+    for (int64_t c = past; c < p.width; c += step) {
         taser_load_piece<T>(from, c, p.width, (T)0.f, v);
+        add(v);
+    }
+    group_sums<0>(sum, none, shared, 0, waves);
+    const float mean = sum / (float)p.width;
+    auto add_square = [&](const TaserPiece<T>& piece, int64_t c) {
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const float away = c + i < p.width ? (float)v.x[i] - mean : 0.f;
+            const float away = c + i < p.width ? (float)piece.x[i] - mean : 0.f;
             squares = fmaf(away, away, squares);
         }
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) add_square(held[h], h * step + threadIdx.x * EACH);
+    for (int64_t c = past; c < p.width; c += step) {
+        taser_load_piece<T>(from, c, p.width, (T)0.f, v);
+        add_square(v, c);
     }
-    group_sums<1024>(squares, none, shared, 1);
+    group_sums<0>(squares, none, shared, 1, waves);
     const float rstd = 1.f / sqrtf(squares / (float)p.width + p.eps);
     if (stats && threadIdx.x == 0) {
         stats[2 * (int64_t)blockIdx.x] = mean;
         stats[2 * (int64_t)blockIdx.x + 1] = rstd;
     }
-    for (int64_t c = threadIdx.x * EACH; c < p.width; c += step) {
-        TaserPiece<T> v;
-        float weight[EACH], bias[EACH];
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) put_out<T>(p, h * step + threadIdx.x * EACH, mean, rstd, held[h], to);
+    for (int64_t c = past; c < p.width; c += step) {
         taser_load_piece<T>(from, c, p.width, (T)0.f, v);
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) weight[i] = 1.f, bias[i] = 0.f;
-        if (p.weight) taser_load_floats<EACH>(p.weight, p.weight_type, c, p.width, weight);
-        if (p.bias) taser_load_floats<EACH>(p.bias, p.weight_type, c, p.width, bias);
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) v.x[i] = (T)fmaf(((float)v.x[i] - mean) * rstd, weight[i], bias[i]);
-        taser_store_piece<T>(to, c, p.width, v);
+        put_out<T>(p, c, mean, rstd, v, to);
     }
 }
 
+template <int S> struct Slot { static constexpr int value = S; };
+
 // dx, and of each block [2][width] sums of dout xhat and dout, if `parts` is given.
 template <typename T, int G, int HELD, int THREADS>
-__global__ __launch_bounds__(THREADS) void norm_grad_kernel(const Norm p, const T* x, const T* dout, const float* stats, T* dx, float* parts) {
-    constexpr int EACH = kTaserEach<T>, GROUPS = THREADS / G, COLUMNS = HELD * EACH;
+__global__ __launch_bounds__(THREADS) void norm_grad_kernel(const Norm p, int waves, const T* x, const T* dout, const float* stats, T* dx, float* parts) {
+    constexpr int EACH = kTaserEach<T>, COLUMNS = HELD * EACH;
     __shared__ float2 shared[2][16];
-    __shared__ float sums[GROUPS > 1 ? THREADS / 2 * COLUMNS : 1];
-    const int lane = threadIdx.x % G, mine = threadIdx.x / G;
-    const int64_t groups = (int64_t)gridDim.x * GROUPS, turns = (p.rows + groups - 1) / groups;
+    __shared__ float sums[THREADS <= 512 ? THREADS / 2 * COLUMNS : 1];   // (a block of more is one group)
+    const int threads = G ? G : waves * 64, lane = threadIdx.x % threads, mine = threadIdx.x / threads, here = blockDim.x / threads;
+    const int64_t groups = (int64_t)gridDim.x * here, turns = (p.rows + groups - 1) / groups;
     float weight[HELD][EACH], dweight[HELD][EACH] = {}, dbias[HELD][EACH] = {};
-    load_weights<T, G, HELD>(p.weight, p.weight_type, lane, p.width, 1.f, weight);
-    TaserPiece<T> next_x[HELD], next_y[HELD];
-    int64_t row = (int64_t)blockIdx.x * GROUPS + mine;
-    float2 next_stats;
-    auto load = [&](int64_t r) {
+    load_weights<T, HELD>(p.weight, p.weight_type, threads, lane, p.width, 1.f, weight);
+    // Two rows ahead of the one at hand are on their way (16 384 x 4096 bf16: 100 us with one).
+    TaserPiece<T> next_x[2][HELD], next_y[2][HELD];
+    float2 next_stats[2];
+    int64_t row = (int64_t)blockIdx.x * here + mine;
+    auto load = [&](int slot, int64_t r) {
         r = r < p.rows ? r : p.rows - 1;
-        load_row<T, G, HELD>(x + r * p.x_stride, lane, p.width, next_x);
-        load_row<T, G, HELD>(dout + r * p.dout_stride, lane, p.width, next_y);
-        next_stats = make_float2(stats[2 * r], stats[2 * r + 1]);
+        load_row<T, HELD>(x + r * p.x_stride, threads, lane, p.width, next_x[slot]);
+        load_row<T, HELD>(dout + r * p.dout_stride, threads, lane, p.width, next_y[slot]);
+        next_stats[slot] = make_float2(stats[2 * r], stats[2 * r + 1]);
     };
-    load(row);
+    load(0, row);
+    if (turns > 1) load(1, row + groups);
     const float by = 1.f / (float)p.width;
-    for (int64_t turn = 0; turn < turns; ++turn, row += groups) {
-        const float mean = next_stats.x, rstd = next_stats.y;
+    auto take = [&](auto at, int64_t turn) {   // the row in a slot
+        constexpr int slot = decltype(at)::value;
+        const float mean = next_stats[slot].x, rstd = next_stats[slot].y;
         float xhat[HELD][EACH], y[HELD][EACH];
         float a = 0.f, b = 0.f;
 #pragma unroll
         for (int h = 0; h < HELD; ++h)
 #pragma unroll
             for (int i = 0; i < EACH; ++i) {
-                xhat[h][i] = (int64_t)(h * G + lane) * EACH + i < p.width ? ((float)next_x[h].x[i] - mean) * rstd : 0.f;
-                y[h][i] = (float)next_y[h].x[i];
+                xhat[h][i] = (int64_t)(h * threads + lane) * EACH + i < p.width ? ((float)next_x[slot][h].x[i] - mean) * rstd : 0.f;
+                y[h][i] = (float)next_y[slot][h].x[i];
                 const float g = y[h][i] * weight[h][i];   // 0 past the row's end, where dout was taken as 0
                 a += g;
                 b = fmaf(g, xhat[h][i], b);
             }
-        if (turn + 1 < turns) load(row + groups);
-        group_sums<G>(a, b, shared, (int)turn);
-        if (row >= p.rows) continue;   // its last turn
-        a *= by;
-        b *= by;
+        if (turn + 2 < turns) load(slot, row + 2 * groups);
+        group_sums<G>(a, b, shared, slot, waves);
+        if (row < p.rows) {   // else its last turn
+            a *= by;
+            b *= by;
 #pragma unroll
-        for (int h = 0; h < HELD; ++h) {
-            TaserPiece<T> d;
+            for (int h = 0; h < HELD; ++h) {
+                TaserPiece<T> d;
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                d.x[i] = (T)(rstd * (fmaf(y[h][i], weight[h][i], -a) - xhat[h][i] * b));
-                dweight[h][i] = fmaf(y[h][i], xhat[h][i], dweight[h][i]);
-                dbias[h][i] += y[h][i];
+                for (int i = 0; i < EACH; ++i) {
+                    d.x[i] = (T)(rstd * (fmaf(y[h][i], weight[h][i], -a) - xhat[h][i] * b));
+                    dweight[h][i] = fmaf(y[h][i], xhat[h][i], dweight[h][i]);
+                    dbias[h][i] += y[h][i];
+                }
+                taser_store_piece<T>(dx + row * p.width, (int64_t)(h * threads + lane) * EACH, p.width, d);
             }
-            taser_store_piece<T>(dx + row * p.width, (int64_t)(h * G + lane) * EACH, p.width, d);
         }
+        row += groups;
+    };
+    for (int64_t turn = 0; turn < turns; turn += 2) {
+        take(Slot<0>(), turn);
+        if (turn + 1 < turns) take(Slot<1>(), turn + 1);
     }
     if (!parts) return;
-    // The upper half of the groups hands its sums to the lower half, until one has them all.
+    // The upper half of the groups (a power of two of them) hands its sums to the lower half, until one has them all.
     auto fold = [&](float (&of)[HELD][EACH]) {
-#pragma unroll
-        for (int half = GROUPS / 2; half >= 1; half >>= 1) {
+        for (int half = here / 2; half >= 1; half >>= 1) {
             __syncthreads();
             if (mine >= half && mine < 2 * half) {
 #pragma unroll
                 for (int h = 0; h < HELD; ++h)
 #pragma unroll
-                    for (int i = 0; i < EACH; ++i) sums[(h * EACH + i) * (half * G) + (mine - half) * G + lane] = of[h][i];
+                    for (int i = 0; i < EACH; ++i) sums[(h * EACH + i) * (half * threads) + (mine - half) * threads + lane] = of[h][i];
             }
             __syncthreads();
             if (mine < half) {
 #pragma unroll
                 for (int h = 0; h < HELD; ++h)
 #pragma unroll
-                    for (int i = 0; i < EACH; ++i) of[h][i] += sums[(h * EACH + i) * (half * G) + mine * G + lane];
+                    for (int i = 0; i < EACH; ++i) of[h][i] += sums[(h * EACH + i) * (half * threads) + mine * threads + lane];
             }
         }
     };
-    if (GROUPS > 1) {
+    if (THREADS <= 512) {
         fold(dweight);
         fold(dbias);
     }
@@ -232,43 +261,62 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const Norm p, const 
     float* to = parts + (int64_t)blockIdx.x * 2 * p.width;
 #pragma unroll
     for (int h = 0; h < HELD; ++h) {
-        taser_store_as<float, EACH>(to, (int64_t)(h * G + lane) * EACH, p.width, dweight[h]);
-        taser_store_as<float, EACH>(to + p.width, (int64_t)(h * G + lane) * EACH, p.width, dbias[h]);
+        taser_store_as<float, EACH>(to, (int64_t)(h * threads + lane) * EACH, p.width, dweight[h]);
+        taser_store_as<float, EACH>(to + p.width, (int64_t)(h * threads + lane) * EACH, p.width, dbias[h]);
     }
 }
 
-template <typename T> __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(const Norm p, const T* x, const T* dout, const float* stats, T* dx) {
+// dx of longer rows: a block each. HELD pieces of either input stay in registers; what is past them is read twice.
+template <typename T, int HELD> __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const Norm p, const T* x, const T* dout, const float* stats, T* dx) {
     constexpr int EACH = kTaserEach<T>;
     __shared__ float2 shared[2][16];
-    const int64_t row = blockIdx.x, step = 1024 * EACH;
+    const int64_t row = blockIdx.x, step = blockDim.x * EACH, past = HELD * step + threadIdx.x * EACH;
+    const T *from = x + row * p.x_stride, *grads = dout + row * p.dout_stride;
+    TaserPiece<T> held_x[HELD], held_y[HELD], v, y;
+    load_row<T, HELD>(from, blockDim.x, threadIdx.x, p.width, held_x);
+    load_row<T, HELD>(grads, blockDim.x, threadIdx.x, p.width, held_y);
     const float mean = stats[2 * row], rstd = stats[2 * row + 1];
-    TaserPiece<T> v, y;
-    float g[EACH], a = 0.f, b = 0.f;
-    auto load = [&](int64_t c) {   // g is 0 past the row's end
-        taser_load_piece<T>(x + row * p.x_stride, c, p.width, (T)0.f, v);
-        taser_load_piece<T>(dout + row * p.dout_stride, c, p.width, (T)0.f, y);
+    float a = 0.f, b = 0.f;
+    auto times_weight = [&](int64_t c, const TaserPiece<T>& of, float (&g)[EACH]) {   // 0 past the row's end
 #pragma unroll
         for (int i = 0; i < EACH; ++i) g[i] = 1.f;
         if (p.weight) taser_load_floats<EACH>(p.weight, p.weight_type, c, p.width, g);
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) g[i] *= (float)y.x[i];
+        for (int i = 0; i < EACH; ++i) g[i] *= (float)of.x[i];
     };
-    for (int64_t c = threadIdx.x * EACH; c < p.width; c += step) {
-        load(c);
+    auto add = [&](int64_t c, const TaserPiece<T>& of_x, const TaserPiece<T>& of_y) {
+        float g[EACH];
+        times_weight(c, of_y, g);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             a += g[i];
-            if (c + i < p.width) b = fmaf(g[i], ((float)v.x[i] - mean) * rstd, b);
+            if (c + i < p.width) b = fmaf(g[i], ((float)of_x.x[i] - mean) * rstd, b);
         }
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) add(h * step + threadIdx.x * EACH, held_x[h], held_y[h]);
+    for (int64_t c = past; c < p.width; c += step) {
+        taser_load_piece<T>(from, c, p.width, (T)0.f, v);
+        taser_load_piece<T>(grads, c, p.width, (T)0.f, y);
+        add(c, v, y);
     }
-    group_sums<1024>(a, b, shared, 0);
+    group_sums<0>(a, b, shared, 0, blockDim.x >> 6);
     a /= (float)p.width;
     b /= (float)p.width;
-    for (int64_t c = threadIdx.x * EACH; c < p.width; c += step) {
-        load(c);
+    auto put = [&](int64_t c, const TaserPiece<T>& of_x, const TaserPiece<T>& of_y) {
+        float g[EACH];
+        TaserPiece<T> d;
+        times_weight(c, of_y, g);
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) v.x[i] = (T)(rstd * (g[i] - a - ((float)v.x[i] - mean) * rstd * b));
-        taser_store_piece<T>(dx + row * p.width, c, p.width, v);
+        for (int i = 0; i < EACH; ++i) d.x[i] = (T)(rstd * (g[i] - a - ((float)of_x.x[i] - mean) * rstd * b));
+        taser_store_piece<T>(dx + row * p.width, c, p.width, d);
+    };
+#pragma unroll
+    for (int h = 0; h < HELD; ++h) put(h * step + threadIdx.x * EACH, held_x[h], held_y[h]);
+    for (int64_t c = past; c < p.width; c += step) {
+        taser_load_piece<T>(from, c, p.width, (T)0.f, v);
+        taser_load_piece<T>(grads, c, p.width, (T)0.f, y);
+        put(c, v, y);
     }
 }
 
@@ -318,6 +366,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* parts, int
     const int64_t c = (int64_t)blockIdx.x * 32 + column;
     float sum = 0.f;
     if (c < 2 * width)
+#pragma unroll 8
         for (int64_t i = slice; i < n_parts; i += 32) sum += parts[i * 2 * width + c];
     sums[slice][column] = sum;
     __syncthreads();
@@ -333,87 +382,82 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float* parts, int
 
 // ---- on the host ---------------------------------------------------------------------------------
 
-// Threads to a row and pieces to a thread.
-struct Shape { int group, held; };
-Shape shape_of(int64_t width, int32_t type) {
-    const int each = type == TASER_F32 ? 4 : 8, most = kColumns / each;
+// How rows are cut: lanes of a group (0: whole waves), waves of a group, pieces of a thread, threads of a block.
+struct Shape { int lanes, waves, held, threads; };
+// Groups of a part of a wave with one piece a lane, or of as many waves as it takes with `columns` columns a thread; blocks of 256 threads or so for the
+// answer, 512 for the gradient, whose blocks' sums are fewer so.
+Shape shape_of(int64_t width, int32_t type, int columns, int threads) {
+    const int each = type == TASER_F32 ? 4 : 8, held = columns / each;
     const int64_t pieces = (width + each - 1) / each;
-    int group = 8;
-    while (group < 64 && group < pieces) group *= 2;
-    if (pieces <= group) return {group, 1};
-    while (group < 1024 && (int64_t)group * most < pieces) group *= 2;
-    return {group, most};
+    for (int lanes = 8; lanes <= 64; lanes *= 2)
+        if (pieces <= lanes) return {lanes, 1, 1, threads};
+    const int waves = (int)((pieces + 64 * held - 1) / (64 * held));
+    int groups = 1;
+    while (2 * groups * waves * 64 <= threads) groups *= 2;
+    return {0, waves, held, groups * waves * 64};
 }
-
-// Blocks that a call of so many rows has, groups of `group` threads in blocks of `threads`: two to four a compute unit.
-int64_t norm_blocks(int64_t rows, int group, int threads, int64_t most) {
-    const int64_t each = threads / group, blocks = (rows + each - 1) / each;
+Shape forward_shape(int64_t width, int32_t type) { return shape_of(width, type, 16, 256); }
+Shape grad_shape(int64_t width, int32_t type) { return shape_of(width, type, 8, 512); }
+int64_t groups_of(const Shape& s) { return s.threads / (s.lanes ? s.lanes : s.waves * 64); }
+int64_t blocks_of(int64_t rows, const Shape& s, int64_t most) {
+    const int64_t blocks = (rows + groups_of(s) - 1) / groups_of(s);
     return blocks < most ? blocks : most;
 }
-int grad_threads(int group) { return group <= 512 ? 512 : 1024; }
+// The gradient's: two of 512 threads a compute unit. More would read a little faster and leave more sums to join.
 int64_t grad_blocks(const Norm& p, int32_t type) {
-    const Shape s = shape_of(p.width, type);
-    const int threads = grad_threads(s.group);
-    return norm_blocks(p.rows, s.group, threads, threads == 512 ? 512 : 256);
+    const Shape s = grad_shape(p.width, type);
+    return blocks_of(p.rows, s, 256 * (s.threads > 512 ? 1 : 2));
 }
-// The wide kernels' slices of the rows.
+// Longer rows' slices for the sums by column.
 int64_t column_slices(const Norm& p) {
     const int64_t n = (p.rows + 15) / 16;
     return n < 64 ? n : 64;
 }
-
-template <typename T, int G, int HELD> void run_norm(const Norm& p, const T* x, T* out, float* stats, hipStream_t stream) {
-    constexpr int THREADS = G <= 256 ? 256 : G;
-    const int64_t blocks = norm_blocks(p.rows, G, THREADS, 256 * (1024 / THREADS));
-    norm_kernel<T, G, HELD, THREADS><<<(unsigned)blocks, THREADS, 0, stream>>>(p, x, out, stats);
-}
-template <typename T, int G, int HELD> void run_grad(const Norm& p, const T* x, const T* dout, const float* stats, T* dx, float* parts, int64_t blocks, hipStream_t stream) {
-    constexpr int THREADS = G <= 512 ? 512 : 1024;
-    norm_grad_kernel<T, G, HELD, THREADS><<<(unsigned)blocks, THREADS, 0, stream>>>(p, x, dout, stats, dx, parts);
-}
-
-// run(G, HELD) of the row's shape, as compile-time numbers.
-template <int G> struct Group { static constexpr int value = G; };
-template <int H> struct Held { static constexpr int value = H; };
-template <typename T, typename F> void with_shape(Shape s, F&& run) {
-    constexpr int MOST = kColumns / kTaserEach<T>;
-    if (s.held == 1) {
-        if (s.group == 8) run(Group<8>(), Held<1>());
-        else if (s.group == 16) run(Group<16>(), Held<1>());
-        else if (s.group == 32) run(Group<32>(), Held<1>());
-        else run(Group<64>(), Held<1>());
-    } else {
-        if (s.group == 64) run(Group<64>(), Held<MOST>());
-        else if (s.group == 128) run(Group<128>(), Held<MOST>());
-        else if (s.group == 256) run(Group<256>(), Held<MOST>());
-        else if (s.group == 512) run(Group<512>(), Held<MOST>());
-        else run(Group<1024>(), Held<MOST>());
-    }
+unsigned long_threads(int64_t width, int32_t type) {
+    const int64_t pieces = (width + 31) / 32, threads = (pieces + 63) / 64 * 64;   // 32 columns a thread
+    return (unsigned)(threads < 1024 ? threads : 1024);
 }
 
 template <typename T> int forward(const Norm& p, int32_t type, const void* x, void* out, float* stats, hipStream_t stream) {
+    constexpr int MANY = 16 / kTaserEach<T>;
     TaserProfileSpan span(stream, "layer_norm");
-    if (p.width > kHeld) norm_wide_kernel<T><<<(unsigned)p.rows, 1024, 0, stream>>>(p, (const T*)x, (T*)out, stats);
-    else with_shape<T>(shape_of(p.width, type), [&](auto g, auto h) { run_norm<T, decltype(g)::value, decltype(h)::value>(p, (const T*)x, (T*)out, stats, stream); });
+    if (p.width > kHeld) {
+        norm_long_kernel<T, 2 * MANY><<<(unsigned)p.rows, long_threads(p.width, type), 0, stream>>>(p, (const T*)x, (T*)out, stats);
+    } else {
+        const Shape s = forward_shape(p.width, type);
+        const unsigned blocks = (unsigned)blocks_of(p.rows, s, 256 * (1024 / s.threads));
+        auto run = [&](auto kernel) { kernel<<<blocks, s.threads, 0, stream>>>(p, s.waves, (const T*)x, (T*)out, stats); };
+        if (s.lanes == 8) run(norm_kernel<T, 8, 1, 256>);
+        else if (s.lanes == 16) run(norm_kernel<T, 16, 1, 256>);
+        else if (s.lanes == 32) run(norm_kernel<T, 32, 1, 256>);
+        else if (s.lanes == 64) run(norm_kernel<T, 64, 1, 256>);
+        else run(norm_kernel<T, 0, MANY, 512>);
+    }
     TASER_HIP_TRY(hipGetLastError());
     return TASER_OK;
 }
 
 template <typename T>
 int backward(const Norm& p, int32_t type, const void* x, const void* dout, const float* stats, void* dx, void* dweight, void* dbias, float* parts, hipStream_t stream) {
+    constexpr int EACH = kTaserEach<T>;
     int64_t n_parts;
     {
         TaserProfileSpan span(stream, "layer_norm_grad");
         if (p.width > kHeld) {
             n_parts = column_slices(p);
-            norm_grad_wide_kernel<T><<<(unsigned)p.rows, 1024, 0, stream>>>(p, (const T*)x, (const T*)dout, stats, (T*)dx);
-            const int64_t across = (p.width + 64 * kTaserEach<T> - 1) / (64 * kTaserEach<T>);
+            norm_grad_long_kernel<T, 32 / EACH><<<(unsigned)p.rows, long_threads(p.width, type), 0, stream>>>(p, (const T*)x, (const T*)dout, stats, (T*)dx);
+            const int64_t across = (p.width + 64 * EACH - 1) / (64 * EACH);
             if (parts) norm_columns_kernel<T><<<dim3((unsigned)across, (unsigned)n_parts), 256, 0, stream>>>(p, (const T*)x, (const T*)dout, stats, parts);
         } else {
+            const Shape s = grad_shape(p.width, type);
             n_parts = grad_blocks(p, type);
-            with_shape<T>(shape_of(p.width, type), [&](auto g, auto h) {
-                run_grad<T, decltype(g)::value, decltype(h)::value>(p, (const T*)x, (const T*)dout, stats, (T*)dx, parts, n_parts, stream);
-            });
+            auto run = [&](auto kernel) { kernel<<<(unsigned)n_parts, s.threads, 0, stream>>>(p, s.waves, (const T*)x, (const T*)dout, stats, (T*)dx, parts); };
+            if (s.lanes == 8) run(norm_grad_kernel<T, 8, 1, 512>);
+            else if (s.lanes == 16) run(norm_grad_kernel<T, 16, 1, 512>);
+            else if (s.lanes == 32) run(norm_grad_kernel<T, 32, 1, 512>);
+            else if (s.lanes == 64) run(norm_grad_kernel<T, 64, 1, 512>);
+            else if (s.threads <= 512) run(norm_grad_kernel<T, 0, 8 / EACH, 512>);
+            else run(norm_grad_kernel<T, 0, 8 / EACH, 1024>);
         }
         TASER_HIP_TRY(hipGetLastError());
     }
