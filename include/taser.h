@@ -701,7 +701,7 @@ int taser_layer_norm_grad(const taser_norm* n, const float* stats, const void* d
  *   betas in [0, 1), eps and weight_decay >= 0
  * Memory that is written (param, m, v and units) must overlap neither other
  * tensors' nor a gradient: such calls are refused. Any number of tensors, at most
- * 2^35 elements each; only launches kernels, one for every 56 tensors.
+ * 2^34 elements each; only launches kernels, one for every 56 tensors.
  *
  * taser_adamw_moments: 8-bit moments of one tensor as numbers of `type`, dense.
  * ------------------------------------------------------------------------- */

@@ -22,7 +22,7 @@
 namespace {
 
 constexpr int kTensors = 56;      // of a launch
-constexpr int kChunk = 4096;      // elements of a block
+constexpr int kChunk = 2048;      // elements of a block (100 M elements: 433 us; 457 with twice, 462 with four times as many, whose loads wait for stores)
 constexpr int kShared = TASER_ADAMW_BLOCK;
 constexpr uint32_t kTag = 0x4144414Du;
 
@@ -90,26 +90,25 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Launch a, const Factor
     const int64_t n = t.n, base = (int64_t)(blockIdx.x - t.first) * kChunk;
     const int p_type = t.types & 3, g_type = t.types >> 2;
     constexpr int AT_ONCE = 2;
-    for (int turn = 0; turn < kChunk / (1024 * AT_ONCE); ++turn) {
-        float p[AT_ONCE][4], g[AT_ONCE][4], m[AT_ONCE][4], v[AT_ONCE][4];
+    static_assert(AT_ONCE * 1024 == kChunk, "256 threads of 4 elements");
+    float p[AT_ONCE][4], g[AT_ONCE][4], m[AT_ONCE][4], v[AT_ONCE][4];
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            const int64_t at = base + (turn * AT_ONCE + j) * 1024 + threadIdx.x * 4;
-            taser_load_floats<4>(t.p, p_type, at, n, p[j]);
-            taser_load_floats<4>(t.g, g_type, at, n, g[j]);
-            taser_load_as<float, 4>(t.m, at, n, m[j]);
-            taser_load_as<float, 4>(t.v, at, n, v[j]);
-        }
+    for (int j = 0; j < AT_ONCE; ++j) {
+        const int64_t at = base + j * 1024 + threadIdx.x * 4;
+        taser_load_floats<4>(t.p, p_type, at, n, p[j]);
+        taser_load_floats<4>(t.g, g_type, at, n, g[j]);
+        taser_load_as<float, 4>(t.m, at, n, m[j]);
+        taser_load_as<float, 4>(t.v, at, n, v[j]);
+    }
 #pragma unroll
-        for (int j = 0; j < AT_ONCE; ++j) {
-            const int64_t at = base + (turn * AT_ONCE + j) * 1024 + threadIdx.x * 4;
-            float root;
+    for (int j = 0; j < AT_ONCE; ++j) {
+        const int64_t at = base + j * 1024 + threadIdx.x * 4;
+        float root;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) update(a.s, f, p[j][k], g[j][k], m[j][k], v[j][k], root);
-            taser_store_floats<4>(t.p, p_type, at, n, p[j]);
-            taser_store_as<float, 4>(t.m, at, n, m[j]);
-            taser_store_as<float, 4>(t.v, at, n, v[j]);
-        }
+        for (int k = 0; k < 4; ++k) update(a.s, f, p[j][k], g[j][k], m[j][k], v[j][k], root);
+        taser_store_floats<4>(t.p, p_type, at, n, p[j]);
+        taser_store_as<float, 4>(t.m, at, n, m[j]);
+        taser_store_as<float, 4>(t.v, at, n, v[j]);
     }
 }
 
@@ -177,59 +176,57 @@ __global__ __launch_bounds__(256) void adamw_bytes_kernel(const Launch a, const 
     const int64_t n = t.n, base = (int64_t)(blockIdx.x - t.first) * kChunk;
     const int p_type = t.types & 3, g_type = t.types >> 2, lane = threadIdx.x & 31;
     const uint32_t number = a.numbers[i];
-    for (int turn = 0; turn < kChunk / 2048; ++turn) {
-        const int64_t at = base + turn * 2048 + threadIdx.x * 8, block = at / kShared;
-        if (block * kShared >= n) return;   // a block's lanes leave together
-        float p[8], g[8];
-        uint8_t mc[8], vc[8];
-        taser_load_floats<8>(t.p, p_type, at, n, p);
-        taser_load_floats<8>(t.g, g_type, at, n, g);
-        load_codes((const uint8_t*)t.m, at, n, mc);
-        load_codes((const uint8_t*)t.v, at, n, vc);
-        const float m_unit = t.m_unit[block], v_unit = t.v_unit[block];
-        uint32_t c[4] = {(uint32_t)(at >> 3), number, (uint32_t)step, kTag}, k0 = a.s.seed_lo, k1 = a.s.seed_hi;
+    const int64_t at = base + threadIdx.x * 8, block = at / kShared;
+    if (block * kShared >= n) return;   // a block's lanes leave together
+    float p[8], g[8];
+    uint8_t mc[8], vc[8];
+    taser_load_floats<8>(t.p, p_type, at, n, p);
+    taser_load_floats<8>(t.g, g_type, at, n, g);
+    load_codes((const uint8_t*)t.m, at, n, mc);
+    load_codes((const uint8_t*)t.v, at, n, vc);
+    const float m_unit = t.m_unit[block], v_unit = t.v_unit[block];
+    uint32_t c[4] = {(uint32_t)(at >> 3), number, (uint32_t)step, kTag}, k0 = a.s.seed_lo, k1 = a.s.seed_hi;
 #pragma unroll
-        for (int r = 0; r < 10; ++r) {
-            philox_round<true>(c, k0, k1);
-            k0 += 0x9E3779B9u;
-            k1 += 0xBB67AE85u;
-        }
-        float m[8], root[8];
-        uint32_t m_most = 0, v_most = 0;
+    for (int r = 0; r < 10; ++r) {
+        philox_round<true>(c, k0, k1);
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    float m[8], root[8];
+    uint32_t m_most = 0, v_most = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            m[j] = m_of(mc[j], m_unit);
-            float v = v_of(vc[j], v_unit);
-            update(a.s, f, p[j], g[j], m[j], v, root[j]);
-            const bool real = at + j < n;
-            const uint32_t size = __float_as_uint(m[j]) & 0x7fffffffu, other = __float_as_uint(root[j]) & 0x7fffffffu;
-            m_most = real && size > m_most ? size : m_most;
-            v_most = real && other > v_most ? other : v_most;
-        }
-        taser_store_floats<8>(t.p, p_type, at, n, p);
+    for (int j = 0; j < 8; ++j) {
+        m[j] = m_of(mc[j], m_unit);
+        float v = v_of(vc[j], v_unit);
+        update(a.s, f, p[j], g[j], m[j], v, root[j]);
+        const bool real = at + j < n;
+        const uint32_t size = __float_as_uint(m[j]) & 0x7fffffffu, other = __float_as_uint(root[j]) & 0x7fffffffu;
+        m_most = real && size > m_most ? size : m_most;
+        v_most = real && other > v_most ? other : v_most;
+    }
+    taser_store_floats<8>(t.p, p_type, at, n, p);
 #pragma unroll
-        for (int s = 1; s < 32; s <<= 1) {
-            const uint32_t x = __shfl_xor(m_most, s), y = __shfl_xor(v_most, s);
-            m_most = x > m_most ? x : m_most;
-            v_most = y > v_most ? y : v_most;
-        }
-        const float m_next = unit_of(m_most, 1.f / (127.f * 127.f)), v_next = unit_of(v_most, 1.f / (255.f * 255.f));
-        // (A unit below 2^-126 has an inverse that may be infinite: moments that small count as 0.)
-        const float m_inverse = m_next >= 1.17549435e-38f ? 1.f / m_next : 0.f, v_inverse = v_next >= 1.17549435e-38f ? 1.f / v_next : 0.f;
+    for (int s = 1; s < 32; s <<= 1) {
+        const uint32_t x = __shfl_xor(m_most, s), y = __shfl_xor(v_most, s);
+        m_most = x > m_most ? x : m_most;
+        v_most = y > v_most ? y : v_most;
+    }
+    const float m_next = unit_of(m_most, 1.f / (127.f * 127.f)), v_next = unit_of(v_most, 1.f / (255.f * 255.f));
+    // (A unit below 2^-126 has an inverse that may be infinite: moments that small count as 0.)
+    const float m_inverse = m_next >= 1.17549435e-38f ? 1.f / m_next : 0.f, v_inverse = v_next >= 1.17549435e-38f ? 1.f / v_next : 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float chance = ((float)(c[j >> 1] >> (16 * (j & 1)) & 0xffffu) + 0.5f) * (1.f / 65536.f);
-            const uint32_t code = code_of<127, false>(fabsf(m[j]), m_inverse, chance);
-            mc[j] = (uint8_t)(code | (m[j] < 0.f && code ? 128u : 0u));
-            const uint32_t other = code_of<255, true>(root[j], v_inverse, chance);
-            vc[j] = (uint8_t)(root[j] > 0.f && !other ? 1u : other);
-        }
-        store_codes((uint8_t*)t.m, at, n, mc);
-        store_codes((uint8_t*)t.v, at, n, vc);
-        if (lane == 0) {
-            t.m_unit[block] = m_next;
-            t.v_unit[block] = v_next;
-        }
+    for (int j = 0; j < 8; ++j) {
+        const float chance = ((float)(c[j >> 1] >> (16 * (j & 1)) & 0xffffu) + 0.5f) * (1.f / 65536.f);
+        const uint32_t code = code_of<127, false>(fabsf(m[j]), m_inverse, chance);
+        mc[j] = (uint8_t)(code | (m[j] < 0.f && code ? 128u : 0u));
+        const uint32_t other = code_of<255, true>(root[j], v_inverse, chance);
+        vc[j] = (uint8_t)(root[j] > 0.f && !other ? 1u : other);
+    }
+    store_codes((uint8_t*)t.m, at, n, mc);
+    store_codes((uint8_t*)t.v, at, n, vc);
+    if (lane == 0) {
+        t.m_unit[block] = m_next;
+        t.v_unit[block] = v_next;
     }
 }
 
@@ -296,7 +293,7 @@ int check(const taser_adamw* a, const taser_adamw_tensor* tensors, int64_t n) {
         if (t.elements < 0) return taser_fail(TASER_E_ARG, "adamw_step: tensor %lld has a negative size", (long long)i);
         if (!t.elements || !t.grad) continue;
         if (t.type < TASER_F32 || t.type > TASER_BF16 || t.grad_type < TASER_F32 || t.grad_type > TASER_BF16) return taser_fail(TASER_E_ARG, "adamw_step: unknown element type of tensor %lld", (long long)i);
-        if (t.elements > (int64_t)1 << 35) return taser_fail(TASER_E_RANGE, "adamw_step: tensor %lld has more than 2^35 elements", (long long)i);
+        if (t.elements > (int64_t)1 << 34) return taser_fail(TASER_E_RANGE, "adamw_step: tensor %lld has more than 2^34 elements", (long long)i);
         if (!t.param || !t.m || !t.v || (a->bits == 8 && (!t.m_unit || !t.v_unit))) return taser_fail(TASER_E_ARG, "adamw_step: null memory of tensor %lld", (long long)i);
         const uint64_t size = t.type == TASER_F32 ? 4 : 2, g_size = t.grad_type == TASER_F32 ? 4 : 2, moment = a->bits == 8 ? 1 : 4, e = (uint64_t)t.elements;
         const uint64_t units = (e + kShared - 1) / kShared * sizeof(float);
