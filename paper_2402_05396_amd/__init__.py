@@ -1096,6 +1096,10 @@ def adamw_step(params, grads, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1
 def adamw_moments(m, v, units, dtype=torch.float32, stream=None):
     """taser_adamw_moments: one tensor's 8-bit moments (codes uint8, units a pair of float32[ceil(n / 256)]) as numbers -> (m, v) of `dtype`, shaped like
     the codes."""
+    if stream is None:
+        r = (_native or _bind()).adamw_moments(m, v, units, dtype)
+        if r is not None:
+            return r
     _want(m, torch.uint8, "m")
     m_unit, v_unit = units
     for name, t, like in (("v", v, torch.uint8), ("m's unit", m_unit, torch.float32), ("v's unit", v_unit, torch.float32)):

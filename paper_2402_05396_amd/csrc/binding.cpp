@@ -16,6 +16,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -46,6 +47,7 @@ struct Api {
     decltype(&taser_layer_norm_grad_bytes) layer_norm_grad_bytes;
     decltype(&taser_layer_norm_grad) layer_norm_grad;
     decltype(&taser_adamw_step) adamw_step;
+    decltype(&taser_adamw_moments) adamw_moments;
     decltype(&taser_last_error) last_error;
 } api;
 PyObject* error_class = nullptr;                                  // TaserError
@@ -836,6 +838,32 @@ PyObject* adamw_step(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
     END_HANDLE_TH_ERRORS
 }
 
+// (m, v, units, dtype), on torch's current stream
+PyObject* adamw_moments(PyObject*, PyObject* const* o, Py_ssize_t n_args) {
+    HANDLE_TH_ERRORS
+    void* stream;
+    if (n_args != 4 || !PyTuple_CheckExact(o[2]) || PyTuple_GET_SIZE(o[2]) != 2 || !THPDtype_Check(o[3]) || !get_stream(Py_None, &stream)) return not_plain();
+    const at::Tensor* m = device_array(o[0], at::kByte);
+    if (!m || !is_current(m)) return not_plain();
+    const at::Tensor *v = beside(device_array(o[1], at::kByte), *m), *m_unit = beside(device_array(PyTuple_GET_ITEM(o[2], 0), at::kFloat), *m),
+                     *v_unit = beside(device_array(PyTuple_GET_ITEM(o[2], 1), at::kFloat), *m);
+    const at::ScalarType dtype = reinterpret_cast<THPDtype*>(o[3])->scalar_type;
+    const int64_t n = m->numel(), units = (n + TASER_ADAMW_BLOCK - 1) / TASER_ADAMW_BLOCK;
+    int32_t type;
+    if (!v || !m_unit || !v_unit || v->sizes() != m->sizes() || m_unit->numel() != units || v_unit->numel() != units || !element_type(dtype, &type)) return not_plain();
+    const at::Tensor a = make(m->sizes(), dtype, m->device()), b = make(m->sizes(), dtype, m->device());
+    const void *p_m = m->data_ptr(), *p_v = v->data_ptr(), *p_mu = m_unit->data_ptr(), *p_vu = v_unit->data_ptr();
+    void *p_a = a.data_ptr(), *p_b = b.data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = api.adamw_moments(static_cast<const uint8_t*>(p_m), static_cast<const uint8_t*>(p_v), static_cast<const float*>(p_mu), static_cast<const float*>(p_vu), n, type, p_a, p_b, stream);
+    Py_END_ALLOW_THREADS
+    if (rc != TASER_OK) return raise(rc);
+    Ref x(THPVariable_Wrap(a)), y(THPVariable_Wrap(b));
+    return x.p && y.p ? PyTuple_Pack(2, x.p, y.p) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(TaserError, {entry point: address})
 template <typename F> bool entry(PyObject* addresses, const char* name, F* to) {
     PyObject* o = PyDict_GetItemString(addresses, name);
@@ -859,7 +887,7 @@ PyObject* bind(PyObject*, PyObject* args) {
         !entry(addresses, "taser_policy_loss", &to.policy_loss) || !entry(addresses, "taser_policy_draw_bytes", &to.policy_draw_bytes) ||
         !entry(addresses, "taser_policy_draw", &to.policy_draw) || !entry(addresses, "taser_layer_norm", &to.layer_norm) ||
         !entry(addresses, "taser_layer_norm_grad_bytes", &to.layer_norm_grad_bytes) || !entry(addresses, "taser_layer_norm_grad", &to.layer_norm_grad) ||
-        !entry(addresses, "taser_adamw_step", &to.adamw_step) || !entry(addresses, "taser_last_error", &to.last_error))
+        !entry(addresses, "taser_adamw_step", &to.adamw_step) || !entry(addresses, "taser_adamw_moments", &to.adamw_moments) || !entry(addresses, "taser_last_error", &to.last_error))
         return nullptr;
     api = to;
     Py_INCREF(cls);
@@ -871,7 +899,7 @@ PyObject* bind(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, FAST("sample", sample), FAST("gather", gather), FAST("encodings", encodings),
                          FAST("select", select), FAST("lookup", lookup), FAST("draw", draw), FAST("update", update), FAST("scores", scores),
                          FAST("attention", attention), FAST("attention_grad", attention_grad), FAST("bias", bias), FAST("bias_grad", bias_grad), FAST("policy", policy),
-                         FAST("policy_draw", policy_draw), FAST("layer_norm", layer_norm), FAST("layer_norm_grad", layer_norm_grad), FAST("adamw_step", adamw_step),
+                         FAST("policy_draw", policy_draw), FAST("layer_norm", layer_norm), FAST("layer_norm_grad", layer_norm_grad), FAST("adamw_step", adamw_step), FAST("adamw_moments", adamw_moments),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Native half of the Python binding, built for " TASER_BINDING_TAG ".", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -177,7 +177,7 @@ template <typename T, int G, int HELD, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const Norm p, int waves, const T* x, const T* dout, const float* stats, T* dx, float* parts) {
     constexpr int EACH = kTaserEach<T>, COLUMNS = HELD * EACH;
     __shared__ float2 shared[2][16];
-    __shared__ float sums[THREADS <= 512 ? THREADS / 2 * COLUMNS : 1];   // (a block of more is one group)
+    __shared__ float sums[THREADS <= 512 ? THREADS / 64 * 2 * COLUMNS * (G ? G : 64) : 1];   // (a block of more is one group)
     const int threads = G ? G : waves * 64, lane = threadIdx.x % threads, mine = threadIdx.x / threads, here = blockDim.x / threads;
     const int64_t groups = (int64_t)gridDim.x * here, turns = (p.rows + groups - 1) / groups;
     float weight[HELD][EACH], dweight[HELD][EACH] = {}, dbias[HELD][EACH] = {};
@@ -234,35 +234,43 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const Norm p, int wa
         if (turn + 1 < turns) take(Slot<1>(), turn + 1);
     }
     if (!parts) return;
-    // The upper half of the groups (a power of two of them) hands its sums to the lower half, until one has them all.
-    auto fold = [&](float (&of)[HELD][EACH]) {
-        for (int half = here / 2; half >= 1; half >>= 1) {
-            __syncthreads();
-            if (mine >= half && mine < 2 * half) {
-#pragma unroll
-                for (int h = 0; h < HELD; ++h)
-#pragma unroll
-                    for (int i = 0; i < EACH; ++i) sums[(h * EACH + i) * (half * threads) + (mine - half) * threads + lane] = of[h][i];
-            }
-            __syncthreads();
-            if (mine < half) {
-#pragma unroll
-                for (int h = 0; h < HELD; ++h)
-#pragma unroll
-                    for (int i = 0; i < EACH; ++i) of[h][i] += sums[(h * EACH + i) * (half * threads) + mine * threads + lane];
-            }
-        }
-    };
-    if (THREADS <= 512) {
-        fold(dweight);
-        fold(dbias);
-    }
-    if (mine) return;
     float* to = parts + (int64_t)blockIdx.x * 2 * p.width;
+    // Groups of a part of a wave add up across it, then what is left of them in LDS, in their order.
+    if (G)
 #pragma unroll
-    for (int h = 0; h < HELD; ++h) {
-        taser_store_as<float, EACH>(to, (int64_t)(h * threads + lane) * EACH, p.width, dweight[h]);
-        taser_store_as<float, EACH>(to + p.width, (int64_t)(h * threads + lane) * EACH, p.width, dbias[h]);
+        for (int m = G; m < 64; m <<= 1)
+#pragma unroll
+            for (int h = 0; h < HELD; ++h)
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) {
+                    dweight[h][i] += __shfl_xor(dweight[h][i], m);
+                    dbias[h][i] += __shfl_xor(dbias[h][i], m);
+                }
+    const int units = G ? THREADS / 64 : here, unit = G ? threadIdx.x >> 6 : mine;
+    if (units == 1) {
+#pragma unroll
+        for (int h = 0; h < HELD; ++h) {
+            taser_store_as<float, EACH>(to, (int64_t)(h * threads + lane) * EACH, p.width, dweight[h]);
+            taser_store_as<float, EACH>(to + p.width, (int64_t)(h * threads + lane) * EACH, p.width, dbias[h]);
+        }
+        return;
+    }
+    if (!G || (threadIdx.x & 63) < G) {
+#pragma unroll
+        for (int h = 0; h < HELD; ++h)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                sums[(unit * 2 * COLUMNS + h * EACH + i) * threads + lane] = dweight[h][i];
+                sums[(unit * 2 * COLUMNS + COLUMNS + h * EACH + i) * threads + lane] = dbias[h][i];
+            }
+    }
+    __syncthreads();
+    for (int at = threadIdx.x; at < 2 * COLUMNS * threads; at += blockDim.x) {
+        float sum = 0.f;
+        for (int u = 0; u < units; ++u) sum += sums[u * 2 * COLUMNS * threads + at];
+        const int k = at / threads, which = k / COLUMNS, of = k % COLUMNS;
+        const int64_t column = (int64_t)(of / EACH * threads + at % threads) * EACH + of % EACH;
+        if (column < p.width) to[which * p.width + column] = sum;
     }
 }
 
