@@ -7,7 +7,9 @@ The graph and its task are synthetic: one edge in five says something about its 
 edge's row which ones do. A uniform choice therefore keeps a fifth of such edges where a root has many candidates; the share kept
 is printed beside the loss.
 
-    python -m paper_2402_05396_amd.adaptive_training [--steps 60] [--roots 4096] [--type bfloat16]
+    python -m paper_2402_05396_amd.adaptive_training [--steps 60] [--roots 4096] [--type bfloat16] [--norm] [--bits 8]
+
+--norm: layer norm between the aggregation and the answer. --bits 8: the optimizers' moments in 8 bits.
 """
 import argparse
 import json
@@ -49,6 +51,39 @@ class PolicyLoss(torch.autograd.Function):
         return ctx.saved_tensors[0] * dloss, None, None, None, None
 
 
+class LayerNorm(torch.autograd.Function):
+    """layer_norm with its gradient. (A gradient of the gradient is an error.)"""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        out, stats = T.layer_norm(x, weight, bias, eps=eps, want_stats=True)
+        ctx.save_for_backward(x, stats, weight, bias)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        x, stats, weight, bias = ctx.saved_tensors
+        return (*T.layer_norm_grad(dout.contiguous(), x, stats, weight, bias), None)
+
+
+class Adam:
+    """adamw_step over a list of leaves: what their gradients say, moments in 32 or 8 bits, without decay unless asked for."""
+
+    def __init__(self, params, lr, weight_decay=0.0, bits=32):
+        self.params, self.lr, self.weight_decay, self.steps = list(params), lr, weight_decay, 0
+        self.m, self.v, self.units = T.adamw_state(self.params, bits)
+
+    def zero_grad(self):
+        for p in self.params:
+            p.grad = None
+
+    def step(self):
+        self.steps += 1
+        grads = [None if p.grad is None else p.grad.contiguous() for p in self.params]
+        T.adamw_step(self.params, grads, self.m, self.v, self.steps, lr=self.lr, weight_decay=self.weight_decay, units=self.units)
+
+
 def synthetic(nodes, edges, dim, seed, device):
     """A graph with time-sorted edges, their rows (element 0: whether the edge says something, 1: what), and per edge the same."""
     rng = torch.Generator().manual_seed(seed)
@@ -67,7 +102,8 @@ def synthetic(nodes, edges, dim, seed, device):
 class Trainer:
     """Both models of the example and what they train on."""
 
-    def __init__(self, roots=4096, candidates=25, picks=10, heads=2, head_dim=32, dim=32, nodes=2000, edges=100_000, dtype=torch.bfloat16, seed=0):
+    def __init__(self, roots=4096, candidates=25, picks=10, heads=2, head_dim=32, dim=32, nodes=2000, edges=100_000, dtype=torch.bfloat16, seed=0,
+                 norm=False, bits=32):
         device = torch.device("cuda")
         self.graph, self.table, self.end = synthetic(nodes, edges, dim, seed, device)
         self.roots, self.candidates, self.picks, self.heads, self.head_dim, self.nodes = roots, candidates, picks, heads, head_dim, nodes
@@ -82,8 +118,10 @@ class Trainer:
         # Powers of two apart: recent interactions are told apart finely, old ones coarsely.
         self.bounds = 2 ** torch.arange(12, 12 + 15, device=device, dtype=torch.int64)
         self.bias = torch.zeros((heads, 16), device=device, requires_grad=True)
-        self.model = torch.optim.Adam([self.query, self.key, self.value, self.answer, self.bias], lr=0.02)
-        self.sampler = torch.optim.Adam([self.score], lr=0.1)
+        learned = [self.query, self.key, self.value, self.answer, self.bias]
+        self.norm = [torch.ones(width, device=device, requires_grad=True), torch.zeros(width, device=device, requires_grad=True)] if norm else None
+        self.model = Adam(learned + (self.norm or []), lr=0.02, bits=bits)
+        self.sampler = Adam([self.score], lr=0.1, bits=bits)
 
     def aggregate(self, rows, times, kept):
         """[R, width]: what each root's kept neighbors' rows come to."""
@@ -91,7 +129,8 @@ class Trainer:
         q = self.query.to(self.dtype).view(1, 1, self.heads, -1).expand(r, 1, self.heads, self.head_dim)
         k, v = ((rows @ w).to(self.dtype).view(r, n, self.heads, self.head_dim) for w in (self.key, self.value))
         out = CrossAttention.apply(q, k, v, self.bias.to(self.dtype), self.bounds, times.view(r, 1), kept["ts"], kept["count"])
-        return out.reshape(r, -1).float()
+        out = out.reshape(r, -1)
+        return (out if self.norm is None else LayerNorm.apply(out, *self.norm, 1e-5)).float()
 
     def step(self, number):
         """One step of both models -> {loss, share of the kept neighbors that say something}."""
@@ -135,8 +174,10 @@ def main(argv=None):
     ap.add_argument("--roots", type=int, default=4096)
     ap.add_argument("--type", choices=["float32", "float16", "bfloat16"], default="bfloat16")
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--norm", action="store_true")
+    ap.add_argument("--bits", type=int, choices=[8, 32], default=32)
     args = ap.parse_args(argv)
-    trainer = Trainer(roots=args.roots, dtype=getattr(torch, args.type), seed=args.seed)
+    trainer = Trainer(roots=args.roots, dtype=getattr(torch, args.type), seed=args.seed, norm=args.norm, bits=args.bits)
     steps = [trainer.step(i) for i in range(args.steps)]
     for i in range(0, args.steps, max(1, args.steps // 10)):
         print("step %d: loss %.4f, kept %.3f" % (i, steps[i]["loss"], steps[i]["share"]), flush=True)
