@@ -218,17 +218,21 @@ def policy_draw(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
         rounded = (w != 0) & (w != 1)   # the others, and their sums, are exact on either side
         slack = lambda s: min(s, w[rounded].sum()) * 2.0 ** -41 + rounded.sum() * 2.0 ** -43
         clear = lambda margin, s: margin > slack(s) or slack(s) == 0
+        k = min(int(top_k[r]), c) if top_k[r] > 0 else c
+        best, there = order[:k], w[order[:k]]
+        before, whole = np.cumsum(there) - there, there.sum()
         keep, certain = np.zeros(c, bool), True
-        k = int(top_k[r]) if top_k[r] > 0 else c
-        before, whole = 0.0, w[order[:k]].sum()
-        for i, at in enumerate(order[:k]):
-            if i and top_p[r] < 1 and before >= top_p[r] * whole:
-                certain = certain and clear(before - top_p[r] * whole, whole)
-                break
-            certain = certain and (i == 0 or top_p[r] >= 1 or clear(top_p[r] * whole - before, whole))
-            certain = certain and (i == 0 or min_p[r] <= 0 or w[at] == 1 or clear(abs(w[at] - min_p[r]), 1.0))
-            keep[at] = i == 0 or w[at] >= min_p[r]
-            before += w[at]
+        stays = np.ones(k, bool)
+        if top_p[r] < 1:
+            stays = before < top_p[r] * whole
+            margin = np.abs(before - top_p[r] * whole)[1:]
+            certain = len(margin) == 0 or clear(margin.min(), whole)
+        if min_p[r] > 0:
+            margin = np.abs(there - min_p[r])[1:][there[1:] != 1]
+            certain = certain and (len(margin) == 0 or clear(margin.min(), 1.0))
+            stays &= there >= min_p[r]
+        stays[0] = True
+        keep[best] = stays
         running = np.cumsum(np.where(keep, w, 0.0))
         last = np.nonzero(np.where(keep, w, 0.0) > 2.0 ** -45)[0][-1]
         s = np.exp(x - top).sum()

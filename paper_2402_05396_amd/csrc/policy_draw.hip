@@ -183,7 +183,7 @@ template <typename T> struct Row {
 
     __device__ Row(const Draws& p, const T* logits, int64_t row, const Rule& rule, const double* powers)
         : from(logits + row * p.stride), n(taking_part(p, row)), top(0.f), scale(wants_number(rule, n) ? 32.f : by_weight(rule)), beta(rule.beta * 256.), powers(powers) {}
-    __device__ static float by_weight(const Rule& rule) { return (float)(rule.beta * 32.); }
+    __device__ static float by_weight(const Rule& rule) { return (float)fmin(rule.beta * 32., 1e30); }   // finite: the largest logit's distance is 0 at any temperature
     __device__ static void fill(double* powers) {
         for (int i = threadIdx.x; i < 256; i += blockDim.x) powers[i] = exp2(kBits - i / 256.);
     }

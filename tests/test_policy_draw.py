@@ -129,6 +129,42 @@ def test_logits_that_are_not_finite(kind):
 
 
 @gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows", [4, 300])
+def test_masks_of_the_types_lowest_value(kind, rows):
+    """Candidates that a mask of the lowest finite number rules out: their distance passes the floats. They are kept where there are too few others, and
+    never drawn, at any temperature there is."""
+    low = torch.finfo(KINDS[kind]).min
+    for W in (20, 300, 9000):
+        for settings in (dict(top_k=12), dict(top_k=12, top_p=0.99), dict(top_p=0.99), dict(temperature=1e-40, top_p=0.9), dict(temperature=1e-44, top_k=12), dict(temperature=1e30, top_k=3), {}):
+            c = _case(kind, rows, W, 3, seed=W, **settings)
+            c["logits"][:, 5:] = low
+            c["logits"][1, :5] = low
+            c["logits"][2, 3] = -low
+            if rows > 100 and W > 300:
+                c = dict(c, logits=c["logits"][:, :1500].contiguous())
+            _check(c, share=0.9)
+
+
+@gpu
+@pytest.mark.parametrize("rows", [1, 257])
+def test_the_widest_rows(rows):
+    """2^20 candidates, in single precision: the most there may be, cut and by one block."""
+    W = T.MAX_DRAW_WIDTH
+    g = torch.Generator("cuda").manual_seed(0)
+    x, u = torch.randn((rows, W), generator=g, device="cuda"), torch.rand((rows, 2), generator=g, device="cuda")
+    x[:, -1] += 3.0
+    for settings in (dict(top_p=0.7), dict(top_k=50, top_p=0.9), dict(top_k=3000), dict(min_p=0.1), dict(temperature=0.0)):
+        actions, logp = (t.cpu() for t in T.policy_draw(x, u, **settings))
+        i = rows - 1
+        given = {n: np.float32(v) for n, v in settings.items()}
+        want, l, off, sure = O.policy_draw(x[i:].double().cpu().numpy(), u[i:].double().cpu().numpy(), **given)
+        assert ((actions[i:].numpy() == want) | ~sure).all() and (np.abs(logp[i:].numpy() - l) <= off)[actions[i:].numpy() == want].all(), settings
+    with pytest.raises(T.TaserError):
+        T.policy_draw(torch.zeros((1, W + 1), device="cuda"), u[:1])
+
+
+@gpu
 def test_zeros_of_both_signs_are_one_value():
     for W in (40, 3000):
         x = torch.full((2, W), -5.0)
