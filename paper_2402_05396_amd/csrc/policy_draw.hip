@@ -87,6 +87,17 @@ template <int G> __device__ inline uint64_t running(uint64_t x) {
     if (G == 64) x += moved<0x143, 0xc>(x);   // the lower half's last
     return x;
 }
+// The largest of a wave's, in the last lane.
+__device__ inline uint32_t largest(uint32_t x) {
+    auto with = [&](uint32_t y) { x = y > x ? y : x; };
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, true));
+    with(__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, true));
+    return x;
+}
 template <int G> __device__ inline uint64_t sum_of(uint64_t x) { return shuffle(running<G>(x), G - 1, G); }
 
 // Rows of at most 64 candidates and draws: G lanes a row.
@@ -179,13 +190,13 @@ template <typename T> struct Row {
     int n;
     float top, scale;       // scale: bins of a distance of 1, 32 for candidates by number, 32 to a power of two of weight for weights
     double beta;            // 256 times the rule's
-    const double* powers;   // in LDS: 2^(kBits - i / 256)
+    const double* powers;   // in LDS: 2^(kBits + i / 256)
 
     __device__ Row(const Draws& p, const T* logits, int64_t row, const Rule& rule, const double* powers)
         : from(logits + row * p.stride), n(taking_part(p, row)), top(0.f), scale(wants_number(rule, n) ? 32.f : by_weight(rule)), beta(rule.beta * 256.), powers(powers) {}
     __device__ static float by_weight(const Rule& rule) { return (float)fmin(rule.beta * 32., 1e30); }   // finite: the largest logit's distance is 0 at any temperature
     __device__ static void fill(double* powers) {
-        for (int i = threadIdx.x; i < 256; i += blockDim.x) powers[i] = exp2(kBits - i / 256.);
+        for (int i = threadIdx.x; i < 256; i += blockDim.x) powers[i] = exp2(kBits + i / 256.);
     }
     __device__ void load(int64_t c, float (&v)[EACH]) const {
         TaserPiece<T> x;
@@ -195,13 +206,13 @@ template <typename T> struct Row {
     }
     // In bins; past the floats, or NaN (minus infinity at a temperature of infinity): the last. It falls as logits rise, roundings included.
     __device__ float distance(float x) const { return fminf((top - x) * scale, (float)(kBins - 1)); }
-    // 2^-y by a table of 256 powers and a series for the rest, |rest| <= 2^-9: 2^-42 off. (The whole part of 256 y is read off a sum with 1.5 2^52.)
+    // 2^y, y <= 0, by a table of 256 powers and a series for the rest, |rest| <= 2^-9: 2^-42 off. (The whole part of 256 y is read off a sum with 1.5 2^52.)
     __device__ uint64_t weight(float x) const {
-        const double y = fmin(((double)top - (double)x) * beta, 60. * 256.), up = y + 6755399441055744., r = y - (up - 6755399441055744.);
-        constexpr double c = -0.6931471805599453 / 256.;
-        const uint32_t j = (uint32_t)__double_as_longlong(up);
+        const double y = fmax(((double)x - (double)top) * beta, -60. * 256.), up = y + 6755399441055744., r = y - (up - 6755399441055744.);
+        constexpr double c = 0.6931471805599453 / 256.;
+        const int j = (int)__double2loint(up);
         const double e = powers[j & 255] * fma(fma(fma(r, c * c * c / 6., c * c / 2.), r, c), r, 1.);
-        const double w = __hiloint2double(__double2hiint(e) - (int)((j >> 8) << 20), __double2loint(e));   // by up to 2^60: no exponent runs out
+        const double w = __hiloint2double(__double2hiint(e) + ((j >> 8) << 20), __double2loint(e));   // by 2^-60 at least: no exponent runs out
         const double whole = w + 4503599627370496.;   // 2^52 more: rounded to a whole number
         return (uint64_t)(uint32_t)(__double2hiint(whole) - 0x43300000) << 32 | (uint32_t)__double2loint(whole);
     }
@@ -276,14 +287,18 @@ struct Found {
     uint64_t before, wanted, all;
     uint32_t bin, upto;
 };
-// The first bin at which the bins' sum comes to target(sum of all), what comes before it and, in 32 bits, what with it (a target of 0, or past the sum: none). By wave 0.
-template <typename F> __device__ inline void find_bin(const uint64_t* bins, Found* found, F&& target) {
+// The first bin at which the bins' sum comes to target(sum of all), what comes before it and, in 32 bits, what with it (a target of 0, or past the sum: none). By
+// wave 0, which leaves the bins empty.
+template <typename F> __device__ inline void find_bin(uint64_t* bins, Found* found, F&& target) {
     __syncthreads();
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
         uint64_t mine[kBins / 64], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kBins / 64; ++i) sum += mine[i] = bins[bin_at(lane * (kBins / 64) + i)];
+        for (int i = 0; i < kBins / 64; ++i) {
+            sum += mine[i] = bins[bin_at(lane * (kBins / 64) + i)];
+            bins[bin_at(lane * (kBins / 64) + i)] = 0;
+        }
         const uint64_t upto = running<64>(sum), all = shuffle(upto, 63), asked = target(all), wanted = asked <= all ? asked : 0;
         const uint64_t hit = __ballot(upto >= wanted);
         if (lane == 0) {
@@ -512,7 +527,7 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
     __shared__ double powers[256];
     __shared__ Found found;
     __shared__ float tops[WAVES], totals[WAVES];
-    __shared__ uint32_t bads[WAVES], lowest, highest, listed, few_rank[kFew];
+    __shared__ uint32_t bads[WAVES], lowest[3], highest[3], first_at, listed, few_rank[kFew];
     __shared__ uint64_t few_weight[kFew], few_sum[kFew], few_all;
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -540,9 +555,10 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
     for (int i = threadIdx.x; i < pieces; i += THREADS) running_sums[i] = 0;
     if (threadIdx.x == 0) {
         listed = 0;
-        lowest = 0xffffffffu;
-        highest = 0;
+        lowest[0] = first_at = 0xffffffffu;
+        highest[0] = 0;
     }
+    int slot = 0;
     if (CUT) {
         r.top = RowWork(s, row).top(s.slices);
         __syncthreads();
@@ -593,10 +609,10 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
                 for (int i = EACH - 1; i >= 0; --i) first = v[i] == r.top && (uint32_t)(c + i) < first ? (uint32_t)(c + i) : first;
                 total += r.soft(r.top, v);
             });
-            if (first != 0xffffffffu) atomicMin(&lowest, first);
+            if (first != 0xffffffffu) atomicMin(&first_at, first);
             join_total();
             __syncthreads();
-            first = lowest;
+            first = first_at;
             total = 0.f;
             for (int w = 0; w < WAVES; ++w) total += totals[w];
         }
@@ -611,12 +627,13 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
     // comes before it. Keys' bits, ten at a time, until there is one key left. known: the target does not go by the sum.
     auto select = [&](bool known, auto&& visit, auto&& key, auto&& amount, auto&& target, uint32_t& at, uint64_t& before, uint64_t& wanted) {
         uint32_t low = 0, high = 0xffffffffu;
-        auto narrow = [&]() {   // to the smallest and largest there are
+        // To the smallest and largest there are. Of three slots one is in use, one may still be read and one is made ready: one barrier is enough.
+        auto narrow = [&]() {
+            const int now = slot, next = slot == 2 ? 0 : slot + 1;
             if (threadIdx.x == 0) {
-                lowest = 0xffffffffu;
-                highest = 0;
+                lowest[next] = 0xffffffffu;
+                highest[next] = 0;
             }
-            __syncthreads();
             uint32_t a = 0xffffffffu, b = 0;
             visit([&](float x, uint32_t c) {
                 const uint32_t k = key(x, c);
@@ -626,21 +643,17 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
                 }
             });
             if (__ballot(b != 0)) {
-#pragma unroll
-                for (int m = 1; m < 64; m <<= 1) {
-                    const uint32_t x = __shfl_xor(a, m), y = __shfl_xor(b, m);
-                    a = x < a ? x : a;
-                    b = y > b ? y : b;
-                }
-                if (lane == 0) {
-                    atomicMin(&lowest, a);
-                    atomicMax(&highest, b);
+                a = ~largest(~a);
+                b = largest(b);
+                if (lane == 63) {
+                    atomicMin(&lowest[now], a);
+                    atomicMax(&highest[now], b);
                 }
             }
             __syncthreads();
-            low = lowest;
-            high = highest;
-            __syncthreads();
+            low = lowest[now];
+            high = highest[now];
+            slot = next;
         };
         narrow();
         before = wanted = at = 0;
@@ -653,8 +666,6 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
             const uint32_t range = high - low;
             const int shift = range >= kBins ? 22 - __clz(range) : 0;
             if (!first && !range) break;
-            for (int i = threadIdx.x; i < kGapped; i += THREADS) bins[i] = 0;
-            __syncthreads();
             visit([&](float x, uint32_t c) {
                 const uint32_t k = key(x, c);
                 if (k && k >= low && k <= high) atomicAdd((unsigned long long*)&bins[bin_at((int)((high - k) >> shift))], (unsigned long long)amount(x));
@@ -715,12 +726,7 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
         }
     }
     if (again || (!CUT && !by_number && rule.top_p)) {
-        if (again) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < kGapped; i += THREADS) bins[i] = 0;
-            __syncthreads();
-            r.scale = r.by_weight(rule);
-        }
+        if (again) r.scale = r.by_weight(rule);
         each([&](int, int, const float (&v)[EACH]) {
             r.count_in(bins, v, weight);
             if (softly) total += r.soft(r.top, v);
@@ -851,7 +857,7 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
         const uint64_t kept = keep && w >= rule.least ? w : 0;
         __syncthreads();   // all have read
         if (real) few_weight[threadIdx.x] = kept;
-        if (threadIdx.x == 0) highest = 0;
+        if (threadIdx.x == 0) first_at = 0;
         if (o.all) {   // and draws from these: each one's sum of those up to it
             if (real) few_sum[threadIdx.x] = 0;
             __syncthreads();
@@ -878,12 +884,10 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
             return;
         }
         __syncthreads();
-        if (keep) atomicMax(&highest, rank + 1);   // the last one kept is the limit
+        if (keep) atomicMax(&first_at, rank + 1);   // the last one kept is the limit
         if (kept) atomicAdd((unsigned long long*)&running_sums[(uint32_t)list[threadIdx.x] / (64 * EACH)], (unsigned long long)kept);
         __syncthreads();
-        if (keep && rank + 1 == highest) {
-            found.before = list[threadIdx.x];
-        }
+        if (keep && rank + 1 == first_at) found.before = list[threadIdx.x];
         __syncthreads();
         limit = logit(found.before);
         cut = (uint32_t)found.before;
