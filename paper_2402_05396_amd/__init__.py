@@ -1046,7 +1046,7 @@ def adamw_step(params, grads, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1
     any of the three types, or None for a tensor that is to be left as it is; m, v, units as adamw_state made them (8 bits where units are
     given). Tensors are contiguous. step: this one's number, from 1, or an int64 tensor that holds it; lr: a number or a float32 tensor;
     grad_scale: a float32 tensor that gradients are multiplied by (where it is NaN nothing changes); seed: of the roundings to 8 bits.
-    For groups of parameters with rates of their own, one call each."""
+    For groups of parameters with rates of their own, one call each. Autograd does not see that the parameters change."""
     params, grads, m, v = (x if isinstance(x, list) else list(x) for x in (params, grads, m, v))
     if stream is None:
         r = (_native or _bind()).adamw_step(params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, units, grad_scale, seed)

@@ -76,6 +76,14 @@ def test_many_rows(kind, shape):
 
 
 @gpu
+def test_weight_or_bias_alone():
+    for W in (60, 3000, 20_000):
+        for weight, bias in ((True, False), (False, True), (False, False)):
+            for kept in ("bfloat16", "float32"):
+                _check(_case("bfloat16", 21, W, kept=kept, weight=weight, bias=bias, seed=W))
+
+
+@gpu
 @pytest.mark.parametrize("W", [50, 1000, 30_000])
 def test_rows_far_from_zero(W):
     """What is away from the mean keeps its digits: a difference of sums of squares would have none left."""

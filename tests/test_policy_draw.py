@@ -83,6 +83,20 @@ def test_flat_and_steep_rows(kind):
 
 
 @gpu
+@pytest.mark.parametrize("kind,W", [(k, 9001) for k in KINDS] + [("bfloat16", 33_001), ("float32", 20_000)])
+def test_many_long_rows(kind, W):
+    """Rows of a block each, as there are enough of them: the same settings, ties and empty places as above."""
+    R = 270
+    for i, settings in enumerate((_rows(R, W), dict(top_p=0.9), dict(temperature=0.7, top_k=5000, top_p=0.8), {})):
+        c = _case(kind, R, W, 2, seed=W + i, count=i != 1, **settings)
+        c["logits"][:20] = (c["logits"][:20].float() * 0.5).round().to(KINDS[kind])   # ties by the thousand
+        c["logits"][20:30] = -0.25
+        c["logits"][30:40, ::2] = -float("inf")
+        c["logits"][40:50, 7] = 50.0
+        _check(c, share=0.9)
+
+
+@gpu
 @pytest.mark.parametrize("kind", KINDS)
 def test_the_smallest_and_largest_numbers(kind):
     for W in (30, 500, 9000):
