@@ -59,13 +59,14 @@ __host__ __device__ inline Factors factors_of(const Step& s, double lr, int64_t 
     return {(float)(1. - lr * s.decay), (float)(lr / c1), (float)(1. / sqrt(c2)), 1.f};
 }
 
-// One element. Without contraction: moments are the same bits as from separate products and sums.
-__device__ inline void update(const Step& s, const Factors& f, float& p, float g, float& m, float& v, float& root) {
+// One element. Without contraction: moments are the same bits as from separate products and sums. EXACT: the root is rounded correctly; else it is off by
+// one in its last place, and 0 for a v below 2^-126 (ten vector instructions an element less, which is what 8-bit moments wait for).
+template <bool EXACT> __device__ inline void update(const Step& s, const Factors& f, float& p, float g, float& m, float& v, float& root) {
 #pragma clang fp contract(off)
     g = g * f.scale;
     m = m * s.b1 + g * s.b1_rest;
     v = v * s.b2 + (g * g) * s.b2_rest;
-    root = sqrtf(v);
+    root = EXACT ? sqrtf(v) : __builtin_amdgcn_sqrtf(v);
     p = p * f.keep - (m * f.rate) * __builtin_amdgcn_rcpf(root * f.root + s.eps);
 }
 
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Launch a, const Factor
         const int64_t at = base + j * 1024 + threadIdx.x * 4;
         float root;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) update(a.s, f, p[j][k], g[j][k], m[j][k], v[j][k], root);
+        for (int k = 0; k < 4; ++k) update<true>(a.s, f, p[j][k], g[j][k], m[j][k], v[j][k], root);
         taser_store_floats<4>(t.p, p_type, at, n, p[j]);
         taser_store_as<float, 4>(t.m, at, n, m[j]);
         taser_store_as<float, 4>(t.v, at, n, v[j]);
@@ -129,14 +130,14 @@ __device__ inline float unit_of(uint32_t most, float share) {
 template <int MOST, bool QUAD> __device__ inline uint32_t code_of(float value, float inverse, float chance) {
 #pragma clang fp contract(off)
     float y = value * inverse;
-    const float c = fminf(floorf(__builtin_amdgcn_sqrtf(y)), (float)(MOST - 1)), d = c + 1.f;
-    float low = c * c, high = d * d;
+    const float c = fminf(floorf(__builtin_amdgcn_sqrtf(y)), (float)(MOST - 1));
+    float low = c * c, apart = c + c + 1.f;   // to (c + 1)^2
     if (QUAD) {
         y = y * y;
+        apart = apart * (low + low + (c + c) + 1.f);
         low = low * low;
-        high = high * high;
     }
-    return (uint32_t)c + (y - low > chance * (high - low) ? 1u : 0u);
+    return (uint32_t)c + (y - low > chance * apart ? 1u : 0u);
 }
 
 __device__ inline void load_codes(const uint8_t* from, int64_t at, int64_t n, uint8_t (&to)[8]) {
@@ -198,11 +199,10 @@ __global__ __launch_bounds__(256) void adamw_bytes_kernel(const Launch a, const 
     for (int j = 0; j < 8; ++j) {
         m[j] = m_of(mc[j], m_unit);
         float v = v_of(vc[j], v_unit);
-        update(a.s, f, p[j], g[j], m[j], v, root[j]);
-        const bool real = at + j < n;
-        const uint32_t size = __float_as_uint(m[j]) & 0x7fffffffu, other = __float_as_uint(root[j]) & 0x7fffffffu;
-        m_most = real && size > m_most ? size : m_most;
-        v_most = real && other > v_most ? other : v_most;
+        update<false>(a.s, f, p[j], g[j], m[j], v, root[j]);   // (places past the tensor's end hold zeros)
+        const uint32_t size = __float_as_uint(m[j]) & 0x7fffffffu, other = __float_as_uint(root[j]);   // NaN is the largest, of either sign
+        m_most = size > m_most ? size : m_most;
+        v_most = other > v_most ? other : v_most;
     }
     taser_store_floats<8>(t.p, p_type, at, n, p);
 #pragma unroll
