@@ -1,11 +1,14 @@
 // The AdamW step over a list of tensors (taser_adamw_step) and 8-bit moments as numbers (taser_adamw_moments).
 //
 //   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  p = p (1 - lr decay) - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps)
-// with c = 1 - beta^step, everything in 32 bits. Bound by memory: moments in 32 bits are 16 of the 28 bytes that an element of a
-// single-precision parameter moves, in 8 bits 4.1 of 16.
+// with c = 1 - beta^step, everything in 32 bits.
+//
+// Moments in 32 bits: bound by memory, 16 bytes of them of the 22 to 28 that an element moves (100 M elements in bfloat16: 433 us, 5.1 TB/s). In 8
+// bits: 4.1 of 14 to 16, and some hundred vector instructions, which take as long (118 M elements, parameters in single precision, gradients in
+// bfloat16: 1.66 GB in 330 us, 5 TB/s).
 //
 // A launch takes up to kTensors tensors, their addresses among its arguments (nothing is copied to the device, so a captured call replays
-// as it is); a block finds its tensor by one comparison a lane.
+// as it is); a block finds its tensor by one comparison a lane. 48 tensors of 0.48 M elements in all: 6 us, and 8 for the host's call.
 //
 // Moments in 8 bits share a unit among 256 neighbors of a tensor: m = sign c^2 unit (7 bits of c), sqrt(v) = c^2 unit. Steps
 // between codes are 2 / c (m) and 4 / c (v) of a value, 1.6 % for the block's largest, over a range of 4.2 (m) and 9.6 (v) decades. Rounded to the

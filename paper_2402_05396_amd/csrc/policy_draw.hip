@@ -8,7 +8,7 @@
 //
 // Rows of up to 64 candidates and draws: a part of a wave, a lane a candidate, whose rank comes from a look at every other one.
 // Longer rows: a block of 512 threads, three of them a compute unit; few of them: slices, four launches. Bound by the vector units: weights take some 20
-// instructions a candidate, twice where top-p looks for its threshold. 4096 x 64 001 bf16: top-p 0.95 630 us, top-k 50 with top-p 313, neither 292 (the
+// instructions a candidate, twice where top-p looks for its threshold. 4096 x 64 001 bf16: top-p 0.95 570 us, top-k 50 with top-p 313, neither 292 (the
 // logits alone 102); 1 x 64 001 with both 20, 64 x 130 000 f32 with top-p 58.
 #include "pieces.h"
 
