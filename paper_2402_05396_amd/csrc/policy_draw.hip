@@ -520,7 +520,7 @@ constexpr int kFew = 256;   // lists up to which every candidate is compared wit
 
 // A row's draws. CUT: slices have gone before. Rows are read again for each pass: held in registers they would leave room for one block a compute
 // unit, whose waits nothing hides (4096 x 64 001 bf16 with top-p: 898 us so held, 606 with three blocks).
-template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREADS, THREADS == 256 ? 4 : 6) void draw_row_kernel(const Draws p, const Slices s, const T* logits, int32_t* actions, float* logp) {
+template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void draw_row_kernel(const Draws p, const Slices s, const T* logits, int32_t* actions, float* logp) {
     constexpr int EACH = kTaserEach<T>, WAVES = THREADS / 64, STEP = THREADS * EACH;
     extern __shared__ uint64_t running_sums[];   // of the row's pieces, 64 lanes' each
     __shared__ uint64_t bins[kGapped], list[kListed];   // list: candidates around a threshold, {logit, number}
@@ -981,7 +981,7 @@ template <typename T> int launch(const Draws& p, int32_t type, const void* logit
     const int64_t pieces = (p.width + kTaserEach<T> - 1) / kTaserEach<T>;
     const int g = most <= 16 ? 16 : (most <= 32 ? 32 : 64), each = 256 / g;
     const bool cut = is_cut(p, type);
-    const int threads = most <= 64 || pieces <= 1024 ? 256 : 512;
+    const int threads = most <= 64 || pieces <= 1024 ? 256 : cut ? 1024 : 512;
     const int64_t blocks = most <= 64 ? (p.rows + each - 1) / each : p.rows;
     if (!taser_launch_fits(blocks, threads)) return taser_fail(TASER_E_RANGE, "policy_draw: too many rows for one launch");
     const unsigned grid = (unsigned)blocks, sums = (unsigned)((pieces + threads - 1) / threads * (threads / 64) * sizeof(uint64_t));
@@ -997,7 +997,7 @@ template <typename T> int launch(const Draws& p, int32_t type, const void* logit
         draw_tops_kernel<T><<<across, kSliceThreads, 0, stream>>>(p, s, (const T*)logits);
         draw_histogram_kernel<T><<<across, kSliceThreads, 0, stream>>>(p, s, (const T*)logits);
         draw_pieces_kernel<T><<<across, kSliceThreads, 0, stream>>>(p, s, (const T*)logits);
-        draw_row_kernel<T, 512, true><<<grid, 512, sums, stream>>>(p, s, (const T*)logits, actions, logp);
+        draw_row_kernel<T, 1024, true><<<grid, 1024, sums, stream>>>(p, s, (const T*)logits, actions, logp);
     } else if (threads == 256) {
         draw_row_kernel<T, 256, false><<<grid, 256, sums, stream>>>(p, Slices{}, (const T*)logits, actions, logp);
     } else {
