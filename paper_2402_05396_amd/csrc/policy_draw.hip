@@ -4,12 +4,12 @@
 // thresholds and draws do not depend on how a row is cut. Nothing is sorted: top-k and top-p keep the candidates above a value, and the first few
 // by index of those at it. The value is found by a histogram of counts (top-k) or weights (top-p) over 1024 bins of the distance to the largest
 // logit, and within a bin over the logits' bits, until a bin has one value: mostly at once. A draw finds its piece of the row in the
-// pieces' running sums, then its candidate in the piece. Lists of up to 256 around the threshold are ranked by comparing all pairs.
+// pieces' running sums, then its candidate in the piece. Short lists around the threshold are ranked by comparing all pairs.
 //
 // Rows of up to 64 candidates and draws: a part of a wave, a lane a candidate, whose rank comes from a look at every other one.
 // Longer rows: a block of 512 threads, three of them a compute unit; few of them: slices, four launches. Bound by the vector units: weights take some 20
 // instructions a candidate, twice where top-p looks for its threshold. 4096 x 64 001 bf16: top-p 0.95 570 us, top-k 50 with top-p 313, neither 292 (the
-// logits alone 102); 1 x 64 001 with both 20, 64 x 130 000 f32 with top-p 58.
+// logits alone 102); 1 x 64 001 with both 20, 64 x 130 000 f32 with top-p 54.
 #include "pieces.h"
 
 namespace {
@@ -337,6 +337,7 @@ __device__ inline Open open_by(const Rule& rule, bool number, const Found& found
     const bool all = number && (rule.top_p || found.upto <= kListed);
     return Open{all ? -1.f : (float)found.bin, (float)(found.bin + 1), all ? found.wanted : found.wanted - found.before, number, all};
 }
+
 // A row cut into slices, each a block's, for calls of few rows: the largest logit; the histogram; what is kept for sure and what is looked at. Each
 // is a launch: a block sees the others' results only in the next.
 struct Slices {
@@ -516,7 +517,9 @@ template <typename T> __global__ __launch_bounds__(kSliceThreads) void draw_piec
         if (base + i < kListed) w.list[base + i] = list[i];
 }
 
-constexpr int kFew = 256;   // lists up to which every candidate is compared with every other one
+// Lists in which every candidate is compared with every other one, 16 pairs a thread: up to 64, 90 or 128 in blocks of 256, 512 or 1024. Longer ones are settled
+// sooner by histograms (4096 x 4000 bf16, lists of 180: 88 us so, 159 by pairs; 2000 x 20 000, of 150: 84 and 101).
+constexpr int kFew = 128;
 
 // A row's draws. CUT: slices have gone before. Rows are read again for each pass: held in registers they would leave room for one block a compute
 // unit, whose waits nothing hides (4096 x 64 001 bf16 with top-p: 898 us so held, 606 with three blocks).
@@ -815,7 +818,7 @@ template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREAD
         select(true, visit, [&](float x, uint32_t c) { return x == limit ? ~c : 0u; }, [](float) { return (uint64_t)1; }, [&](uint64_t) { return at_limit; }, cut, before, wanted);
         cut = ~cut;
     };
-    if (open && listed && listed <= (uint32_t)kFew) {
+    if (open && listed && listed <= (uint32_t)kFew && listed * listed <= 16u * THREADS) {
         // How many lie before each of a short list, and what they weigh: all pairs, a part of them a thread.
         const int count = (int)listed, wide = (count + 63) & ~63, parts = THREADS / wide, mine = threadIdx.x % wide, part = threadIdx.x / wide, each_part = (count + parts - 1) / parts;
         const bool real = (int)threadIdx.x < count;
