@@ -622,7 +622,8 @@ int taser_policy_loss(const taser_policy_batch* p, float* loss, float* logp, voi
  * value, whatever the order, and the same call gives the same actions. A w
  * below 2^-44 counts as 0: such a candidate may be kept, but is never drawn.
  * Works in `work` (16-byte aligned, as much as taser_policy_draw_bytes says, 0
- * for many calls). Only launches kernels.
+ * for many calls). Only launches kernels; rows for which one would need 2^32
+ * threads (2^23 long ones) are refused.
  * ------------------------------------------------------------------------- */
 #define TASER_MAX_DRAW_WIDTH (1 << 20)
 
@@ -658,7 +659,7 @@ int taser_policy_draw(const taser_policy_draws* p, int32_t* actions, float* logp
  * taser_layer_norm_grad works in `work` (16-byte aligned, as much as
  * taser_layer_norm_grad_bytes says, none where dweight and dbias are NULL). Sums
  * are in 32 bits in a fixed order; out and the gradients are rounded once. Both
- * only launch kernels.
+ * only launch kernels; 2^22 rows of more than 8192 are refused.
  * ------------------------------------------------------------------------- */
 typedef struct taser_norm {
     int32_t type, weight_type;

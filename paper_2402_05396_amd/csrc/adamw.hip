@@ -5,7 +5,7 @@
 //
 // Moments in 32 bits: bound by memory, 16 bytes of them of the 22 to 28 that an element moves (100 M elements in bfloat16: 433 us, 5.1 TB/s). In 8
 // bits: 4.1 of 14 to 16, and some hundred vector instructions, which take as long (118 M elements, parameters in single precision, gradients in
-// bfloat16: 1.66 GB in 330 us, 5 TB/s).
+// bfloat16: 1.66 GB in 347 us, 4.8 TB/s).
 //
 // A launch takes up to kTensors tensors, their addresses among its arguments (nothing is copied to the device, so a captured call replays
 // as it is); a block finds its tensor by one comparison a lane. 48 tensors of 0.48 M elements in all: 6 us, and 8 for the host's call.
