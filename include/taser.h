@@ -696,12 +696,13 @@ int taser_layer_norm_grad(const taser_norm* n, const float* stats, const void* d
  *             has a code of 1 at least; moments whose unit would be below 2^-126,
  *             and a v below that, count as 0. Where a moment is not finite the
  *             unit, and so its whole block, is NaN.
- *   step      counts from 1; step_at: device int64, read in its place (NULL: none)
+ *   step      counts from 1; step_at: device int64, read in its place (NULL:
+ *             none), where it is below 1 the call changes nothing
  *   lr        >= 0; lr_at: device float, read in its place
  *   grad_scale  device float; where it is NaN the call changes nothing
  *   betas in [0, 1), eps and weight_decay >= 0
  * Memory that is written (param, m, v and units) must overlap neither other
- * tensors' nor a gradient: such calls are refused. Any number of tensors, at most
+ * tensors', a gradient nor a number that is read: such calls are refused. Any number of tensors, at most
  * 2^34 elements each; only launches kernels, one for every 56 tensors.
  *
  * taser_adamw_moments: 8-bit moments of one tensor as numbers of `type`, dense.

@@ -1044,7 +1044,7 @@ def _scalar_at(x, dtype, name, device):
 def adamw_step(params, grads, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, units=None, grad_scale=None, seed=0, stream=None):
     """taser_adamw_step: updates params, m and v (and units) in place. params: tensors of float32, float16 or bfloat16, on one device; grads: as many, of
     any of the three types, or None for a tensor that is to be left as it is; m, v, units as adamw_state made them (8 bits where units are
-    given). Tensors are contiguous. step: this one's number, from 1, or an int64 tensor that holds it; lr: a number or a float32 tensor;
+    given). Tensors are contiguous. step: this one's number, from 1, or an int64 tensor that holds it (below 1 nothing changes); lr: a number or a float32 tensor;
     grad_scale: a float32 tensor that gradients are multiplied by (where it is NaN nothing changes); seed: of the roundings to 8 bits.
     For groups of parameters with rates of their own, one call each. Autograd does not see that the parameters change."""
     params, grads, m, v = (x if isinstance(x, list) else list(x) for x in (params, grads, m, v))

@@ -82,7 +82,7 @@ __device__ inline bool find(const Launch& a, const Factors& given, int& tensor, 
     step = a.s.step_at ? *a.s.step_at : a.s.step;
     if (a.s.step_at || a.s.lr_at) f = factors_of(a.s, a.s.lr_at ? (double)*a.s.lr_at : a.s.lr, step);
     if (a.s.grad_scale) f.scale = *a.s.grad_scale;
-    return f.scale == f.scale;
+    return f.scale == f.scale && step >= 1;
 }
 
 __global__ __launch_bounds__(256) void adamw_kernel(const Launch a, const Factors given) {
@@ -310,6 +310,13 @@ int check(const taser_adamw* a, const taser_adamw_tensor* tensors, int64_t n) {
             add(5, t.v_unit, units, true);
         }
     }
+    // Blocks read these while others write.
+    const Span read[3] = {{(uintptr_t)a->step_at, (uintptr_t)a->step_at + 8, false}, {(uintptr_t)a->lr_at, (uintptr_t)a->lr_at + 4, false}, {(uintptr_t)a->grad_scale, (uintptr_t)a->grad_scale + 4, false}};
+    for (const Span& r : read)
+        if (r.from)
+            for (const auto& list : lists)
+                for (const Span& s : list)
+                    if (s.written && s.from < r.to && r.from < s.to) return taser_fail(TASER_E_ARG, "adamw_step: the step's number, the rate or the gradients' factor lies in memory that is written");
     if (overlap(lists, 6)) return taser_fail(TASER_E_ARG, "adamw_step: tensors overlap in memory");
     return TASER_OK;
 }

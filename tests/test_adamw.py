@@ -203,6 +203,19 @@ def test_a_factor_of_nan_changes_nothing(bits):
 
 @gpu
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("number", [0, -3])
+def test_a_step_on_the_device_below_1_changes_nothing(number, bits):
+    before = _case(bits, seed=5)
+    after = _copy(before)
+    _step(after, torch.tensor([number], device="cuda"))
+    for n in ("params", "m", "v"):
+        assert all(torch.equal(x, y) for x, y in zip(before[n], after[n]))
+    if bits == 8:
+        assert all(torch.equal(x, y) for u, w in zip(before["units"], after["units"]) for x, y in zip(u, w))
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
 def test_gradients_that_are_not_finite(bits):
     before = _case(bits, sizes=[1000], seed=6)
     before["grads"][0][[3, 700]] = torch.tensor([float("nan"), float("inf")], device="cuda")
@@ -340,6 +353,20 @@ def test_argument_errors_without_a_gpu():
     assert call(tensor=dict(elements=0)) == 0 and call(tensor=dict(grad=None)) == 0
     moments = lambda m=16, v=16, n=5, kind=0, out=16: L.taser_adamw_moments(m, v, 16, 16, n, kind, out, out, None)
     assert moments(m=None) == moments(v=None) == moments(n=-1) == moments(kind=3) == moments(out=None) == E_ARG and moments(n=2 ** 36) == E_RANGE and moments(n=0, m=None) == 0
+
+
+@pytest.mark.parametrize("name, size", [("step_at", 8), ("lr_at", 4), ("grad_scale", 4)])
+def test_numbers_that_lie_in_what_is_written_are_refused(name, size):
+    """Found without a GPU: the call is refused before anything is launched."""
+    starts, units = (0x1000, 0x3000, 0x4000), (0x100, 0x200)   # of 10 elements' parameters, m and v; of a unit each
+    for bits in (32, 8):
+        ends = (40, 40 if bits == 32 else 10, 40 if bits == 32 else 10) + (4, 4)
+        for at, length in list(zip(starts + units, ends))[:3 if bits == 32 else 5]:
+            for place in (at, at + length - 1, at - size + 1):
+                a = T._Adamw(bits, 1, None, 1e-3, 0.9, 0.999, 1e-8, 0.01, None, None, 0)
+                setattr(a, name, place)
+                t = (T._AdamwTensor * 1)(T._AdamwTensor(0, 0, 10, 0x1000, 0x2000, 0x3000, 0x4000, 0x100, 0x200))
+                assert T.lib().taser_adamw_step(ctypes.byref(a), t, 1, None) == -1 and "that is written" in T.last_error(), (bits, hex(place))
 
 
 def test_the_oracle_against_another_form_of_the_step():
