@@ -150,20 +150,22 @@ def policy_loss(logits, actions, advantage, kind, old=None, ref=None, count=None
     return {"loss": loss, "logp": logp, "grad": grad}, {"loss": eloss, "logp": elogp, "grad": egrad}
 
 
-def layer_norm(x, kind, weight=None, bias=None, eps=1e-5, dout=None, kept=None):
-    """x, dout float64 [R, W]; kept: the weights' kind, kind unless given -> (results, bounds) of out and, with `dout`, dx, dweight, dbias.
-    The operator's sums are in 32 bits; out and the gradients are rounded to their types once."""
+def layer_norm(x, kind, weight=None, bias=None, eps=1e-5, dout=None, kept=None, depth=None):
+    """x, dout float64 [R, W]; kept: the weights' kind, kind unless given -> (results, bounds) of out, the statistics mean and rstd [R, 1] and, with `dout`,
+    dx, dweight, dbias. The operator's sums are in 32 bits; out and the gradients are rounded to their types once. depth: how many additions
+    a number goes through at most, in a row's sums and in those over the rows (unless given: as many as there are numbers, which says least)."""
     R, W = x.shape
+    across, down = (W, R) if depth is None else depth
     u, tiny = U[kind], TINY[kind]
     u2, tiny2 = U[kept or kind], TINY[kept or kind]
     w = np.ones(W) if weight is None else weight
     b = np.zeros(W) if bias is None else bias
     mean = x.mean(1, keepdims=True)
     away = x - mean
-    em = (W + 4) * E32 * np.abs(x).mean(1, keepdims=True) + E32 * np.abs(mean)
+    em = (across + 4) * E32 * np.abs(x).mean(1, keepdims=True) + E32 * np.abs(mean)
     ea = em + E32 * np.abs(away)
     var = (away ** 2).mean(1, keepdims=True) + eps
-    evar = (2 * np.abs(away) * ea + ea ** 2).mean(1, keepdims=True) + (W + 8) * E32 * var
+    evar = (2 * np.abs(away) * ea + ea ** 2).mean(1, keepdims=True) + (across + 8) * E32 * var
     rstd = var ** -0.5
     part = np.minimum(evar / var, 0.99)
     er = rstd * ((1 - part) ** -0.5 - 1 + 4 * E32)
@@ -171,20 +173,20 @@ def layer_norm(x, kind, weight=None, bias=None, eps=1e-5, dout=None, kept=None):
     ex = ea * (rstd + er) + np.abs(away) * er + 2 * E32 * np.abs(xhat)
     out = xhat * w + b
     eo = ex * np.abs(w) + 4 * E32 * (np.abs(xhat * w) + np.abs(b))
-    res, off = {"out": out}, {"out": eo + u * (np.abs(out) + eo) + tiny}
+    res, off = {"out": out, "mean": mean, "rstd": rstd}, {"out": eo + u * (np.abs(out) + eo) + tiny, "mean": em, "rstd": er}
     if dout is None:
         return res, off
     g = dout * w
     s, t = g.mean(1, keepdims=True), (g * xhat).mean(1, keepdims=True)
-    es = (W + 6) * E32 * np.abs(g).mean(1, keepdims=True)
-    et = (np.abs(g) * ex).mean(1, keepdims=True) + (W + 8) * E32 * np.abs(g * xhat).mean(1, keepdims=True)
+    es = (across + 6) * E32 * np.abs(g).mean(1, keepdims=True)
+    et = (np.abs(g) * ex).mean(1, keepdims=True) + (across + 8) * E32 * np.abs(g * xhat).mean(1, keepdims=True)
     inner = g - s - xhat * t
     ei = 4 * E32 * (np.abs(g) + np.abs(s) + np.abs(xhat * t)) + es + ex * (np.abs(t) + et) + np.abs(xhat) * et
     dx = rstd * inner
     ed = (rstd + er) * ei + er * np.abs(inner) + 2 * E32 * np.abs(dx)
     dweight, dbias = (dout * xhat).sum(0), dout.sum(0)
-    ew = (np.abs(dout) * ex).sum(0) + (R + 8) * E32 * np.abs(dout * xhat).sum(0)
-    eb = (R + 8) * E32 * np.abs(dout).sum(0)
+    ew = (np.abs(dout) * ex).sum(0) + (down + 8) * E32 * np.abs(dout * xhat).sum(0)
+    eb = (down + 8) * E32 * np.abs(dout).sum(0)
     res.update(dx=dx, dweight=dweight, dbias=dbias)
     off.update(dx=ed + u * (np.abs(dx) + ed) + tiny, dweight=ew + u2 * (np.abs(dweight) + ew) + tiny2, dbias=eb + u2 * (np.abs(dbias) + eb) + tiny2)
     return res, off

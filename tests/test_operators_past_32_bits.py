@@ -68,3 +68,24 @@ def test_adamw(bits):
         a = T.adamw_moments(m[0], v[0], (units[0][0], units[1][0]), dtype=torch.bfloat16)
         b = T.adamw_moments(m[0][-tail:].clone(), v[0][-tail:].clone(), tuple(u[0][-(-(-tail // 256)):].clone() for u in units), dtype=torch.bfloat16)
         assert all(torch.equal(x[-tail:], y) for x, y in zip(a, b)) and a[1][-tail:].all()
+
+
+def test_layer_norms_sums_over_the_last_rows():
+    """Only rows past the border have a gradient: dbias is their sum of whole numbers, exactly, and dweight a sum of 300 products that are off by
+    four roundings each (what is away from the mean, its reciprocal deviation, the product, the sum so far)."""
+    W, few = 8192, 300
+    R = MORE // W + few
+    x = _filled(R, W)
+    weight, bias = torch.randn(W, device="cuda"), torch.randn(W, device="cuda")
+    out, stats = T.layer_norm(x, weight, bias, want_stats=True)
+    del out
+    dout = torch.zeros((R, W), dtype=torch.bfloat16, device="cuda")
+    dout[-few:] = torch.randint(-3, 4, (few, W), generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    dx, dweight, dbias = T.layer_norm_grad(dout, x, stats, weight, bias)
+    assert not dx[:-few].any() and dx[-few:].any(1).all()
+    tail = dout[-few:].double()
+    assert torch.equal(dbias.double(), tail.sum(0))
+    each = tail * (x[-few:].double() - stats[-few:, :1].double()) * stats[-few:, 1:].double()
+    assert ((dweight.double() - each.sum(0)).abs() <= (few + 4) * 2.0 ** -24 * each.abs().sum(0)).all()
+    lost = (each[0].abs() > (few + 4) * 2.0 ** -24 * each.abs().sum(0)).float().mean()   # of one row: seen wherever its gradient is not 0
+    assert lost > 0.8
