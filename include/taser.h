@@ -693,9 +693,10 @@ int taser_layer_norm_grad(const taser_norm* n, const float* stats, const void* d
  *             expectation exact; r: 16 bits, 16 * (e % 2) of word e % 8 / 2 of Philox
  *             4x32-10 with key `seed` and counter (e / 8, the tensor's place in the
  *             list, step, 0x4144414D), e the element's index. A v that is not 0
- *             has a code of 1 at least; moments whose unit would be below 2^-126,
- *             and a v below that, count as 0. Where a moment is not finite the
- *             unit, and so its whole block, is NaN.
+ *             has a code of 1 at least; moments whose unit would be below 2^-126
+ *             count as 0, and so does a v below that where eps outweighs its
+ *             root (eps >= 2^-39 / sqrt(1 - beta2)). Where a moment is not finite
+ *             the unit, and so its whole block, is NaN.
  *   step      counts from 1; step_at: device int64, read in its place (NULL:
  *             none), where it is below 1 the call changes nothing
  *   lr        >= 0; lr_at: device float, read in its place

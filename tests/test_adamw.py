@@ -404,3 +404,35 @@ def test_the_oracles_random_words(golden_dir):
         numbers = [int(x, 16) for x in row[-10:]]
         got = O.philox([np.array([x]) for x in numbers[:4]], numbers[4:6])
         assert [int(x[0]) for x in got] == numbers[6:]
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-16, 1e-12])
+def test_small_gradients_beside_a_small_eps(bits, eps):
+    """Second moments below 2^-126 count where eps does not outweigh them. The first step, from moments of zero: m / sqrt(v) is 0.1 / sqrt(0.001) of the gradient's sign. In 32
+    bits (1 - beta2) g^2 is off by 2^-24 of itself twice and by half the spacing of the smallest numbers, 2^-150, of either product; its root has half of that."""
+    g = torch.Generator().manual_seed(12)
+    for size in (1e-18, 1e-19, 3e-17, 1e-15, 1e-3):
+        grad = ((0.5 + torch.rand(700, generator=g)) * (1 - 2.0 * torch.randint(0, 2, (700,), generator=g)) * size).cuda()
+        p = [torch.zeros(700, device="cuda")]
+        m, v, units = T.adamw_state(p, bits)
+        T.adamw_step(p, [grad], m, v, 1, lr=0.01, eps=eps, weight_decay=0.0, units=units)
+        x, e = _arr(grad), float(np.float32(eps))
+        root = np.abs(x)   # of v / c2
+        off = root * ((2 * O.E32 * 0.001 * x * x + 2.0 ** -150 * 1.001) / (0.001 * x * x) + 6 * O.E32)
+        want = -0.01 * x / (root + e)
+        far = np.abs(_arr(p[0]) - want) - np.abs(want) * (off / (root + e - off) + 12 * O.E32)
+        assert (far <= 0).all(), (size, float(far.max()), float(want[0]), p[0][0].item())
+
+
+@gpu
+def test_small_gradients_for_some_steps_in_8_bits():
+    """Equal gradients of 1e-18 or 1e-16 and an eps of 0: m / sqrt(v) is theirs' sign at each step, so that a parameter moves by lr. Every moment is its block's
+    largest, kept as its unit: three roundings a step of m, of v's root no more, and v's own of 2^-149 of some 1e-39 at first."""
+    for size in (1e-18, 1e-16):
+        p = [torch.zeros(600, device="cuda")]
+        m, v, units = T.adamw_state(p, 8)
+        for step in range(1, 6):
+            T.adamw_step(p, [torch.full((600,), size, device="cuda")], m, v, step, lr=0.01, eps=0.0, weight_decay=0.0, units=units)
+        assert (p[0].double() + 0.05).abs().max() <= 0.05 * (5 * 12 * O.E32 + 5 * 2.0 ** -149 / 1e-39), size
