@@ -701,7 +701,8 @@ int taser_layer_norm_grad(const taser_norm* n, const float* stats, const void* d
  *             none), where it is below 1 the call changes nothing
  *   lr        >= 0; lr_at: device float, read in its place
  *   grad_scale  device float; where it is NaN the call changes nothing
- *   betas in [0, 1), eps and weight_decay >= 0
+ *   betas in [0, 1), weight_decay >= 0, eps >= 0 (one below 2^-126 counts as
+ *             2^-126; 0: an element whose v is 0 in 32 bits is divided by 0)
  * Memory that is written (param, m, v and units) must overlap neither other
  * tensors', a gradient nor a number that is read: such calls are refused. Any number of tensors, at most
  * 2^34 elements each; only launches kernels, one for every 56 tensors.

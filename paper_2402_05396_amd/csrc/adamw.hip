@@ -342,7 +342,8 @@ extern "C" int taser_adamw_step(const taser_adamw* a, const taser_adamw_tensor* 
     l.s.b1_rest = (float)(1. - a->beta1);
     l.s.b2 = (float)a->beta2;
     l.s.b2_rest = (float)(1. - a->beta2);
-    l.s.eps = (float)a->eps;
+    // v_rcp_f32 of a number below 2^-126 may be infinite, and a moment of 0 times that NaN. No root but 0 is below 2^-75: beside the others a raised eps is nothing.
+    l.s.eps = a->eps > 0. ? std::max((float)a->eps, 0x1p-126f) : 0.f;
     l.s.step = a->step;
     l.s.step_at = a->step_at;
     l.s.lr_at = a->lr_at;

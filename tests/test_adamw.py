@@ -436,3 +436,18 @@ def test_small_gradients_for_some_steps_in_8_bits():
         for step in range(1, 6):
             T.adamw_step(p, [torch.full((600,), size, device="cuda")], m, v, step, lr=0.01, eps=0.0, weight_decay=0.0, units=units)
         assert (p[0].double() + 0.05).abs().max() <= 0.05 * (5 * 12 * O.E32 + 5 * 2.0 ** -149 / 1e-39), size
+
+
+@gpu
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-40, 2.0 ** -149, 1e-38, 1e-37])
+def test_an_eps_at_the_end_of_the_numbers(bits, eps):
+    """Elements without a gradient so far stay as they are (0 / eps), the others move by lr."""
+    p = [torch.ones(300, device="cuda")]
+    grad = torch.zeros(300, device="cuda")
+    grad[::3] = 0.5
+    m, v, units = T.adamw_state(p, bits)
+    for step in (1, 2):
+        T.adamw_step(p, [grad], m, v, step, lr=0.01, eps=eps, weight_decay=0.0, units=units)
+    assert (p[0][1::3] == 1).all() and (p[0][2::3] == 1).all()
+    assert (p[0][::3] - 0.98).abs().max() <= 0.02 * 24 * O.E32 + 4 * O.E32
