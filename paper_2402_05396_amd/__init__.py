@@ -922,7 +922,7 @@ def _draw_block(logits, uniform, temperature, top_k, top_p, min_p, count):
         if isinstance(x, torch.Tensor):
             setattr(p, "row_" + name, _rows_of(x, dtype, rows, name, logits.device))
         else:
-            setattr(p, name, x if name != "top_k" else min(x, 2 ** 31 - 1))
+            setattr(p, name, x if name != "top_k" else max(min(x, 2 ** 31 - 1), -1))   # (ctypes would take its low 32 bits)
     if count is not None:
         p.count = _rows_of(count, torch.int32, rows, "count", logits.device)
     return p
@@ -1082,6 +1082,8 @@ def adamw_step(params, grads, m, v, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1
     if isinstance(step, torch.Tensor):
         a.step_at = _scalar_at(step, torch.int64, "step", device)
     else:
+        if not -2 ** 63 <= step < 2 ** 63:   # (ctypes would take its low 64 bits)
+            raise ValueError("step: expected a number of 64 bits")
         a.step = step
     if isinstance(lr, torch.Tensor):
         a.lr_at = _scalar_at(lr, torch.float32, "lr", device)

@@ -451,3 +451,19 @@ def test_an_eps_at_the_end_of_the_numbers(bits, eps):
         T.adamw_step(p, [grad], m, v, step, lr=0.01, eps=eps, weight_decay=0.0, units=units)
     assert (p[0][1::3] == 1).all() and (p[0][2::3] == 1).all()
     assert (p[0][::3] - 0.98).abs().max() <= 0.02 * 24 * O.E32 + 4 * O.E32
+
+
+@gpu
+def test_a_step_past_64_bits_is_refused(monkeypatch):
+    for native in (True, False):
+        with monkeypatch.context() as change:
+            if not native:
+                change.setattr(T, "_native", Absent())
+            p, g = [torch.zeros(5, device="cuda")], [torch.ones(5, device="cuda")]
+            m, v, _ = T.adamw_state(p)
+            for step in (2 ** 63, 2 ** 64 + 1, -2 ** 64 + 1, -2 ** 63 - 1):
+                with pytest.raises(ValueError):
+                    T.adamw_step(p, g, m, v, step)
+            assert not p[0].any() and not m[0].any()
+            T.adamw_step(p, g, m, v, 2 ** 63 - 1)
+            assert p[0].all()

@@ -329,3 +329,19 @@ def test_the_oracle_by_hand():
     assert near(kept(temperature=0.0), {4: 1.0}) and near(kept(top_p=0.0), {4: 1.0})
     assert abs(O.policy_draw(x, np.array([[0.0]]), temperature=0.0)[1][0, 0] - np.log(0.4)) < 1e-12
     assert O.policy_draw(x, np.array([[0.3]]), count=[0])[0][0, 0] == -1
+
+
+@gpu
+def test_a_top_k_past_32_bits(monkeypatch):
+    """Below 0 it is refused, however far; above, it keeps all."""
+    x, u = torch.randn((3, 40), generator=torch.Generator().manual_seed(0)).cuda(), torch.rand((3, 5), generator=torch.Generator().manual_seed(1)).cuda()
+    want = T.policy_draw(x, u)
+    for native in (True, False):
+        with monkeypatch.context() as change:
+            if not native:
+                change.setattr(T, "_native", Absent())
+            for k in (-1, -2 ** 31, -2 ** 31 - 1, -2 ** 32, -2 ** 32 + 5, -2 ** 64 + 1):
+                with pytest.raises(T.TaserError):
+                    T.policy_draw(x, u, top_k=k)
+            for k in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 2 ** 64):
+                assert all(torch.equal(a, b) for a, b in zip(T.policy_draw(x, u, top_k=k), want)), k
