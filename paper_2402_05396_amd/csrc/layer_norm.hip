@@ -9,8 +9,8 @@
 // through LDS, a second launch the blocks', in an order that the sizes fix. Rows of more than 8192 are a block's each, held in registers up to 32768
 // and read again for each pass past that, and their dweight and dbias come from a kernel of their own, by columns.
 //
-// 8192 x 5120 bf16, the answer: 34 us (168 MB at 4.9 TB/s; 5120 is five waves' 1024 columns each: with groups of powers of two 50). 16 384 x 4096 bf16: 48 and,
-// for the gradient, 101 + 5 us (4.1 TB/s; two blocks of eight waves a compute unit are what its registers leave, and 17 MB of parts are written and read).
+// 8192 x 5120 bf16, the answer: 33 us (168 MB at 5.1 TB/s; 5120 is five waves' 1024 columns each: with groups of powers of two 50). 16 384 x 4096 bf16: 48 and,
+// for the gradient, 100 + 5 us (4.1 TB/s; two blocks of eight waves a compute unit are what its registers leave, and 17 MB of parts are written and read).
 // 12 000 x 100 f32: 5.5 and 7 + 3.5 us: three launches. One row of 4096: 4 us.
 #include "pieces.h"
 
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(const Norm p, int wa
     const int64_t groups = (int64_t)gridDim.x * here, turns = (p.rows + groups - 1) / groups;
     float weight[HELD][EACH], dweight[HELD][EACH] = {}, dbias[HELD][EACH] = {};
     load_weights<T, HELD>(p.weight, p.weight_type, threads, lane, p.width, 1.f, weight);
-    // Two rows ahead of the one at hand are on their way (16 384 x 4096 bf16: 100 us with one).
+    // Two rows ahead of the one at hand are on their way. (One does as well: 16 384 x 4096 bf16 100 to 101 us with either, 12 000 x 100 f32 and its join 10.0.)
     TaserPiece<T> next_x[2][HELD], next_y[2][HELD];
     float2 next_stats[2];
     int64_t row = (int64_t)blockIdx.x * here + mine;

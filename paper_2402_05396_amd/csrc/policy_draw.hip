@@ -8,8 +8,8 @@
 //
 // Rows of up to 64 candidates and draws: a part of a wave, a lane a candidate, whose rank comes from a look at every other one.
 // Longer rows: a block of 512 threads, three of them a compute unit; few of them: slices, four launches. Bound by the vector units: weights take some 20
-// instructions a candidate, twice where top-p looks for its threshold. 4096 x 64 001 bf16: top-p 0.95 570 us, top-k 50 with top-p 313, neither 292 (the
-// logits alone 102); 1 x 64 001 with both 20, 64 x 130 000 f32 with top-p 54.
+// instructions a candidate, twice where top-p looks for its threshold. 4096 x 64 001 bf16: top-p 0.95 555 us, top-k 50 with top-p 318, neither 281, the largest
+// 183 (the logits alone 102); 1 x 64 001 with both 20, 64 x 130 000 f32 with top-p 53. (All on a card at its clock: the first 25 ms after a rest take up to a quarter more.)
 #include "pieces.h"
 
 namespace {
@@ -522,7 +522,8 @@ template <typename T> __global__ __launch_bounds__(kSliceThreads) void draw_piec
 constexpr int kFew = 128;
 
 // A row's draws. CUT: slices have gone before. Rows are read again for each pass: held in registers they would leave room for one block a compute
-// unit, whose waits nothing hides (4096 x 64 001 bf16 with top-p: 898 us so held, 606 with three blocks).
+// unit, whose waits nothing hides (4096 x 64 001 bf16 with top-p, with the rest as it was then: 898 us so held, 606 with three blocks, which are 555 now). Three blocks
+// leave 80 registers: 112 bytes a lane of a 16-bit row are spilled, 60 of a float32 one; the other sizes of block spill 48 in 16 bits, where the last loop's load is a call.
 template <typename T, int THREADS, bool CUT> __global__ __launch_bounds__(THREADS, THREADS == 512 ? 6 : 4) void draw_row_kernel(const Draws p, const Slices s, const T* logits, int32_t* actions, float* logp) {
     constexpr int EACH = kTaserEach<T>, WAVES = THREADS / 64, STEP = THREADS * EACH;
     extern __shared__ uint64_t running_sums[];   // of the row's pieces, 64 lanes' each
